@@ -172,6 +172,66 @@ fdd_status fdd_prefix_pack(const void *prefix_v, int32_t L, int32_t Hkv, int32_t
                            void *packed, size_t packed_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * A prefix cache in 8 bits.
+ *
+ * K and V of the shared prefix as e4m3 codes (4 bits of exponent, 3 of mantissa, largest value 448, no
+ * infinities) with one scale for every FDD_QUANT_BLOCK rows of a KV head: half the bytes of bf16.  The
+ * value of an element is code * scale.  A scale is a power of two, the smallest one that brings the largest
+ * magnitude of its rows to 448 or less, but at least 2^-117 and at most 2^119.  Scaling is therefore exact:
+ * an element is rounded once, to the nearest code and to even on ties (relative error 2^-4 at most, 2^-10
+ * of the scale for codes below 2^-6), and its value is exact in bf16 and fp32.
+ *
+ * A head's rows lie together, so that the tile of FDD_QUANT_BLOCK keys that attention works on is one
+ * piece of memory.  Rows behind the last one written, and their scales, are never used.
+ */
+#define FDD_QUANT_BLOCK 64
+typedef struct fdd_quant_cache {
+    void *k;                       /* [Hkv,capacity,D] e4m3 */
+    void *v;                       /* [Hkv,capacity,D] e4m3 */
+    float *k_scale;                /* [Hkv,capacity/FDD_QUANT_BLOCK] */
+    float *v_scale;
+    int32_t Hkv, D;                /* D 64 or 128 */
+    int32_t capacity;              /* rows allocated per head, a multiple of FDD_QUANT_BLOCK */
+    int32_t reserved;              /* must be 0 */
+    int64_t batch_stride;          /* fdd_block_attn_quant with batch > 1: elements from one problem's codes to the next's */
+    int64_t scale_batch_stride;    /* likewise scales */
+} fdd_quant_cache;
+
+/* Rows of K and V in their own precision: the source of fdd_prefix_quantize, the destination of
+ * fdd_prefix_dequantize. */
+typedef struct fdd_quant_rows {
+    void *k;                       /* [rows,Hkv,D], consecutive rows k_row_stride apart; only read by fdd_prefix_quantize */
+    void *v;
+    int64_t k_row_stride;          /* elements; at least Hkv*D, rows 16-byte aligned; 0 = Hkv*D */
+    int64_t v_row_stride;
+    int32_t rows;                  /* may be 0 */
+    int32_t dtype;                 /* fdd_dtype */
+} fdd_quant_rows;
+
+/* fdd_prefix_quantize: the rows become rows [row0, row0 + rows) of the cache, which then ends with them: a
+ * prompt (row0 = 0), or a finished block behind the rows that are there (row0 = their number).  Where row0
+ * lies inside a block of the cache, the block's scale may grow: the rows in front are then rounded again,
+ * to the codes of the new scale (exact, except for codes that fall below 2^-6), else they are left as they
+ * are.  It does not shrink.  Codes behind row0 + rows and scales of later blocks are left as they were.
+ * Values: an infinity or a magnitude above 448 * 2^119 is stored as the largest code, a NaN as a NaN;
+ * infinities and NaN have no part in the scale.  The source must not overlap the cache.
+ *
+ * fdd_prefix_dequantize: rows [row0, row0 + rows) of the cache are read back, exactly. */
+fdd_status fdd_prefix_quantize(const fdd_quant_cache *cache, int32_t row0, const fdd_quant_rows *src, void *stream);
+fdd_status fdd_prefix_dequantize(const fdd_quant_cache *cache, int32_t row0, const fdd_quant_rows *dst, void *stream);
+
+/* fdd_block_attn_quant: fdd_block_attn with the prefix in a cache of 8 bits.  `p` as for fdd_block_attn,
+ * except that prefix_k, prefix_v and prefix_v_packed are NULL (prefix_batch_stride and packed_batch_stride
+ * are ignored): the L keys and values of the prefix are rows [0, L) of `cache`, L <= cache->capacity,
+ * converted without an error.  Queries, blocks, extensions and outputs are of type p->dtype.  The result is
+ * that of fdd_block_attn on the rows as fdd_prefix_dequantize returns them, up to the order of sums.
+ * `cache` may be NULL iff L == 0.  The workspace is fdd_block_attn_quant_workspace(p): more than that of
+ * fdd_block_attn where the call converts the prefix once, for all of its workgroups, instead of tile by
+ * tile.  Values and q_positions as with fdd_block_attn; a NaN in the cache is a NaN. */
+size_t fdd_block_attn_quant_workspace(const fdd_attn_params *p);
+fdd_status fdd_block_attn_quant(const fdd_attn_params *p, const fdd_quant_cache *cache);
+
+/* ------------------------------------------------------------------------
  * fdd_unmask_step: one confidence-threshold unmask iteration over N blocks.
  *
  * A position (n,b) is eligible when mask[n,b] == 1 and scaffold_mask[n,b]
@@ -306,6 +366,47 @@ typedef struct fdd_verify_params {
  * `temperature`: the greedy verifier cuts a row into more pieces than the sampled one. */
 size_t fdd_verify_workspace(const fdd_verify_params *p);
 fdd_status fdd_verify_step(const fdd_verify_params *p);
+
+/* ------------------------------------------------------------------------
+ * fdd_token_logprobs: what a row of logits says about a token, without a sample or a decision.
+ *
+ * With p = softmax(logits[n,b,:] / temperature), for every selected position (row_mask NULL, or
+ * row_mask[n,b] == 1):
+ *     logprobs[n,b]       = ln p[tokens[n,b]]; -inf for a token outside [0, V)
+ *     entropy[n,b]        = -sum_v p[v] ln p[v]   (nats; entries of probability 0 contribute nothing)
+ *     top_ids[n,b,0..top) = the ids of the `top` largest logits, largest first, the lowest id first among
+ *                           equal ones; top_logprobs their ln p
+ * Positions that are not selected keep what their outputs held, and their logits are not read.  An output
+ * that is NULL is not computed (top_ids and top_logprobs both or neither).
+ *
+ * The sums run in fp32 over pieces of a row, which are joined in fp64; the largest term is kept out of the
+ * sum and joins in ln(1 + rest), so that the log probability of a token that is nearly certain keeps its
+ * digits.  Logits: finite values, and -inf for entries that can never be chosen.  A row without a
+ * finite entry has no softmax: its logprobs, entropy and top_logprobs are NaN, its top_ids 0..top-1.  NaN and
+ * +inf are not supported: such a row's outputs are undefined (nothing is read or written out of bounds).
+ */
+#define FDD_LOGPROBS_MAX_TOP 32
+typedef struct fdd_logprob_params {
+    int32_t N, B;
+    int64_t V;
+    int32_t dtype;                 /* fdd_dtype of logits */
+    int32_t top;                   /* 0 .. min(V, FDD_LOGPROBS_MAX_TOP) */
+    float temperature;             /* positive and finite */
+    int32_t reserved;              /* must be 0 */
+    const void *logits;            /* [N,B,V] */
+    const int32_t *tokens;         /* [N,B]; may be NULL iff logprobs is */
+    const uint8_t *row_mask;       /* [N,B], 1 = selected; may be NULL (= all) */
+    float *logprobs;               /* [N,B] out; may be NULL */
+    float *entropy;                /* [N,B] out; may be NULL */
+    int32_t *top_ids;              /* [N,B,top] out; may be NULL */
+    float *top_logprobs;           /* [N,B,top] out; may be NULL */
+    void *workspace;               /* >= fdd_token_logprobs_workspace() bytes */
+    size_t workspace_bytes;
+    void *stream;
+} fdd_logprob_params;
+
+size_t fdd_token_logprobs_workspace(const fdd_logprob_params *p);
+fdd_status fdd_token_logprobs(const fdd_logprob_params *p);
 
 /* ------------------------------------------------------------------------
  * Rollout-fork bookkeeping ("fork the KV cache N times").

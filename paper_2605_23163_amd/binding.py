@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import Any, NamedTuple
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libfdd.so")
@@ -18,7 +19,11 @@ _marshal = None       # native argument marshalling of the two calls of a denois
 
 FDD_F32, FDD_BF16 = 0, 1
 FDD_ATTN_CAUSAL_BLOCK = 1
+FDD_QUANT_BLOCK = 64
+FDD_LOGPROBS_MAX_TOP = 32
 EXPORTS = ("fdd_block_attn_workspace", "fdd_block_attn", "fdd_prefix_pack_bytes", "fdd_prefix_pack",
+           "fdd_prefix_quantize", "fdd_prefix_dequantize", "fdd_block_attn_quant_workspace", "fdd_block_attn_quant",
+           "fdd_token_logprobs_workspace", "fdd_token_logprobs",
            "fdd_unmask_workspace", "fdd_unmask_step", "fdd_unmask_step_static", "fdd_verify_workspace", "fdd_verify_step",
            "fdd_fork_block", "fdd_block_kv_update", "fdd_block_commit", "fdd_traj_mean", "fdd_profile_attn_events", "fdd_last_error", "fdd_version")
 
@@ -41,6 +46,25 @@ class AttnParams(C.Structure):
                 ("q_batch_stride", C.c_int64), ("prefix_batch_stride", C.c_int64), ("block_batch_stride", C.c_int64),
                 ("ext_batch_stride", C.c_int64), ("out_batch_stride", C.c_int64), ("packed_batch_stride", C.c_size_t),
                 ("q_positions", C.c_void_p)]
+
+
+class QuantCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("Hkv", C.c_int32), ("D", C.c_int32), ("capacity", C.c_int32), ("reserved", C.c_int32),
+                ("batch_stride", C.c_int64), ("scale_batch_stride", C.c_int64)]
+
+
+class QuantRows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_row_stride", C.c_int64), ("v_row_stride", C.c_int64),
+                ("rows", C.c_int32), ("dtype", C.c_int32)]
+
+
+class LogprobParams(C.Structure):
+    _fields_ = [("N", C.c_int32), ("B", C.c_int32), ("V", C.c_int64), ("dtype", C.c_int32), ("top", C.c_int32),
+                ("temperature", C.c_float), ("reserved", C.c_int32), ("logits", C.c_void_p), ("tokens", C.c_void_p),
+                ("row_mask", C.c_void_p), ("logprobs", C.c_void_p), ("entropy", C.c_void_p), ("top_ids", C.c_void_p),
+                ("top_logprobs", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+                ("stream", C.c_void_p)]
 
 
 class UnmaskParams(C.Structure):
@@ -118,6 +142,18 @@ def load_library():
         lib.fdd_prefix_pack.restype = C.c_int
         lib.fdd_prefix_pack.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t,
                                         C.c_void_p]
+        lib.fdd_prefix_quantize.restype = C.c_int
+        lib.fdd_prefix_quantize.argtypes = [C.POINTER(QuantCache), C.c_int32, C.POINTER(QuantRows), C.c_void_p]
+        lib.fdd_prefix_dequantize.restype = C.c_int
+        lib.fdd_prefix_dequantize.argtypes = [C.POINTER(QuantCache), C.c_int32, C.POINTER(QuantRows), C.c_void_p]
+        lib.fdd_block_attn_quant_workspace.restype = C.c_size_t
+        lib.fdd_block_attn_quant_workspace.argtypes = [C.POINTER(AttnParams)]
+        lib.fdd_block_attn_quant.restype = C.c_int
+        lib.fdd_block_attn_quant.argtypes = [C.POINTER(AttnParams), C.POINTER(QuantCache)]
+        lib.fdd_token_logprobs_workspace.restype = C.c_size_t
+        lib.fdd_token_logprobs_workspace.argtypes = [C.POINTER(LogprobParams)]
+        lib.fdd_token_logprobs.restype = C.c_int
+        lib.fdd_token_logprobs.argtypes = [C.POINTER(LogprobParams)]
         lib.fdd_unmask_workspace.restype = C.c_size_t
         lib.fdd_unmask_workspace.argtypes = [C.POINTER(UnmaskParams)]
         lib.fdd_unmask_step.restype = C.c_int
@@ -232,16 +268,20 @@ def _set_workspace(p, workspace, query, device, stream):
 
 
 def _attn_params(q, prefix_k, prefix_v, block_k, block_v, scaffold_mask, out, scale, splits, prefix_v_packed=None,
-                 causal_block=False, ext_k=None, ext_v=None, E=0):
+                 causal_block=False, ext_k=None, ext_v=None, E=0, L=None):
+    """``L``: the prefix is in a cache of 8 bits, whose first L rows it is (prefix_k and prefix_v are None)."""
     N, B, Hq, D = q.shape
-    ks, bs, dt = prefix_k.shape, block_k.shape, q.dtype
-    L, Hkv = ks[0], bs[2]
-    if ks[1:] != (Hkv, D) or prefix_v.shape != ks:
-        raise ValueError("prefix_k / prefix_v must be [L,Hkv,D]")
+    bs, dt = block_k.shape, q.dtype
+    Hkv = bs[2]
+    if prefix_k is not None:
+        ks = prefix_k.shape
+        L = ks[0]
+        if ks[1:] != (Hkv, D) or prefix_v.shape != ks:
+            raise ValueError("prefix_k / prefix_v must be [L,Hkv,D]")
     if bs != (N, B, Hkv, D) or block_v.shape != bs:
         raise ValueError("block_k / block_v must be [N,B,Hkv,D]")
     code = _dtype_code(q)
-    if prefix_k.dtype != dt or prefix_v.dtype != dt or block_k.dtype != dt or block_v.dtype != dt:
+    if prefix_k is not None and (prefix_k.dtype != dt or prefix_v.dtype != dt) or block_k.dtype != dt or block_v.dtype != dt:
         raise TypeError("q, k and v must share one element type")
     p = AttnParams(N, B, L, Hq, Hkv, D, code, 0.0 if scale is None else float(scale), _dev(q, "q"),
                    _dev(prefix_k, "prefix_k") if L > 0 else None, _dev(prefix_v, "prefix_v") if L > 0 else None,
@@ -318,7 +358,7 @@ def fdd_block_attn(q, prefix_k, prefix_v, block_k, block_v, scaffold_mask=None, 
     return out
 
 
-def _batched_params(q, prefix_k, prefix_v, block_k, block_v, out, scale, splits, prefix_v_packed, causal_block, ext_k, ext_v, E):
+def _batched_params(q, prefix_k, prefix_v, block_k, block_v, out, scale, splits, prefix_v_packed, causal_block, ext_k, ext_v, E, L=None):
     """Parameters of a batch of independent problems: every array has a leading batch dimension."""
     P = q.shape[0]
     for name, t in (("prefix_k", prefix_k), ("prefix_v", prefix_v), ("block_k", block_k), ("block_v", block_v),
@@ -326,14 +366,14 @@ def _batched_params(q, prefix_k, prefix_v, block_k, block_v, out, scale, splits,
         if t is not None and (t.shape[0] != P or not t[0].is_contiguous()):
             raise ValueError(f"{name} must have leading dimension {P} and contiguous problems")
     sub = lambda t: None if t is None else t[0]
-    p = _attn_params(q[0], prefix_k[0], prefix_v[0], block_k[0], block_v[0], None, sub(out), scale, splits,
-                     sub(prefix_v_packed), causal_block, sub(ext_k), sub(ext_v), E)
+    p = _attn_params(q[0], sub(prefix_k), sub(prefix_v), block_k[0], block_v[0], None, sub(out), scale, splits,
+                     sub(prefix_v_packed), causal_block, sub(ext_k), sub(ext_v), E, L=L)
     p.batch = P
-    if prefix_k.stride(0) != prefix_v.stride(0) or block_k.stride(0) != block_v.stride(0) or \
+    if (prefix_k is not None and prefix_k.stride(0) != prefix_v.stride(0)) or block_k.stride(0) != block_v.stride(0) or \
             (ext_k is not None and ext_k.stride(0) != ext_v.stride(0)):
         raise ValueError("K and V arrays of a batch must share their batch stride")
     p.q_batch_stride, p.out_batch_stride = q.stride(0), (out.stride(0) if out is not None else q[0].numel())
-    p.prefix_batch_stride, p.block_batch_stride = prefix_k.stride(0), block_k.stride(0)
+    p.prefix_batch_stride, p.block_batch_stride = 0 if prefix_k is None else prefix_k.stride(0), block_k.stride(0)
     p.ext_batch_stride = ext_k.stride(0) if ext_k is not None else 0
     p.packed_batch_stride = prefix_v_packed.stride(0) * prefix_v_packed.element_size() if prefix_v_packed is not None else 0
     return p
@@ -359,6 +399,239 @@ def fdd_block_attn_batched(q, prefix_k, prefix_v, block_k, block_v, out=None, sc
     p.stream = _stream_ptr(stream)
     _check(lib.fdd_block_attn(C.byref(p)))
     return out
+
+
+class QuantPrefix(NamedTuple):
+    """A prefix cache in 8 bits (see include/fdd.h): codes ``k``, ``v`` [Hkv,capacity,D] float8_e4m3fn and their scales
+    ``k_scale``, ``v_scale`` [Hkv,capacity/64] float32; with a leading dimension, a cache for each problem of a batch."""
+    k: Any
+    v: Any
+    k_scale: Any
+    v_scale: Any
+
+
+def fdd_quant_prefix(capacity, Hkv, D, device="cuda", batch=None) -> QuantPrefix:
+    """A cache without rows for ``capacity`` of them, rounded up to whole blocks of 64."""
+    load_library()
+    blocks = (int(capacity) + FDD_QUANT_BLOCK - 1) // FDD_QUANT_BLOCK
+    lead = () if batch is None else (int(batch),)
+    codes = [torch.empty(lead + (Hkv, blocks * FDD_QUANT_BLOCK, D), dtype=torch.float8_e4m3fn, device=device) for _ in range(2)]
+    scales = [torch.empty(lead + (Hkv, blocks), dtype=torch.float32, device=device) for _ in range(2)]
+    return QuantPrefix(*codes, *scales)
+
+
+def _on_current_device(*tensors):
+    """The library launches on the current device: all tensors of a call have to be there."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"tensors must live on the current device cuda:{torch.cuda.current_device()}, not on {t.device}")
+
+
+def _quant_cache(prefix, batch=None):
+    """The cache as the library takes it.  Problems of a batch may lie apart, the arrays of one are dense."""
+    k, v, ks, vs = prefix
+    lead = 0 if batch is None else 1
+    if k.dim() != 3 + lead or v.shape != k.shape or k.shape[-2] % FDD_QUANT_BLOCK or \
+            ks.shape != k.shape[:-2] + (k.shape[-2] // FDD_QUANT_BLOCK,) or vs.shape != ks.shape or (lead and k.shape[0] != batch):
+        raise ValueError("a cache is k, v [Hkv,capacity,D] and k_scale, v_scale [Hkv,capacity/64], with a leading dimension for a batch")
+    if k.dtype != torch.float8_e4m3fn or v.dtype != k.dtype or ks.dtype != torch.float32 or vs.dtype != ks.dtype:
+        raise TypeError("codes of a cache are float8_e4m3fn and its scales float32")
+    _on_current_device(*prefix)
+    c = QuantCache()
+    if lead:
+        if k.stride(0) != v.stride(0) or ks.stride(0) != vs.stride(0):
+            raise ValueError("K and V arrays of a batch must share their batch stride")
+        c.batch_stride, c.scale_batch_stride = k.stride(0), ks.stride(0)
+        k, v, ks, vs = k[0], v[0], ks[0], vs[0]
+    c.k, c.v, c.k_scale, c.v_scale = _dev(k, "cache k"), _dev(v, "cache v"), _dev(ks, "k_scale"), _dev(vs, "v_scale")
+    c.Hkv, c.capacity, c.D = k.shape
+    return c
+
+
+def _quant_rows(k, v, cache, row0):
+    """Rows [rows,Hkv,D] of K and V; consecutive rows may lie apart (a part of a fused projection)."""
+    if k.dim() != 3 or v.shape != k.shape or k.shape[1:] != (cache.Hkv, cache.D):
+        raise ValueError("k / v must be [rows,Hkv,D] with the cache's Hkv and D")
+    if v.dtype != k.dtype:
+        raise TypeError("k and v must share one element type")
+    r = QuantRows()
+    r.rows, r.dtype = k.shape[0], _dtype_code(k)
+    if not 0 <= row0 <= cache.capacity - r.rows:
+        raise ValueError(f"rows [{row0}, {row0 + r.rows}) do not fit a cache of {cache.capacity}")
+    _on_current_device(k, v)
+    for t, name in ((k, "k"), (v, "v")):
+        if not t.is_cuda:
+            raise ValueError(f"{name} must live in GPU memory")
+        if r.rows and not t[0].is_contiguous():
+            raise ValueError(f"the heads and channels of a row of {name} must be contiguous")
+    if r.rows > 1:      # (the stride of a dimension of one entry means nothing)
+        r.k_row_stride, r.v_row_stride = k.stride(0), v.stride(0)
+        if min(k.stride(0), v.stride(0)) < cache.Hkv * cache.D:
+            raise ValueError("rows of k / v must not overlap")
+    r.k, r.v = k.data_ptr(), v.data_ptr()
+    return r
+
+
+def fdd_prefix_quantize(k, v, prefix, row0=0, stream=None):
+    """The rows k, v [rows,Hkv,D] (bf16 or fp32; rows may lie apart) become rows [row0, row0 + rows) of the cache
+    ``prefix``, which then ends with them (in place); returns row0 + rows, the number of rows it holds."""
+    lib = load_library()
+    cache = _quant_cache(prefix)
+    r = _quant_rows(k, v, cache, int(row0))
+    _check(lib.fdd_prefix_quantize(C.byref(cache), int(row0), C.byref(r), _stream_ptr(stream)))
+    return int(row0) + r.rows
+
+
+def fdd_prefix_dequantize(prefix, rows, row0=0, dtype=None, k=None, v=None, stream=None):
+    """Rows [row0, row0 + rows) of the cache as (k, v) [rows,Hkv,D], exactly; ``dtype`` bf16 (default) or fp32, or into
+    the given k and v."""
+    lib = load_library()
+    cache = _quant_cache(prefix)
+    if (k is None) != (v is None):
+        raise ValueError("give both k and v, or neither")
+    rows, row0 = int(rows), int(row0)
+    if rows < 0 or not 0 <= row0 <= cache.capacity - rows:
+        raise ValueError(f"rows [{row0}, {row0 + rows}) do not fit a cache of {cache.capacity}")
+    if k is None:
+        dev = prefix.k.device
+        new = torch.empty if stream is None else _maker(stream, dev, torch.empty)
+        k, v = (new((rows, cache.Hkv, cache.D), dtype=torch.bfloat16 if dtype is None else dtype, device=dev) for _ in range(2))
+    elif k.dim() != 3 or k.shape[0] != rows or (dtype is not None and k.dtype != dtype):
+        raise ValueError("k / v must be [rows,Hkv,D] of the requested type")
+    r = _quant_rows(k, v, cache, row0)
+    _check(lib.fdd_prefix_dequantize(C.byref(cache), row0, C.byref(r), _stream_ptr(stream)))
+    return k, v
+
+
+def _quant_attn_params(q, prefix, L, block_k, block_v, scaffold_mask, out, scale, splits, causal_block, ext_k, ext_v, E):
+    """Parameters of a call (prefix in a cache) and the cache, or None in its place where there is no prefix."""
+    cache = None if prefix is None else _quant_cache(prefix)
+    L = int(L)
+    if not 0 <= L <= (0 if cache is None else cache.capacity):
+        raise ValueError(f"L={L} is outside the cache")
+    if cache is not None and (cache.Hkv != block_k.shape[2] or cache.D != q.shape[3]):
+        raise ValueError("the cache must have the block's Hkv and D")
+    _on_current_device(q, block_k, block_v, scaffold_mask, out, ext_k, ext_v)
+    return _attn_params(q, None, None, block_k, block_v, scaffold_mask, out, scale, splits, None, causal_block, ext_k, ext_v, E, L=L), cache
+
+
+def _set_q_positions(p, q_positions):
+    if q_positions.dtype != torch.int32 or q_positions.dim() != 1 or not q_positions.is_contiguous():
+        raise ValueError("q_positions must be a contiguous 1-D int32 tensor")
+    p.q_positions = _dev(q_positions, "q_positions")
+    p.n_q_positions = q_positions.numel()
+
+
+def fdd_block_attn_quant_workspace(q, prefix, L, block_k, block_v, splits=0, ext_k=None, ext_v=None, E=0, n_q_positions=0) -> int:
+    """Workspace bytes of the fdd_block_attn_quant call with these arguments."""
+    p, _ = _quant_attn_params(q, prefix, L, block_k, block_v, None, None, None, splits, False, ext_k, ext_v, E)
+    p.n_q_positions = int(n_q_positions)
+    return load_library().fdd_block_attn_quant_workspace(C.byref(p))
+
+
+def fdd_block_attn_quant(q, prefix, L, block_k, block_v, scaffold_mask=None, out=None, scale=None, workspace=None, stream=None,
+                         splits=0, causal_block=False, ext_k=None, ext_v=None, E=0, q_positions=None):
+    """``fdd_block_attn`` with the shared prefix in 8 bits: its keys and values are the first L rows of the cache
+    ``prefix`` (a QuantPrefix; may be None iff L == 0).  Everything else is as there."""
+    lib = load_library()
+    if out is None:
+        out = (torch.empty_like if stream is None else _maker(stream, q.device, torch.empty_like))(q)
+    p, cache = _quant_attn_params(q, prefix, L, block_k, block_v, scaffold_mask, out, scale, splits, causal_block, ext_k, ext_v, E)
+    if q_positions is not None:
+        _on_current_device(q_positions)
+        _set_q_positions(p, q_positions)
+        if p.n_q_positions == 0:      # (0 stands for all positions in the library)
+            return out
+    ws = _set_workspace(p, workspace, lib.fdd_block_attn_quant_workspace, q.device, stream)  # noqa: F841
+    p.stream = _stream_ptr(stream)
+    _check(lib.fdd_block_attn_quant(C.byref(p), None if cache is None else C.byref(cache)))
+    return out
+
+
+def _batched_quant_params(q, prefix, L, block_k, block_v, out, scale, splits, causal_block, ext_k, ext_v, E):
+    P = q.shape[0]
+    cache = _quant_cache(prefix, batch=P)
+    L = int(L)
+    if not 0 <= L <= cache.capacity:
+        raise ValueError(f"L={L} is outside the cache")
+    if cache.Hkv != block_k.shape[3] or cache.D != q.shape[4]:
+        raise ValueError("the cache must have the block's Hkv and D")
+    _on_current_device(q, block_k, block_v, out, ext_k, ext_v)
+    return _batched_params(q, None, None, block_k, block_v, out, scale, splits, None, causal_block, ext_k, ext_v, E, L=L), cache
+
+
+def fdd_block_attn_quant_batched_workspace(q, prefix, L, block_k, block_v, splits=0, ext_k=None, ext_v=None, E=0) -> int:
+    p, _ = _batched_quant_params(q, prefix, L, block_k, block_v, None, None, splits, False, ext_k, ext_v, E)
+    return load_library().fdd_block_attn_quant_workspace(C.byref(p))
+
+
+def fdd_block_attn_quant_batched(q, prefix, L, block_k, block_v, out=None, scale=None, workspace=None, stream=None, splits=0,
+                                 causal_block=False, ext_k=None, ext_v=None, E=0):
+    """``fdd_block_attn_batched`` with every problem's prefix in a cache of 8 bits: ``prefix`` has a leading batch
+    dimension like the other arrays, L rows of each cache are used."""
+    lib = load_library()
+    if out is None:
+        out = (torch.empty_like if stream is None else _maker(stream, q.device, torch.empty_like))(q)
+    p, cache = _batched_quant_params(q, prefix, L, block_k, block_v, out, scale, splits, causal_block, ext_k, ext_v, E)
+    ws = _set_workspace(p, workspace, lib.fdd_block_attn_quant_workspace, q.device, stream)  # noqa: F841
+    p.stream = _stream_ptr(stream)
+    _check(lib.fdd_block_attn_quant(C.byref(p), C.byref(cache)))
+    return out
+
+
+def _logprob_params(logits, top, temperature):
+    p = LogprobParams()
+    p.N, p.B, p.V = logits.shape
+    if not 0 <= int(top) <= FDD_LOGPROBS_MAX_TOP:
+        raise ValueError(f"top must be 0 to {FDD_LOGPROBS_MAX_TOP}")
+    p.dtype, p.top, p.temperature = _dtype_code(logits), int(top), float(temperature)
+    return p
+
+
+def fdd_token_logprobs_workspace(logits, top=0) -> int:
+    p = _logprob_params(logits, top, 1.0)
+    return load_library().fdd_token_logprobs_workspace(C.byref(p))
+
+
+def fdd_token_logprobs(logits, tokens, mask=None, top=0, temperature=1.0, logprobs=None, entropy=None, top_ids=None, top_logprobs=None,
+                       workspace=None, stream=None):
+    """Log probabilities of ``tokens`` [N,B] under softmax(logits [N,B,V] / temperature), the entropy of every row and
+    its ``top`` most probable tokens (see include/fdd.h).  ``mask`` (uint8 [N,B]): only positions where it is 1;
+    the others' outputs stay as they were (0, and ids -1, in outputs that are allocated here).
+
+    Returns (logprobs [N,B], entropy [N,B], top_ids [N,B,top], top_logprobs [N,B,top])."""
+    lib = load_library()
+    N, B, V = logits.shape
+    if tokens.dtype != torch.int32 or tokens.shape != (N, B):
+        raise TypeError("tokens must be torch.int32 [N,B]")
+    if mask is not None and (mask.dtype != torch.uint8 or mask.shape != (N, B)):
+        raise TypeError("mask must be torch.uint8 [N,B]")
+    p = _logprob_params(logits, top, temperature)
+    dev = logits.device
+    if mask is None:
+        new = lambda shape, dtype, value: torch.empty(shape, dtype=dtype, device=dev)
+    else:
+        new = lambda shape, dtype, value: torch.full(shape, value, dtype=dtype, device=dev)
+    if stream is not None:
+        new = _maker(stream, dev, new)
+    outs = []
+    for t, shape, dtype, value, name in ((logprobs, (N, B), torch.float32, 0.0, "logprobs"), (entropy, (N, B), torch.float32, 0.0, "entropy"),
+                                         (top_ids, (N, B, p.top), torch.int32, -1, "top_ids"),
+                                         (top_logprobs, (N, B, p.top), torch.float32, 0.0, "top_logprobs")):
+        if t is None:
+            t = new(shape, dtype, value)
+        elif t.dtype != dtype or t.shape != shape:
+            raise TypeError(f"{name} must be {dtype} {list(shape)}")
+        outs.append(t)
+    _on_current_device(logits, tokens, mask, *outs)
+    p.logits, p.tokens, p.row_mask = _dev(logits, "logits"), _dev(tokens, "tokens"), _dev(mask, "mask")
+    p.logprobs, p.entropy = _dev(outs[0], "logprobs"), _dev(outs[1], "entropy")
+    if p.top:
+        p.top_ids, p.top_logprobs = _dev(outs[2], "top_ids"), _dev(outs[3], "top_logprobs")
+    ws = _set_workspace(p, workspace, lib.fdd_token_logprobs_workspace, dev, stream)  # noqa: F841
+    p.stream = _stream_ptr(stream)
+    _check(lib.fdd_token_logprobs(C.byref(p)))
+    return tuple(outs)
 
 
 def _unmask_params(logits, mask, scaffold_mask, tokens, tau, confidences, n_unmasked, committed, refresh=None):

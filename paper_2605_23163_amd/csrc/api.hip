@@ -32,61 +32,76 @@ namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-fdd_status check_attn_shape(const fdd_attn_params* p)
+}  // namespace
+
+fdd_status check_attn_shape(const fdd_attn_params* p, const char* fn, bool own_prefix)
 {
-    if (!p) return fail(FDD_ERR_NULL, "fdd_block_attn: params is NULL");
+    if (!p) return fail(FDD_ERR_NULL, "%s: params is NULL", fn);
     if (p->N <= 0 || p->B <= 0 || p->L < 0 || p->Hq <= 0 || p->Hkv <= 0 || p->D <= 0)
-        return fail(FDD_ERR_SHAPE, "fdd_block_attn: N, B, Hq, Hkv, D must be positive and L >= 0 (got N=%d B=%d L=%d Hq=%d Hkv=%d D=%d)",
+        return fail(FDD_ERR_SHAPE, "%s: N, B, Hq, Hkv, D must be positive and L >= 0 (got N=%d B=%d L=%d Hq=%d Hkv=%d D=%d)", fn,
                     p->N, p->B, p->L, p->Hq, p->Hkv, p->D);
-    if (p->Hq % p->Hkv) return fail(FDD_ERR_SHAPE, "fdd_block_attn: Hq=%d is not a multiple of Hkv=%d", p->Hq, p->Hkv);
-    if (p->dtype != FDD_F32 && p->dtype != FDD_BF16) return fail(FDD_ERR_DTYPE, "fdd_block_attn: dtype %d is neither FDD_F32 nor FDD_BF16", p->dtype);
-    if (p->D != 64 && p->D != 128) return fail(FDD_ERR_UNSUPPORTED, "fdd_block_attn: head size D=%d not supported (64 or 128)", p->D);
-    if (p->splits < 0 || p->splits > 64) return fail(FDD_ERR_UNSUPPORTED, "fdd_block_attn: splits=%d outside [0, 64]", p->splits);
-    if (p->flags & ~FDD_ATTN_CAUSAL_BLOCK) return fail(FDD_ERR_UNSUPPORTED, "fdd_block_attn: unknown bits in flags (0x%x)", p->flags);
+    if (p->Hq % p->Hkv) return fail(FDD_ERR_SHAPE, "%s: Hq=%d is not a multiple of Hkv=%d", fn, p->Hq, p->Hkv);
+    if (p->dtype != FDD_F32 && p->dtype != FDD_BF16) return fail(FDD_ERR_DTYPE, "%s: dtype %d is neither FDD_F32 nor FDD_BF16", fn, p->dtype);
+    if (p->D != 64 && p->D != 128) return fail(FDD_ERR_UNSUPPORTED, "%s: head size D=%d not supported (64 or 128)", fn, p->D);
+    if (p->splits < 0 || p->splits > 64) return fail(FDD_ERR_UNSUPPORTED, "%s: splits=%d outside [0, 64]", fn, p->splits);
+    if (p->flags & ~FDD_ATTN_CAUSAL_BLOCK) return fail(FDD_ERR_UNSUPPORTED, "%s: unknown bits in flags (0x%x)", fn, p->flags);
     // (every product below is bounded before the next factor is multiplied in: no 64-bit overflow for any int32 input)
     const long long nb = (long long)p->N * p->B;
     if (nb > (1ll << 30) || nb * (p->Hq / p->Hkv) > (1ll << 30) || nb * p->Hq > (1ll << 33))
-        return fail(FDD_ERR_SHAPE, "fdd_block_attn: N*B*Hq too large");
+        return fail(FDD_ERR_SHAPE, "%s: N*B*Hq too large", fn);
     if ((long long)p->L * p->Hkv >= (1ll << 31) || (long long)p->L * p->Hkv * p->D * 4 >= (1ll << 31))
-        return fail(FDD_ERR_SHAPE, "fdd_block_attn: prefix K (L*Hkv*D elements) must stay below 2 GiB");
+        return fail(FDD_ERR_SHAPE, "%s: prefix K (L*Hkv*D elements) must stay below 2 GiB", fn);
     if (nb * p->Hkv >= (1ll << 32) || nb * p->Hkv * p->D * 4 >= (1ll << 32))
-        return fail(FDD_ERR_SHAPE, "fdd_block_attn: block K (N*B*Hkv*D elements) must stay below 4 GiB");
-    if (p->batch < 0 || p->batch > 65535 / p->Hkv) return fail(FDD_ERR_SHAPE, "fdd_block_attn: batch=%d outside [0, 65535 / Hkv]", p->batch);
+        return fail(FDD_ERR_SHAPE, "%s: block K (N*B*Hkv*D elements) must stay below 4 GiB", fn);
+    if (p->batch < 0 || p->batch > 65535 / p->Hkv) return fail(FDD_ERR_SHAPE, "%s: batch=%d outside [0, 65535 / Hkv]", fn, p->batch);
     {
         // work units of the bf16 path: (KV head, 256-row M-tile, 64-key prefix tile)
         const long long mt = (nb * (p->Hq / p->Hkv) + 255) / 256;            // <= 2^22
         const long long tpu = (p->L + 63) / 64 + 64;          // prefix tiles plus the units booked for private tiles (bounded by 64 here)
         const long long heads = (long long)p->Hkv * (p->batch > 1 ? p->batch : 1);                 // <= 2^16
-        if (heads * mt >= (1ll << 31) || heads * mt * tpu >= (1ll << 31)) return fail(FDD_ERR_SHAPE, "fdd_block_attn: batch*N*B*Hq*L too large");
+        if (heads * mt >= (1ll << 31) || heads * mt * tpu >= (1ll << 31)) return fail(FDD_ERR_SHAPE, "%s: batch*N*B*Hq*L too large", fn);
     }
-    if (std::isnan(p->scale) || std::isinf(p->scale)) return fail(FDD_ERR_UNSUPPORTED, "fdd_block_attn: scale is not finite");
+    if (std::isnan(p->scale) || std::isinf(p->scale)) return fail(FDD_ERR_UNSUPPORTED, "%s: scale is not finite", fn);
     if (p->n_q_positions < 0 || (long long)p->n_q_positions > (long long)p->N * p->B)
-        return fail(FDD_ERR_SHAPE, "fdd_block_attn: n_q_positions=%d outside [0, N*B]", p->n_q_positions);
+        return fail(FDD_ERR_SHAPE, "%s: n_q_positions=%d outside [0, N*B]", fn, p->n_q_positions);
     if (p->batch > 1) {
         const long long es = p->dtype == FDD_BF16 ? 2 : 4;
         struct { const char* name; long long stride, need; } st[] = {
             {"q_batch_stride", p->q_batch_stride, (long long)p->N * p->B * p->Hq * p->D},
             {"out_batch_stride", p->out_batch_stride, (long long)p->N * p->B * p->Hq * p->D},
             {"block_batch_stride", p->block_batch_stride, (long long)p->N * p->B * p->Hkv * p->D},
-            {"prefix_batch_stride", p->prefix_batch_stride, (long long)p->L * p->Hkv * p->D},
+            {"prefix_batch_stride", own_prefix ? p->prefix_batch_stride : 0, own_prefix ? (long long)p->L * p->Hkv * p->D : 0},
             {"ext_batch_stride", p->ext_batch_stride, p->E > 0 ? (long long)p->N * p->ext_capacity * p->Hkv * p->D : 0},
         };
         for (const auto& x : st)
             if (x.stride < x.need || (x.stride * es) % 16)
-                return fail(FDD_ERR_SHAPE, "fdd_block_attn: %s=%lld must be at least %lld elements and a multiple of 16 bytes",
+                return fail(FDD_ERR_SHAPE, "%s: %s=%lld must be at least %lld elements and a multiple of 16 bytes", fn,
                             x.name, x.stride, x.need);
         if (p->prefix_v_packed && (p->packed_batch_stride % 256 ||
                                    p->packed_batch_stride < (size_t)p->Hkv * (p->L / 64) * 64 * p->D * 2))
-            return fail(FDD_ERR_SHAPE, "fdd_block_attn: packed_batch_stride must be a multiple of 256 and hold one packed prefix V");
+            return fail(FDD_ERR_SHAPE, "%s: packed_batch_stride must be a multiple of 256 and hold one packed prefix V", fn);
     }
     if (p->E < 0 || p->ext_capacity < 0 || p->E > p->ext_capacity)
-        return fail(FDD_ERR_SHAPE, "fdd_block_attn: need 0 <= E <= ext_capacity (got E=%d, ext_capacity=%d)", p->E, p->ext_capacity);
+        return fail(FDD_ERR_SHAPE, "%s: need 0 <= E <= ext_capacity (got E=%d, ext_capacity=%d)", fn, p->E, p->ext_capacity);
     if ((long long)p->N * p->ext_capacity * p->Hkv * p->D * 4 >= (1ll << 32))
-        return fail(FDD_ERR_SHAPE, "fdd_block_attn: extension K (N*ext_capacity*Hkv*D elements) must stay below 4 GiB");
+        return fail(FDD_ERR_SHAPE, "%s: extension K (N*ext_capacity*Hkv*D elements) must stay below 4 GiB", fn);
     return FDD_OK;
 }
 
-}  // namespace
+fdd_status check_attn_pointers(const fdd_attn_params* p, const char* fn, bool own_prefix)
+{
+    if (!p->q || !p->block_k || !p->block_v || !p->out) return fail(FDD_ERR_NULL, "%s: q, block_k, block_v and out must not be NULL", fn);
+    if (own_prefix && p->L > 0 && (!p->prefix_k || !p->prefix_v)) return fail(FDD_ERR_NULL, "%s: prefix_k / prefix_v is NULL with L=%d", fn, p->L);
+    if (p->E > 0 && (!p->ext_k || !p->ext_v)) return fail(FDD_ERR_NULL, "%s: ext_k / ext_v is NULL with E=%d", fn, p->E);
+    if (p->n_q_positions > 0 && !p->q_positions) return fail(FDD_ERR_NULL, "%s: q_positions is NULL with n_q_positions=%d", fn, p->n_q_positions);
+    if (p->n_q_positions > 0 && (reinterpret_cast<uintptr_t>(p->q_positions) & 3u)) return fail(FDD_ERR_UNSUPPORTED, "%s: q_positions must be 4-byte aligned", fn);
+    const void* ptrs[] = {p->q, p->prefix_k, p->prefix_v, p->block_k, p->block_v, p->out, p->prefix_v_packed,
+                          p->E > 0 ? p->ext_k : nullptr, p->E > 0 ? p->ext_v : nullptr};
+    for (const void* x : ptrs)
+        if (x && !aligned16(x)) return fail(FDD_ERR_UNSUPPORTED, "%s: data pointers must be 16-byte aligned", fn);
+    if (p->out == p->q) return fail(FDD_ERR_UNSUPPORTED, "%s: out must not alias q", fn);
+    return FDD_OK;
+}
 
 // Workgroups per row tile of the fp32 path, and the time that is expected of them.
 //   32-row tiles (attn_f32_kernel): a round of workgroups takes ceil(tiles / (8 S)) tiles per wavefront, two wavefronts per
@@ -443,7 +458,7 @@ extern "C" {
 
 size_t fdd_block_attn_workspace(const fdd_attn_params* p)
 {
-    if (check_attn_shape(p) != FDD_OK) return 0;
+    if (check_attn_shape(p, "fdd_block_attn", true) != FDD_OK) return 0;
     AttnPlan plan;
     make_attn_plan(*p, &plan);
     size_t partials = plan.ws_o_bytes + plan.ws_ml_bytes;
@@ -459,18 +474,10 @@ size_t fdd_block_attn_workspace(const fdd_attn_params* p)
 
 fdd_status fdd_block_attn(const fdd_attn_params* p)
 {
-    fdd_status st = check_attn_shape(p);
+    fdd_status st = check_attn_shape(p, "fdd_block_attn", true);
     if (st != FDD_OK) return st;
-    if (!p->q || !p->block_k || !p->block_v || !p->out) return fail(FDD_ERR_NULL, "fdd_block_attn: q, block_k, block_v and out must not be NULL");
-    if (p->L > 0 && (!p->prefix_k || !p->prefix_v)) return fail(FDD_ERR_NULL, "fdd_block_attn: prefix_k / prefix_v is NULL with L=%d", p->L);
-    if (p->E > 0 && (!p->ext_k || !p->ext_v)) return fail(FDD_ERR_NULL, "fdd_block_attn: ext_k / ext_v is NULL with E=%d", p->E);
-    if (p->n_q_positions > 0 && !p->q_positions) return fail(FDD_ERR_NULL, "fdd_block_attn: q_positions is NULL with n_q_positions=%d", p->n_q_positions);
-    if (p->n_q_positions > 0 && (reinterpret_cast<uintptr_t>(p->q_positions) & 3u)) return fail(FDD_ERR_UNSUPPORTED, "fdd_block_attn: q_positions must be 4-byte aligned");
-    const void* ptrs[] = {p->q, p->prefix_k, p->prefix_v, p->block_k, p->block_v, p->out, p->prefix_v_packed,
-                          p->E > 0 ? p->ext_k : nullptr, p->E > 0 ? p->ext_v : nullptr};
-    for (const void* x : ptrs)
-        if (x && !aligned16(x)) return fail(FDD_ERR_UNSUPPORTED, "fdd_block_attn: data pointers must be 16-byte aligned");
-    if (p->out == p->q) return fail(FDD_ERR_UNSUPPORTED, "fdd_block_attn: out must not alias q");
+    st = check_attn_pointers(p, "fdd_block_attn", true);
+    if (st != FDD_OK) return st;
     AttnPlan plan;
     make_attn_plan(*p, &plan);
     size_t need = plan.ws_o_bytes + plan.ws_ml_bytes + plan.ws_vt_bytes;

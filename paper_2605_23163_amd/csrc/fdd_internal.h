@@ -72,6 +72,10 @@ bool make_attn_plan(const fdd_attn_params& p, AttnPlan* plan, bool ample = true)
 
 // Records the message fdd_last_error() returns on this thread; returns `code`.
 fdd_status set_error(fdd_status code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+// Host-side checks of an attention call: shapes and strides; pointers.  `own_prefix`: the prefix is the call's own prefix_k and
+// prefix_v (not a cache in 8 bits, which is checked where it is used); `fn` names the entry point in messages.
+fdd_status check_attn_shape(const fdd_attn_params* p, const char* fn, bool own_prefix);
+fdd_status check_attn_pointers(const fdd_attn_params* p, const char* fn, bool own_prefix);
 // Host-side checks of an unmask call (everything but the workspace); `fn` names the entry point in messages.
 fdd_status check_unmask_args(const fdd_unmask_params* p, const char* fn);
 
@@ -170,6 +174,9 @@ __host__ __device__ inline int unit_begin(int w, int base, int rem) { return w *
 // `before_main`, if not null, is recorded on the stream right before the main kernel (after the V pre-pass).
 hipError_t launch_attn_bf16(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s, hipEvent_t before_main);
 hipError_t launch_prefix_pack(const void* prefix_v, int L, int Hkv, int D, void* packed, hipStream_t s);
+// K and V of the first `rows` rows of a cache of 8 bits, [batch][rows,Hkv,D] of type `dtype`, problems batch_stride elements apart
+hipError_t launch_dequantize(const fdd_quant_cache& c, int row0, const fdd_quant_rows& dst, int batch, long long batch_stride, hipStream_t s);
+hipError_t launch_quantize(const fdd_quant_cache& c, int row0, const fdd_quant_rows& src, hipStream_t s);
 hipError_t launch_attn_f32(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s);
 hipError_t launch_attn_combine(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s);      // fp32 path
 hipError_t launch_attn_merge_bf16(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s);   // bf16 path
@@ -185,6 +192,7 @@ bool make_unmask_plan(const fdd_unmask_params& p, UnmaskPlan* plan);
 bool make_vocab_plan(int N, int B, long long V, int dtype, bool argmax_only, UnmaskPlan* plan);
 hipError_t launch_unmask(const fdd_unmask_params& p, const UnmaskPlan& plan, hipStream_t s);
 hipError_t launch_verify(const fdd_verify_params& p, const UnmaskPlan& plan, hipStream_t s);
+hipError_t launch_logprobs(const fdd_logprob_params& p, hipStream_t s);
 
 hipError_t launch_fork_block(int N, size_t bytes, const void* src, void* dst, hipStream_t s);
 hipError_t launch_kv_update(const fdd_kv_update_params& p, hipStream_t s);
