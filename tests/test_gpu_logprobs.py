@@ -114,6 +114,20 @@ def test_ties_order_and_missing_entries(F, V, dtype):
         check(F, x, tokens.astype(np.int32), dtype, top)
 
 
+@pytest.mark.parametrize("dtype", [W.BF16, W.F32])
+@pytest.mark.parametrize("V", [9001, 15000, 100000])
+def test_largest_entries_in_few_places(F, V, dtype):
+    """Rows whose largest entries repeat with a period: a few threads of a workgroup have them all."""
+    print_case(test="logprobs_few_places", V=V, dtype=dtype)
+    rng = np.random.default_rng([V, 2])
+    per = 16 // (2 if dtype == W.BF16 else 4) * 64
+    x = rng.standard_normal((1, 6, V))
+    for b, share in enumerate((1, 8, 30, 31, 33, 64)):
+        x[0, b] += 20.0 * ((np.arange(V) % per) < per // 64 * share)
+    for top in (1, 5, 32):
+        check(F, W.to_storage(x, dtype), np.zeros((1, 6), np.int32), dtype, top)
+
+
 def test_a_row_without_entries(F):
     print_case(test="logprobs_empty")
     for V in (5, 700, 40000):
