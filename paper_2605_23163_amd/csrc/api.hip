@@ -26,6 +26,12 @@ fdd_status set_error(fdd_status code, const char* fmt, ...)
     return code;
 }
 
+void attn_events(hipEvent_t* start, hipEvent_t* stop)
+{
+    *start = g_ev_stop ? g_ev_start : nullptr;
+    *stop = g_ev_start ? g_ev_stop : nullptr;
+}
+
 namespace {
 
 #define fail set_error

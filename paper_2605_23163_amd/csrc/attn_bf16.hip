@@ -141,6 +141,15 @@ struct Args {
     FastDiv dB, dBG, dTTPR, dBase, dBase1;
 };
 
+// The same with the prefix in 8 bits: pk and pv are its codes, [Hkv][capacity][D] and p_bs bytes from problem to problem.
+struct QuantArgs : Args {
+    const float* ks;      // scales of K and V, [Hkv][capacity / 64]
+    const float* vs;
+    long long s_bs;       // problems' scales
+    long long head_bytes; // capacity D
+    int head_scales;      // capacity / 64
+};
+
 template <int D, int WAVES, int SLOTS>
 struct Cfg {
     static constexpr int THREADS = WAVES * 64;
@@ -157,6 +166,25 @@ struct Cfg {
     static constexpr int LDS_BYTES = DUMP + T_BYTES;
     static_assert(NI >= 1 && T_BYTES % (1024 * WAVES) == 0, "tile must divide over the wavefronts");
     static_assert((NB - 1) * IPT < 64, "outstanding loads must fit the counter");
+};
+
+// The prefix in 8 bits.  A tile of codes, 64 D bytes in one piece, goes into a ring of codes in LDS (1 KB pieces, one per
+// wavefront instruction); every lane converts the 16 codes that it had moved itself, so that this needs no barrier, and writes them
+// into the two slots of the bf16 ring.
+template <int D, int WAVES>
+struct QuantCfg {
+    using C = Cfg<D, WAVES, 2>;
+    static constexpr int T_BYTES = KT * D;
+    static constexpr int SLOTS = 4;
+    static constexpr int AHEAD = 3;                                // steps from the request of a tile's codes to their conversion
+    static constexpr bool HALF = T_BYTES / 1024 < WAVES;           // the first half of the wavefronts moves K, the second V
+    static constexpr int NP = HALF ? 1 : T_BYTES / 1024 / WAVES;   // pieces per wavefront, tile and operand
+    static constexpr int LOADS = HALF ? 1 : 2 * NP;                // load instructions per wavefront and step
+    static constexpr int K_RING = 4 * C::T_BYTES;                  // LDS offsets: behind the bf16 rings
+    static constexpr int V_RING = K_RING + SLOTS * T_BYTES;
+    static constexpr int SCALES = V_RING + SLOTS * T_BYTES;        // scales of K and of V of 128 tiles each, in a ring
+    static constexpr int LDS_BYTES = SCALES + 2 * 128 * 4;
+    static_assert(T_BYTES / 1024 % WAVES == 0 || 2 * (T_BYTES / 1024) == WAVES, "tile must divide over the wavefronts");
 };
 
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -183,6 +211,8 @@ __device__ __forceinline__ void wait_vm()
 // fences global memory, which makes the compiler drain every tile still on
 // its way into the ring.)  No memory access is moved across it.
 __device__ __forceinline__ void wg_barrier() { asm volatile("s_barrier" ::: "memory"); }
+// The same after this wavefront's own writes to LDS.
+__device__ __forceinline__ void wg_barrier_written() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // Nothing is scheduled across this point: the source order of the pieces it
 // separates is the order the hardware sees.
@@ -225,11 +255,30 @@ __device__ __forceinline__ i16x4 read_tr(const lds_i16x4* __restrict__ p)
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16(const_cast<lds_i16x4*>(p));
 }
 
-template <int D, int WAVES, int SLOTS, bool PACKED>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kernel(Args a)
+// reads of codes and scales that have landed (`restrict` as above)
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) float lds_f32;
+__device__ __forceinline__ u32x4 read_codes(const lds_u32x4* __restrict__ p) { return *p; }
+__device__ __forceinline__ float read_scale(const lds_f32* __restrict__ p) { return *p; }
+
+// 8 codes, times the power of two `scale`: exact
+__device__ __forceinline__ u32x4 convert8(uint32_t lo, uint32_t hi, float scale)
+{
+    u32x4 w;
+    w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+    w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+    w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+    w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
+    return w;
+}
+
+template <int D, int WAVES, int SLOTS, bool PACKED, bool Q8>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kernel(std::conditional_t<Q8, QuantArgs, Args> a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)   // the host pass only needs the launch stub
     using C = Cfg<D, WAVES, SLOTS>;
+    using Q = QuantCfg<D, WAVES>;
+    static_assert(!Q8 || (SLOTS == 2 && !PACKED), "codes are converted into two slots, V as it lies");
     constexpr int NB = C::NB;
     constexpr int KS = D / 16;   // MFMA k-steps of Q K^T
     constexpr int DB = D / 32;   // 32-channel blocks of the output
@@ -265,7 +314,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
         int q3 = a.G, q4 = a.R, q5 = a.Hq, q6 = a.NB;
         uint32_t q7 = a.dG.mul, q8 = a.dG.shift;
         const uint32_t* ap = reinterpret_cast<const uint32_t*>(&a);
-        static_assert(sizeof(Args) > 80 * 4 && sizeof(Args) <= 96 * 4, "one touch per 64-byte line of Args");
+        static_assert(Q8 || sizeof(Args) > 80 * 4 && sizeof(Args) <= 96 * 4, "one touch per 64-byte line of Args");
         uint32_t t3 = ap[48], t4 = ap[64], t5 = ap[80];
         asm volatile("" ::"s"(q0), "s"(q1), "s"(q2), "s"(q3), "s"(q4), "s"(q5), "s"(q6), "s"(q7), "s"(q8), "s"(t3), "s"(t4), "s"(t5));
     }
@@ -315,6 +364,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
     // V as it lies in memory: 32-byte columns are XOR-swizzled by the row, for
     // the transposing reads.  Packed V^T tiles are copied as they are.
     uint32_t k_voff[C::NI];
+    if constexpr (!Q8)
 #pragma unroll
     for (int jn = 0; jn < C::NI; ++jn) {
         const int r = (wave * C::NI + jn) * C::RPB + lane / C::CH;
@@ -331,6 +381,20 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
         v_voff = (uint32_t)r * stride2 + (uint32_t)(((lane % C::CH) ^ ((((r / C::RPL) & 3) << 2) & (C::CH - 1))) * 16);
     }
     const uint32_t v_piece = PACKED ? 0u : C::RPB * stride2 - 1024u;      // between pieces, beyond the 1 KB of the instruction's offset
+    // Q8: this lane converts the 16 codes at byte 16 lane of each of its wavefront's pieces.  Offset of the codes behind the ring's
+    // start, and offsets in a tile of the bf16 ring of the first 8 channels of piece 0; the other 8 lie at the offset ^ 16 (the
+    // swizzles move pairs of 16-byte pieces), the next piece Q_ROWS rows on, with K_XOR in K's swizzle.
+    const int q_wave = Q::HALF ? wave_u & (WAVES / 2 - 1) : wave_u;
+    const bool q_v = Q::HALF && wave_u >= WAVES / 2;             // HALF: this wavefront moves V
+    uint32_t q_rd = 0, q_wk = 0, q_wv = 0;
+    constexpr int Q_ROWS = 1024 / D;                              // rows of a piece
+    constexpr uint32_t K_XOR = D == 128 ? 128 : 0;                // 8 rows on: bit 3 of K's swizzle, which repeats every 16 rows
+    if constexpr (Q8) {
+        const int r = q_wave * Q::NP * Q_ROWS + lane / (D / 16), ch = lane % (D / 16) * 2;
+        q_rd = (uint32_t)(q_wave * Q::NP * 1024 + lane * 16);
+        q_wk = (uint32_t)(r * D * 2 + (ch ^ ((r / C::RPL) & (C::CH - 1))) * 16);
+        q_wv = (uint32_t)(r * D * 2 + (ch ^ (((r / C::RPL & 3) << 2) & (C::CH - 1))) * 16);
+    }
     auto k_frag = [&](uint32_t kbase, int kb, int ks) -> bf16x8 {
         return *reinterpret_cast<const bf16x8*>(lds + (kbase + k_fragoff[ks]) + kb * 32 * D * 2);
     };
@@ -356,8 +420,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
         const int pb = a.batch > 1 ? fast_div(khv, a.dHkv) : 0;
         const int kh = khv - pb * a.Hkv;
         // (the arrays of problem pb are addressed where they are used: few of these pointers are live at a time)
-        const uint16_t* const pk = a.pk + pb * a.p_bs;
-        const uint16_t* const pv = PACKED ? a.vt + pb * a.vt_bs : a.pv + pb * a.p_bs;
+        const uint16_t* const pk = a.pk + (Q8 ? 0 : pb * a.p_bs);
+        const uint16_t* const pv = PACKED ? a.vt + pb * a.vt_bs : a.pv + (Q8 ? 0 : pb * a.p_bs);
         const uint32_t pk_bytes = (uint32_t)a.L * stride2;
         const uint32_t pv_bytes = PACKED ? (uint32_t)(a.Hkv * a.TPF) * C::T_BYTES : pk_bytes;
         // stores of the previous segment are out of the way of the load counting below
@@ -390,7 +454,67 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
             };
             for_slots(piece, std::make_integer_sequence<int, P1 - P0>());
         };
+        // ---- Q8: codes and scales of tile j: global memory -> their rings; codes -> slot of the bf16 ring ----------
+        const uint8_t *qk = nullptr, *qv = nullptr;
+        const float *qks = nullptr, *qvs = nullptr;
+        if constexpr (Q8) {
+            qk = reinterpret_cast<const uint8_t*>(a.pk) + pb * a.p_bs + kh * a.head_bytes;
+            qv = reinterpret_cast<const uint8_t*>(a.pv) + pb * a.p_bs + kh * a.head_bytes;
+            qks = a.ks + pb * a.s_bs + (long long)kh * a.head_scales;
+            qvs = a.vs + pb * a.s_bs + (long long)kh * a.head_scales;
+        }
+        // (a request for a tile that there is not reads nothing and leaves zeros)
+        auto q_request = [&](bool v, int j, auto piece) {
+            constexpr int jn = decltype(piece)::value;
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(v ? qv : qk), 0, j < F ? (uint32_t)a.L * D : 0u, RSRC_FLAGS);
+            unsigned char* const dst = lds + (v ? Q::V_RING : Q::K_RING) + (j & (Q::SLOTS - 1)) * Q::T_BYTES + q_wave * (Q::NP * 1024);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)dst, 16, q_rd, (uint32_t)(t0 + j) * Q::T_BYTES, jn * 1024, 0);
+        };
+        auto q_scales = [&](int j) {      // of tiles j .. j + 63, j a multiple of 64; every wavefront for itself, into one place
+            const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(qks), 0, (uint32_t)a.TP * 4, RSRC_FLAGS);
+            const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(qvs), 0, (uint32_t)a.TP * 4, RSRC_FLAGS);
+            unsigned char* const dst = lds + Q::SCALES + (j & 64) * 4;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void*)dst, 4, (uint32_t)lane * 4, (uint32_t)(t0 + j) * 4, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(dst + 512), 4, (uint32_t)lane * 4, (uint32_t)(t0 + j) * 4, 0, 0);
+        };
+        struct Codes {
+            u32x4 w;
+            float scale;
+        };
+        auto q_read = [&](bool v, int j, auto piece) {
+            constexpr int jn = decltype(piece)::value;
+            Codes c;
+            c.w = read_codes((const lds_u32x4*)(lds + q_rd + ((v ? Q::V_RING : Q::K_RING) + (j & (Q::SLOTS - 1)) * Q::T_BYTES + jn * 1024)));
+            c.scale = read_scale((const lds_f32*)(lds + Q::SCALES + (v ? 512 : 0) + (j & 127) * 4));
+            return c;
+        };
+        auto q_write = [&](bool v, int j, auto piece, auto half, const Codes& c) {
+            constexpr int jn = decltype(piece)::value, h = decltype(half)::value;
+            const uint32_t at = v ? q_wv + C::V_RING : q_wk ^ (jn * K_XOR);
+            *reinterpret_cast<u32x4*>(lds + (at ^ (h * 16)) + ((j & 1) * C::T_BYTES + jn * Q_ROWS * D * 2)) = convert8(c.w[2 * h], c.w[2 * h + 1], c.scale);
+        };
         const std::integral_constant<int, 0> p_0;
+        const std::integral_constant<int, 1> p_1;
+        auto q_convert = [&](bool v, int j) {     // all of this wavefront's pieces of tile j
+            auto one = [&](auto piece) {
+                const Codes c = q_read(v, j, piece);
+                q_write(v, j, piece, p_0, c);
+                q_write(v, j, piece, p_1, c);
+            };
+            for_slots(one, std::make_integer_sequence<int, Q::NP>());
+        };
+        // what a step requests: K of tile j + 1 and V of tile j, HALF: whichever this wavefront moves
+        auto q_request_step = [&](int j) {
+            auto one = [&](auto piece) {
+                if constexpr (Q::HALF) {
+                    q_request(q_v, q_v ? j : j + 1, piece);
+                } else {
+                    q_request(false, j + 1, piece);
+                    q_request(true, j, piece);
+                }
+            };
+            for_slots(one, std::make_integer_sequence<int, Q::NP>());
+        };
         const std::integral_constant<int, C::NI> p_all;
         const std::true_type is_v;
         const std::false_type is_k;
@@ -425,9 +549,25 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
         // one step earlier, and one more half tile per workgroup is on its way at any time)
         // Only what the first step needs is requested here; the rest of the ring follows in the shadow of its first scores (all at
         // once, every workgroup's first tile waited behind the others' fourth: first barrier 4.5 -> 4.0 us after the start at N=8, L=4096).
-        fetch_k(0, 0);
-        fetch_v(0, 0);
-        fetch_k(1, C::T_BYTES);
+        if constexpr (Q8) {
+            q_scales(0);
+            q_scales(64);
+            if constexpr (Q::HALF) {
+                q_request(q_v, 0, p_0);
+                if (!q_v) q_request(false, 1, p_0);
+            } else {
+                auto first = [&](auto piece) { q_request(false, 0, piece); };
+                auto second = [&](auto piece) { q_request(true, 0, piece); };
+                auto third = [&](auto piece) { q_request(false, 1, piece); };
+                for_slots(first, std::make_integer_sequence<int, Q::NP>());
+                for_slots(second, std::make_integer_sequence<int, Q::NP>());
+                for_slots(third, std::make_integer_sequence<int, Q::NP>());
+            }
+        } else {
+            fetch_k(0, 0);
+            fetch_v(0, 0);
+            fetch_k(1, C::T_BYTES);
+        }
         issued = min(NB - 1, F);
         FDD_SCHED_FENCE();
 
@@ -579,10 +719,39 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(kdst + C::V_RING), 16, row_off + v_col16, soff, 0, 0);
             }
         };
+        // Q8: the ragged last prefix tile, through registers
+        auto fetch_codes = [&](int j) {
+            const Tile t = tile_at(j);
+            auto one = [&](bool v, auto piece) {
+                constexpr int jn = decltype(piece)::value;
+                const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(v ? qv : qk), 0, (uint32_t)a.L * D, RSRC_FLAGS);
+                const int r = (q_wave * Q::NP + jn) * Q_ROWS + lane / (D / 16);
+                Codes c;
+                c.w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (uint32_t)(min(r, t.valid - 1) * D + lane % (D / 16) * 16), (uint32_t)t.row_base * D, 0));
+                c.scale = (v ? qvs : qks)[t0 + j];
+                q_write(v, j, piece, p_0, c);
+                q_write(v, j, piece, p_1, c);
+            };
+            auto both = [&](auto piece) {
+                if constexpr (Q::HALF) {
+                    one(q_v, piece);
+                } else {
+                    one(false, piece);
+                    one(true, piece);
+                }
+            };
+            for_slots(both, std::make_integer_sequence<int, Q::NP>());
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the barriers before a masked tile wait for loads only)
+        };
         // tile j: global memory -> ring slot j % NB, no registers in between
         auto fetch = [&](int j_) {
             const int j = __builtin_amdgcn_readfirstlane(j_);
-            fetch_masked(j);
+            if constexpr (Q8) {
+                if (j < n_prefix) fetch_codes(j);
+                else fetch_masked(j);
+            } else {
+                fetch_masked(j);
+            }
             issued = j + 1;
         };
         // block until tile t has landed in LDS for the whole workgroup; tiles are
@@ -652,8 +821,21 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
         if (F > 0) {
             const std::integral_constant<int, 2 * C::NI> first;
             const std::integral_constant<int, (NB - 2) * 2 * C::NI> rest;
-            wait_but(first);       // Q, K0
-            wg_barrier();
+            if constexpr (Q8) {
+                wait_vm<Q::HALF ? 0 : 2 * Q::NP>();      // Q, scales, K0
+                if (!q_v) q_convert(false, 0);
+                wg_barrier_written();
+            } else {
+                wait_but(first);       // Q, K0
+                wg_barrier();
+            }
+            // Q8: V0 and K1, once the first AHEAD steps' codes have been requested
+            auto q_first = [&] {
+                wait_vm<Q::AHEAD * Q::LOADS>();
+                if (!Q::HALF || q_v) q_convert(true, 0);
+                if (!Q::HALF || !q_v) q_convert(false, 1);
+                wg_barrier_written();
+            };
             // what the ring still has room for: V1 K2 V2 K3
             auto request_rest = [&](auto c) {        // half tile c
                 constexpr int h = decltype(c)::value;
@@ -664,6 +846,18 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                 // A wavefront without rows (the M-tile is not full) only moves its share of the tiles: the matrix pipe and
                 // the power are left to the others (8 requests of N=1, 224 of 256 rows, L=16384: 84.0 -> 82.1 us; with 112
                 // rows or fewer a SIMD has one wavefront to serve).  Same requests, waits and barriers as in the steps below.
+                if constexpr (Q8) {
+                    for (int x = 1; x <= Q::AHEAD; ++x) q_request_step(x);
+                    q_first();
+                    for (int i = 0; i < F; ++i) {
+                        if ((i & 63) == 0 && i > 0) q_scales(i + 64);
+                        wait_vm<(Q::AHEAD - 1) * Q::LOADS>();
+                        if (!Q::HALF || !q_v) q_convert(false, i + 2);
+                        if (!Q::HALF || q_v) q_convert(true, i + 1);
+                        q_request_step(i + 1 + Q::AHEAD);
+                        wg_barrier_written();
+                    }
+                } else {
                 for_slots(request_rest, std::make_integer_sequence<int, 2 * (NB - 2)>());
                 wait_but(rest);
                 wg_barrier();
@@ -672,6 +866,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                     fetch_v(i + NB - 1, (uint32_t)((i + NB - 1) & (NB - 1)) * C::T_BYTES);
                     wait_step();
                     wg_barrier();
+                }
                 }
             } else {
                 // prologue: scores of tile 0, the other requests of the ring spread over them
@@ -699,7 +894,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                                 else request(is_k, 2 + h / 2, (uint32_t)(2 + h / 2) * C::T_BYTES, p0, p1);
                             }
                         };
-                        for_slots(req, std::make_integer_sequence<int, 4>());
+                        if constexpr (!Q8) for_slots(req, std::make_integer_sequence<int, 4>());
+                        else if constexpr (j < Q::AHEAD) q_request_step(1 + j);
                         FDD_SCHED_FENCE();
                     };
                     static_assert(2 * (NB - 2) * C::NI <= 4 * 2 * KS, "four requests a slot");
@@ -713,8 +909,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                 // there while another one is still reading.  (They can be far apart here: the first workgroups of a
                 // launch fetch these instructions from memory.)
                 FDD_SCHED_FENCE();
-                wait_but(rest);        // V0, K1
-                wg_barrier();
+                if constexpr (Q8) {
+                    q_first();
+                } else {
+                    wait_but(rest);        // V0, K1
+                    wg_barrier();
+                }
 
                 // One pipelined step: probabilities and P V of tile i from s_cur while the scores of tile i+1 go to s_nxt.
                 //   slots  0-15  S(i+1), first and second 32 keys  ||  exponentials of tile i
@@ -735,7 +935,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                 auto step = [&](auto par, int i, f32x16 (&s_cur)[2], f32x16 (&s_nxt)[2]) {
                     constexpr int P = decltype(par)::value;
                     constexpr uint32_t KSLOT = (uint32_t)((P + 1) % NB) * C::T_BYTES;
-                    constexpr uint32_t VSLOT = (uint32_t)P * C::T_BYTES;
+                    constexpr uint32_t VSLOT = (uint32_t)(P % NB) * C::T_BYTES;
                     constexpr uint32_t KNEW = (uint32_t)P * C::T_BYTES, VNEW = (uint32_t)((P + NB - 1) % NB) * C::T_BYTES;
                     constexpr int AH = 3;                                         // fragments requested ahead
                     constexpr int NS = 2 * KS, NPV = 4 * DB, NSL = NS + NPV;      // slots of the scores, of P V, of the step
@@ -766,6 +966,29 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                         pw[k / 4][k % 4] = u;
                     };
                     bf16x8 f[AH + 1];
+                    // Q8: what the step does for later tiles, spread over its slots: a piece's codes are read, converted (8 at a time), and
+                    // the piece AHEAD steps on is requested.  K of tile i+2 goes into the slot of K of tile i (read last in step i-1),
+                    // V of tile i+1 into that of tile i-1, codes into slots that were converted in step i-1.
+                    constexpr int NE = Q::HALF ? 4 : 8 * Q::NP;
+                    Codes codes;
+                    auto event = [&](auto ec) {
+                        constexpr int e = decltype(ec)::value;
+                        const std::integral_constant<int, e / 4 % Q::NP> piece;
+                        const bool v = Q::HALF ? q_v : e / 4 / Q::NP == 1;
+                        // (the ring slots of codes and tiles by the step's place among four: constants)
+                        const int jc = i + (v ? 1 : 2), jr = jc + Q::AHEAD;
+                        if constexpr (e % 4 == 0) {
+                            if constexpr (e == 0) wait_vm<(Q::AHEAD - 1) * Q::LOADS>();
+                            codes = q_read(v, jc, piece);
+                        } else if constexpr (e % 4 < 3) {
+                            q_write(v, jc, piece, std::integral_constant<int, e % 4 - 1>(), codes);
+                        } else {
+                            q_request(v, jr, piece);
+                        }
+                    };
+                    if constexpr (Q8 && P == 0) {
+                        if ((i & 63) == 0 && i > 0) q_scales(i + 64);
+                    }
                     FDD_SCHED_FENCE();
 #pragma unroll
                     for (int j = 0; j < AH; ++j) f[j] = frag(j);
@@ -793,7 +1016,13 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                             o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[j % (AH + 1)], __builtin_bit_cast(bf16x8, pw[t4]), o[db], 0, 0, 0);
                         }
                         FDD_SCHED_FENCE();
-                        if constexpr (j % 2 == 1) {
+                        if constexpr (Q8) {
+                            auto ev = [&](auto ec) {
+                                if constexpr (1 + decltype(ec)::value * (NSL - 2) / NE == j) event(ec);
+                            };
+                            for_slots(ev, std::make_integer_sequence<int, NE>());
+                            FDD_SCHED_FENCE();
+                        } else if constexpr (j % 2 == 1) {
                             constexpr int r = j / 2;
                             const std::integral_constant<int, r % C::NI> p0;
                             const std::integral_constant<int, r % C::NI + 1> p1;
@@ -832,8 +1061,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                         acc1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)pw[(k + 1) / 4][(k + 1) % 4]), ones, acc1, false);
                     }
                     l_run += acc0 + acc1;
-                    wait_step();
-                    wg_barrier();
+                    if constexpr (Q8) {
+                        wg_barrier_written();
+                    } else {
+                        wait_step();
+                        wg_barrier();
+                    }
                 };
                 const std::integral_constant<int, 0> r0;
                 const std::integral_constant<int, 1> r1;
@@ -844,7 +1077,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                     if (++i == F) break;
                     step(r1, i, sb, sa);
                     if (++i == F) break;
-                    if constexpr (NB == 4) {
+                    if constexpr (NB == 4 || Q8) {
                         step(r2, i, sa, sb);
                         if (++i == F) break;
                         step(r3, i, sb, sa);
@@ -1164,12 +1397,12 @@ __global__ __launch_bounds__(256) void attn_merge_bf16_kernel(MergeArgs a)
     *reinterpret_cast<bf16x4*>(op + 8) = hi;
 }
 
-template <int D, int WAVES, int SLOTS, bool PACKED>
-hipError_t launch(const Args& a, bool pack_now, hipStream_t stream, hipEvent_t before_main)
+template <int D, int WAVES, int SLOTS, bool PACKED, bool Q8 = false>
+hipError_t launch(const std::conditional_t<Q8, QuantArgs, Args>& a, bool pack_now, hipStream_t stream, hipEvent_t before_main)
 {
     using C = Cfg<D, WAVES, SLOTS>;
-    const size_t lds_bytes = C::LDS_BYTES;
-    const auto kern = &attn_bf16_kernel<D, WAVES, SLOTS, PACKED>;
+    const size_t lds_bytes = Q8 ? (size_t)QuantCfg<D, WAVES>::LDS_BYTES : (size_t)C::LDS_BYTES;
+    const auto kern = &attn_bf16_kernel<D, WAVES, SLOTS, PACKED, Q8>;
     // the LDS limit of this instantiation is raised once per device (bit d of `done`: device d)
     static std::atomic<uint64_t> done{0};
     int dev = 0;
@@ -1200,9 +1433,8 @@ hipError_t launch(const Args& a, bool pack_now, hipStream_t stream, hipEvent_t b
 
 using namespace attn_bf16;
 
-hipError_t launch_attn_bf16(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s, hipEvent_t before_main)
+static void fill_args(Args& a, const fdd_attn_params& p, const AttnPlan& plan, float scale)
 {
-    Args a;
     a.q = static_cast<const uint16_t*>(p.q);
     a.pk = static_cast<const uint16_t*>(p.prefix_k);
     a.pv = static_cast<const uint16_t*>(p.prefix_v);
@@ -1250,6 +1482,13 @@ hipError_t launch_attn_bf16(const fdd_attn_params& p, const AttnPlan& plan, floa
     // (with 2..16 pieces of 32 units or more a shift of 3 % is at least one unit)
     a.w_even = 100;
     a.w_odd = (a.S >= 2 && a.S <= 16 && a.TPU >= 32 * a.S) ? ODD_XCD_WEIGHT : 100;
+}
+
+hipError_t launch_attn_bf16(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s, hipEvent_t before_main)
+{
+    Args a;
+    fill_args(a, p, plan, scale);
+    const bool pack_now = plan.packed && !p.prefix_v_packed;
     auto go = [&](auto waves, auto slots) {
         constexpr int WAVES = decltype(waves)::value, SLOTS = decltype(slots)::value;
         if (plan.packed)
@@ -1261,6 +1500,25 @@ hipError_t launch_attn_bf16(const fdd_attn_params& p, const AttnPlan& plan, floa
     const std::integral_constant<int, 2> s2;
     if (plan.mtile_rows == 256) return go(w8, s4);
     if (plan.mtile_rows == 128) return plan.slots == 2 ? go(w4, s2) : go(w4, s4);
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_attn_quant(const fdd_attn_params& p, const fdd_quant_cache* cache, const AttnPlan& plan, float scale, hipStream_t s, hipEvent_t before_main)
+{
+    QuantArgs a;
+    fill_args(a, p, plan, scale);
+    const fdd_quant_cache none = {};
+    const fdd_quant_cache& c = p.L > 0 ? *cache : none;
+    a.pk = static_cast<const uint16_t*>(c.k);
+    a.pv = static_cast<const uint16_t*>(c.v);
+    a.p_bs = c.batch_stride;
+    a.ks = c.k_scale;
+    a.vs = c.v_scale;
+    a.s_bs = c.scale_batch_stride;
+    a.head_bytes = (long long)c.capacity * p.D;
+    a.head_scales = c.capacity / KT;
+    if (plan.mtile_rows == 256) return p.D == 128 ? launch<128, 8, 2, false, true>(a, false, s, before_main) : launch<64, 8, 2, false, true>(a, false, s, before_main);
+    if (plan.mtile_rows == 128) return p.D == 128 ? launch<128, 4, 2, false, true>(a, false, s, before_main) : launch<64, 4, 2, false, true>(a, false, s, before_main);
     return hipErrorInvalidValue;
 }
 

@@ -76,6 +76,8 @@ fdd_status set_error(fdd_status code, const char* fmt, ...) __attribute__((forma
 // prefix_v (not a cache in 8 bits, which is checked where it is used); `fn` names the entry point in messages.
 fdd_status check_attn_shape(const fdd_attn_params* p, const char* fn, bool own_prefix);
 fdd_status check_attn_pointers(const fdd_attn_params* p, const char* fn, bool own_prefix);
+// the events of fdd_profile_attn_events on this thread, or nullptrs
+void attn_events(hipEvent_t* start, hipEvent_t* stop);
 // Host-side checks of an unmask call (everything but the workspace); `fn` names the entry point in messages.
 fdd_status check_unmask_args(const fdd_unmask_params* p, const char* fn);
 
@@ -173,6 +175,8 @@ __host__ __device__ inline int unit_begin(int w, int base, int rem) { return w *
 
 // `before_main`, if not null, is recorded on the stream right before the main kernel (after the V pre-pass).
 hipError_t launch_attn_bf16(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s, hipEvent_t before_main);
+// the same with the prefix in a cache of 8 bits (nullptr: no prefix); p's own prefix is not used
+hipError_t launch_attn_quant(const fdd_attn_params& p, const fdd_quant_cache* cache, const AttnPlan& plan, float scale, hipStream_t s, hipEvent_t before_main);
 hipError_t launch_prefix_pack(const void* prefix_v, int L, int Hkv, int D, void* packed, hipStream_t s);
 // K and V of the first `rows` rows of a cache of 8 bits, [batch][rows,Hkv,D] of type `dtype`, problems batch_stride elements apart
 hipError_t launch_dequantize(const fdd_quant_cache& c, int row0, const fdd_quant_rows& dst, int batch, long long batch_stride, hipStream_t s);

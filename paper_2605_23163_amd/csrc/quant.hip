@@ -12,6 +12,8 @@
 //   quantize    one workgroup per (block of 64 rows, KV head, K or V): it holds the block in registers between the
 //               maximum and the rounding, so a row is read once.
 //   dequantize  one thread per 16 elements in the order of the destination.
+#include <cmath>
+
 #include "fdd_internal.h"
 #include "wave.h"
 
@@ -318,6 +320,16 @@ fdd_attn_params plain_call(const fdd_attn_params& p)
     return q;
 }
 
+// Whether a call converts the prefix tile by tile, in the attention kernel, and its plan.
+bool plan_by_tile(const fdd_attn_params& p, AttnPlan* plan)
+{
+    if (p.dtype != FDD_BF16) return false;
+    make_attn_plan(p, plan);
+    plan->packed = false;
+    plan->ws_vt_bytes = 0;
+    return true;
+}
+
 const char* const kAttn = "fdd_block_attn_quant";
 
 }  // namespace
@@ -345,6 +357,8 @@ fdd_status fdd_prefix_dequantize(const fdd_quant_cache* cache, int32_t row0, con
 size_t fdd_block_attn_quant_workspace(const fdd_attn_params* p)
 {
     if (check_attn_shape(p, kAttn, false) != FDD_OK) return 0;
+    AttnPlan plan;
+    if (plan_by_tile(*p, &plan)) return plan.ws_o_bytes + plan.ws_ml_bytes;
     const fdd_attn_params q = plain_call(*p);
     return 2 * plain_bytes(*p) + fdd_block_attn_workspace(&q);
 }
@@ -373,10 +387,22 @@ fdd_status fdd_block_attn_quant(const fdd_attn_params* p, const fdd_quant_cache*
         if (!aligned(p->workspace, 256)) return fail(FDD_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", kAttn);
         if (p->workspace_bytes < need) return fail(FDD_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", kAttn, p->workspace_bytes, need);
     }
+    const hipStream_t stream = static_cast<hipStream_t>(p->stream);
+    AttnPlan plan;
+    if (plan_by_tile(*p, &plan)) {
+        const float scale = p->scale > 0.f ? p->scale : 1.f / std::sqrt((float)p->D);
+        hipEvent_t start, stop;
+        attn_events(&start, &stop);
+        hipError_t e = launch_attn_quant(*p, cache, plan, scale, stream, start);
+        if (e == hipSuccess && stop) e = hipEventRecord(stop, stream);
+        if (e == hipSuccess && plan.ws_o_bytes > 0) e = launch_attn_merge_bf16(*p, plan, scale, stream);
+        if (e != hipSuccess) return fail(FDD_ERR_LAUNCH, "%s: launch failed: %s", kAttn, hipGetErrorString(e));
+        return FDD_OK;
+    }
     const fdd_attn_params q = plain_call(*p);
     if (p->L > 0) {
         fdd_quant_rows rows = {const_cast<void*>(q.prefix_k), const_cast<void*>(q.prefix_v), 0, 0, p->L, p->dtype};
-        hipError_t e = launch_dequantize(*cache, 0, rows, p->batch > 1 ? p->batch : 1, q.prefix_batch_stride, static_cast<hipStream_t>(p->stream));
+        hipError_t e = launch_dequantize(*cache, 0, rows, p->batch > 1 ? p->batch : 1, q.prefix_batch_stride, stream);
         if (e != hipSuccess) return fail(FDD_ERR_LAUNCH, "%s: launch failed: %s", kAttn, hipGetErrorString(e));
     }
     return fdd_block_attn(&q);
