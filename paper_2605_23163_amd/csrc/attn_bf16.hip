@@ -463,43 +463,47 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
             qks = a.ks + pb * a.s_bs + (long long)kh * a.head_scales;
             qvs = a.vs + pb * a.s_bs + (long long)kh * a.head_scales;
         }
-        // (a request for a tile that there is not reads nothing and leaves zeros)
-        auto q_request = [&](bool v, int j, auto piece) {
+        // (whole descriptors and constant ring slots: beside a matrix instruction every scalar instruction counts as much as a vector
+        // one.  Instead of a tile that there is not the last one is requested again.)
+        const __amdgpu_buffer_rsrc_t qk_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(qk), 0, (uint32_t)a.L * D, RSRC_FLAGS);
+        const __amdgpu_buffer_rsrc_t qv_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(qv), 0, (uint32_t)a.L * D, RSRC_FLAGS);
+        const uint32_t q_ring = Q8 ? (uint32_t)(size_t)(lds_void*)lds + q_wave * (Q::NP * 1024) : 0u;      // this wavefront's part of a slot
+        auto q_request = [&](bool v, int j, int slot, auto piece) {
             constexpr int jn = decltype(piece)::value;
-            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(v ? qv : qk), 0, j < F ? (uint32_t)a.L * D : 0u, RSRC_FLAGS);
-            unsigned char* const dst = lds + (v ? Q::V_RING : Q::K_RING) + (j & (Q::SLOTS - 1)) * Q::T_BYTES + q_wave * (Q::NP * 1024);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)dst, 16, q_rd, (uint32_t)(t0 + j) * Q::T_BYTES, jn * 1024, 0);
+            const uint32_t soff = (uint32_t)(t0 + min(j, F - 1)) * Q::T_BYTES;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(v ? qv_rsrc : qk_rsrc, (lds_void*)(size_t)(q_ring + (v ? Q::V_RING : Q::K_RING) + slot * Q::T_BYTES), 16, q_rd, soff,
+                                                     jn * 1024, 0);
         };
-        auto q_scales = [&](int j) {      // of tiles j .. j + 63, j a multiple of 64; every wavefront for itself, into one place
-            const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(qks), 0, (uint32_t)a.TP * 4, RSRC_FLAGS);
-            const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(qvs), 0, (uint32_t)a.TP * 4, RSRC_FLAGS);
-            unsigned char* const dst = lds + Q::SCALES + (j & 64) * 4;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void*)dst, 4, (uint32_t)lane * 4, (uint32_t)(t0 + j) * 4, 0, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(dst + 512), 4, (uint32_t)lane * 4, (uint32_t)(t0 + j) * 4, 0, 0);
+        // Scales that the steps i .. i + 63 use, i a multiple of 64: of K of tile i + 2 and of V of tile i + 1 on.  Every wavefront
+        // requests them for itself, into one place.
+        auto q_scales = [&](int i) {
+            const int at = min(t0 + i + 1, a.TP);      // (entries behind the last tile's are zeros)
+            const __amdgpu_buffer_rsrc_t v_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(qvs + at), 0, (uint32_t)(a.TP - at) * 4, RSRC_FLAGS);
+            const __amdgpu_buffer_rsrc_t k_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(qks + min(at + 1, a.TP)), 0, (uint32_t)(a.TP - min(at + 1, a.TP)) * 4, RSRC_FLAGS);
+            unsigned char* const dst = lds + Q::SCALES + (i & 64) * 4;
+            uint32_t lane4 = q_rd;      // (worked out here, like the lane below: nothing stays in a register for it)
+            FDD_PIN(lane4);
+            lane4 = (lane4 >> 2) & 255u;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(k_rsrc, (lds_void*)dst, 4, lane4, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(v_rsrc, (lds_void*)(dst + 512), 4, lane4, 0, 0, 0);
         };
-        struct Codes {
-            u32x4 w;
-            float scale;
-        };
-        auto q_read = [&](bool v, int j, auto piece) {
+        auto q_scale = [&](bool v, int i) { return read_scale((const lds_f32*)(lds + Q::SCALES + (v ? 512 : 0) + (i & 127) * 4)); };
+        auto q_read = [&](bool v, int slot, auto piece) {
             constexpr int jn = decltype(piece)::value;
-            Codes c;
-            c.w = read_codes((const lds_u32x4*)(lds + q_rd + ((v ? Q::V_RING : Q::K_RING) + (j & (Q::SLOTS - 1)) * Q::T_BYTES + jn * 1024)));
-            c.scale = read_scale((const lds_f32*)(lds + Q::SCALES + (v ? 512 : 0) + (j & 127) * 4));
-            return c;
+            return read_codes((const lds_u32x4*)(lds + q_rd + ((v ? Q::V_RING : Q::K_RING) + slot * Q::T_BYTES + jn * 1024)));
         };
-        auto q_write = [&](bool v, int j, auto piece, auto half, const Codes& c) {
+        auto q_write = [&](bool v, int slot, auto piece, auto half, const u32x4& codes, float scale) {
             constexpr int jn = decltype(piece)::value, h = decltype(half)::value;
-            const uint32_t at = v ? q_wv + C::V_RING : q_wk ^ (jn * K_XOR);
-            *reinterpret_cast<u32x4*>(lds + (at ^ (h * 16)) + ((j & 1) * C::T_BYTES + jn * Q_ROWS * D * 2)) = convert8(c.w[2 * h], c.w[2 * h + 1], c.scale);
+            const uint32_t at = v ? q_wv + (C::V_RING + h * 16) : (q_wk ^ (jn * K_XOR)) ^ (h * 16);       // (V: its swizzle leaves that bit 0)
+            *reinterpret_cast<u32x4*>(lds + at + (slot * C::T_BYTES + jn * Q_ROWS * D * 2)) = convert8(codes[2 * h], codes[2 * h + 1], scale);
         };
         const std::integral_constant<int, 0> p_0;
         const std::integral_constant<int, 1> p_1;
-        auto q_convert = [&](bool v, int j) {     // all of this wavefront's pieces of tile j
+        auto q_convert = [&](bool v, int slot, int tile_slot, float scale) {     // all of this wavefront's pieces of a tile
             auto one = [&](auto piece) {
-                const Codes c = q_read(v, j, piece);
-                q_write(v, j, piece, p_0, c);
-                q_write(v, j, piece, p_1, c);
+                const u32x4 c = q_read(v, slot, piece);
+                q_write(v, tile_slot, piece, p_0, c, scale);
+                q_write(v, tile_slot, piece, p_1, c, scale);
             };
             for_slots(one, std::make_integer_sequence<int, Q::NP>());
         };
@@ -507,14 +511,15 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
         auto q_request_step = [&](int j) {
             auto one = [&](auto piece) {
                 if constexpr (Q::HALF) {
-                    q_request(q_v, q_v ? j : j + 1, piece);
+                    q_request(q_v, q_v ? j : j + 1, (q_v ? j : j + 1) & 3, piece);
                 } else {
-                    q_request(false, j + 1, piece);
-                    q_request(true, j, piece);
+                    q_request(false, j + 1, (j + 1) & 3, piece);
+                    q_request(true, j, j & 3, piece);
                 }
             };
             for_slots(one, std::make_integer_sequence<int, Q::NP>());
         };
+        float q_k0 = 0.f, q_k1 = 0.f, q_v0 = 0.f;      // scales of the tiles converted before the first step
         const std::integral_constant<int, C::NI> p_all;
         const std::true_type is_v;
         const std::false_type is_k;
@@ -550,18 +555,23 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
         // Only what the first step needs is requested here; the rest of the ring follows in the shadow of its first scores (all at
         // once, every workgroup's first tile waited behind the others' fourth: first barrier 4.5 -> 4.0 us after the start at N=8, L=4096).
         if constexpr (Q8) {
-            q_scales(0);
-            q_scales(64);
-            if constexpr (Q::HALF) {
-                q_request(q_v, 0, p_0);
-                if (!q_v) q_request(false, 1, p_0);
-            } else {
-                auto first = [&](auto piece) { q_request(false, 0, piece); };
-                auto second = [&](auto piece) { q_request(true, 0, piece); };
-                auto third = [&](auto piece) { q_request(false, 1, piece); };
-                for_slots(first, std::make_integer_sequence<int, Q::NP>());
-                for_slots(second, std::make_integer_sequence<int, Q::NP>());
-                for_slots(third, std::make_integer_sequence<int, Q::NP>());
+            if (F > 0) {
+                q_k0 = qks[t0];
+                q_v0 = qvs[t0];
+                q_k1 = qks[min(t0 + 1, a.TP - 1)];
+                q_scales(0);
+                q_scales(64);
+                if constexpr (Q::HALF) {
+                    q_request(q_v, 0, 0, p_0);
+                    if (!q_v) q_request(false, 1, 1, p_0);
+                } else {
+                    auto first = [&](auto piece) { q_request(false, 0, 0, piece); };
+                    auto second = [&](auto piece) { q_request(true, 0, 0, piece); };
+                    auto third = [&](auto piece) { q_request(false, 1, 1, piece); };
+                    for_slots(first, std::make_integer_sequence<int, Q::NP>());
+                    for_slots(second, std::make_integer_sequence<int, Q::NP>());
+                    for_slots(third, std::make_integer_sequence<int, Q::NP>());
+                }
             }
         } else {
             fetch_k(0, 0);
@@ -722,15 +732,16 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
         // Q8: the ragged last prefix tile, through registers
         auto fetch_codes = [&](int j) {
             const Tile t = tile_at(j);
+            int tid_f = tid;
+            FDD_PIN(tid_f);
+            const int lane = tid_f & 63;
             auto one = [&](bool v, auto piece) {
                 constexpr int jn = decltype(piece)::value;
-                const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(v ? qv : qk), 0, (uint32_t)a.L * D, RSRC_FLAGS);
                 const int r = (q_wave * Q::NP + jn) * Q_ROWS + lane / (D / 16);
-                Codes c;
-                c.w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (uint32_t)(min(r, t.valid - 1) * D + lane % (D / 16) * 16), (uint32_t)t.row_base * D, 0));
-                c.scale = (v ? qvs : qks)[t0 + j];
-                q_write(v, j, piece, p_0, c);
-                q_write(v, j, piece, p_1, c);
+                const u32x4 c = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(v ? qv_rsrc : qk_rsrc, (uint32_t)(min(r, t.valid - 1) * D + lane % (D / 16) * 16), (uint32_t)t.row_base * D, 0));
+                const float scale = (v ? qvs : qks)[t0 + j];
+                q_write(v, j & 1, piece, p_0, c, scale);
+                q_write(v, j & 1, piece, p_1, c, scale);
             };
             auto both = [&](auto piece) {
                 if constexpr (Q::HALF) {
@@ -823,7 +834,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
             const std::integral_constant<int, (NB - 2) * 2 * C::NI> rest;
             if constexpr (Q8) {
                 wait_vm<Q::HALF ? 0 : 2 * Q::NP>();      // Q, scales, K0
-                if (!q_v) q_convert(false, 0);
+                if (!q_v) q_convert(false, 0, 0, q_k0);
                 wg_barrier_written();
             } else {
                 wait_but(first);       // Q, K0
@@ -832,8 +843,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
             // Q8: V0 and K1, once the first AHEAD steps' codes have been requested
             auto q_first = [&] {
                 wait_vm<Q::AHEAD * Q::LOADS>();
-                if (!Q::HALF || q_v) q_convert(true, 0);
-                if (!Q::HALF || !q_v) q_convert(false, 1);
+                if (!Q::HALF || q_v) q_convert(true, 0, 0, q_v0);
+                if (!Q::HALF || !q_v) q_convert(false, 1, 1, q_k1);
                 wg_barrier_written();
             };
             // what the ring still has room for: V1 K2 V2 K3
@@ -852,8 +863,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                     for (int i = 0; i < F; ++i) {
                         if ((i & 63) == 0 && i > 0) q_scales(i + 64);
                         wait_vm<(Q::AHEAD - 1) * Q::LOADS>();
-                        if (!Q::HALF || !q_v) q_convert(false, i + 2);
-                        if (!Q::HALF || q_v) q_convert(true, i + 1);
+                        if (!Q::HALF || !q_v) q_convert(false, (i + 2) & 3, i & 1, q_scale(false, i));
+                        if (!Q::HALF || q_v) q_convert(true, (i + 1) & 3, (i + 1) & 1, q_scale(true, i));
                         q_request_step(i + 1 + Q::AHEAD);
                         wg_barrier_written();
                     }
@@ -937,7 +948,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                     constexpr uint32_t KSLOT = (uint32_t)((P + 1) % NB) * C::T_BYTES;
                     constexpr uint32_t VSLOT = (uint32_t)(P % NB) * C::T_BYTES;
                     constexpr uint32_t KNEW = (uint32_t)P * C::T_BYTES, VNEW = (uint32_t)((P + NB - 1) % NB) * C::T_BYTES;
-                    constexpr int AH = 3;                                         // fragments requested ahead
+                    constexpr int AH = Q8 && D == 128 && WAVES == 4 ? 2 : 3;      // fragments requested ahead
                     constexpr int NS = 2 * KS, NPV = 4 * DB, NSL = NS + NPV;      // slots of the scores, of P V, of the step
                     typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
                     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
@@ -970,20 +981,24 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                     // the piece AHEAD steps on is requested.  K of tile i+2 goes into the slot of K of tile i (read last in step i-1),
                     // V of tile i+1 into that of tile i-1, codes into slots that were converted in step i-1.
                     constexpr int NE = Q::HALF ? 4 : 8 * Q::NP;
-                    Codes codes;
+                    if constexpr (Q8) {       // (the pieces' places are worked out where they are used: kept from step to step they cost what is left of the registers)
+                        FDD_PIN(q_wk);
+                        FDD_PIN(q_wv);
+                    }
+                    u32x4 codes;
+                    float code_scale = 0.f;
                     auto event = [&](auto ec) {
                         constexpr int e = decltype(ec)::value;
                         const std::integral_constant<int, e / 4 % Q::NP> piece;
                         const bool v = Q::HALF ? q_v : e / 4 / Q::NP == 1;
-                        // (the ring slots of codes and tiles by the step's place among four: constants)
-                        const int jc = i + (v ? 1 : 2), jr = jc + Q::AHEAD;
                         if constexpr (e % 4 == 0) {
                             if constexpr (e == 0) wait_vm<(Q::AHEAD - 1) * Q::LOADS>();
-                            codes = q_read(v, jc, piece);
+                            codes = q_read(v, v ? (P + 1) % 4 : (P + 2) % 4, piece);
+                            if constexpr (e % (4 * Q::NP) == 0) code_scale = q_scale(v, i);
                         } else if constexpr (e % 4 < 3) {
-                            q_write(v, jc, piece, std::integral_constant<int, e % 4 - 1>(), codes);
+                            q_write(v, v ? (P + 1) % 2 : P % 2, piece, std::integral_constant<int, e % 4 - 1>(), codes, code_scale);
                         } else {
-                            q_request(v, jr, piece);
+                            q_request(v, i + (v ? 1 : 2) + Q::AHEAD, (P + (v ? 1 : 2) + Q::AHEAD) % 4, piece);
                         }
                     };
                     if constexpr (Q8 && P == 0) {
