@@ -59,6 +59,14 @@ class QuantRows(C.Structure):
                 ("rows", C.c_int32), ("dtype", C.c_int32)]
 
 
+class QuantCall(C.Structure):
+    _fields_ = [("cache", QuantCache), ("rows", QuantRows)]
+
+
+class AttnQuantCall(C.Structure):
+    _fields_ = [("p", AttnParams), ("cache", QuantCache)]
+
+
 class LogprobParams(C.Structure):
     _fields_ = [("N", C.c_int32), ("B", C.c_int32), ("V", C.c_int64), ("dtype", C.c_int32), ("top", C.c_int32),
                 ("temperature", C.c_float), ("reserved", C.c_int32), ("logits", C.c_void_p), ("tokens", C.c_void_p),
@@ -118,7 +126,9 @@ def _import_marshal():
         from . import _marshal as m
     except ImportError:
         return None
-    fits = torch.__version__.split("+")[0] == m.torch_version and (m.attn_bytes, m.unmask_bytes) == (C.sizeof(AttnParams), C.sizeof(UnmaskParams))
+    fits = torch.__version__.split("+")[0] == m.torch_version and \
+        (m.attn_bytes, m.unmask_bytes, m.quant_bytes, m.attn_quant_bytes, m.logprobs_bytes) == \
+        tuple(C.sizeof(t) for t in (AttnParams, UnmaskParams, QuantCall, AttnQuantCall, LogprobParams))
     return m if fits else None
 
 
@@ -143,17 +153,17 @@ def load_library():
         lib.fdd_prefix_pack.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t,
                                         C.c_void_p]
         lib.fdd_prefix_quantize.restype = C.c_int
-        lib.fdd_prefix_quantize.argtypes = [C.POINTER(QuantCache), C.c_int32, C.POINTER(QuantRows), C.c_void_p]
+        lib.fdd_prefix_quantize.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
         lib.fdd_prefix_dequantize.restype = C.c_int
-        lib.fdd_prefix_dequantize.argtypes = [C.POINTER(QuantCache), C.c_int32, C.POINTER(QuantRows), C.c_void_p]
+        lib.fdd_prefix_dequantize.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
         lib.fdd_block_attn_quant_workspace.restype = C.c_size_t
-        lib.fdd_block_attn_quant_workspace.argtypes = [C.POINTER(AttnParams)]
+        lib.fdd_block_attn_quant_workspace.argtypes = [C.c_void_p]
         lib.fdd_block_attn_quant.restype = C.c_int
-        lib.fdd_block_attn_quant.argtypes = [C.POINTER(AttnParams), C.POINTER(QuantCache)]
+        lib.fdd_block_attn_quant.argtypes = [C.c_void_p, C.c_void_p]
         lib.fdd_token_logprobs_workspace.restype = C.c_size_t
-        lib.fdd_token_logprobs_workspace.argtypes = [C.POINTER(LogprobParams)]
+        lib.fdd_token_logprobs_workspace.argtypes = [C.c_void_p]
         lib.fdd_token_logprobs.restype = C.c_int
-        lib.fdd_token_logprobs.argtypes = [C.POINTER(LogprobParams)]
+        lib.fdd_token_logprobs.argtypes = [C.c_void_p]
         lib.fdd_unmask_workspace.restype = C.c_size_t
         lib.fdd_unmask_workspace.argtypes = [C.POINTER(UnmaskParams)]
         lib.fdd_unmask_step.restype = C.c_int
@@ -227,6 +237,15 @@ def _stream_ptr(stream):
     # the current stream's handle without a stream object around it (0.3 us instead of 2.7), where this torch has that
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
+
+
+def _device_and_stream(stream):
+    """The current device's index, and the handle of the call's stream."""
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -1
+    if stream is not None:
+        return dev, stream.cuda_stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return dev, None if dev < 0 else torch.cuda.current_stream().cuda_stream if raw is None else raw(dev)
 
 
 def _maker(stream, device, make, returned=True):
@@ -472,34 +491,48 @@ def _quant_rows(k, v, cache, row0):
     return r
 
 
+_ROWS_AT = QuantCall.rows.offset
+_CACHE_AT = AttnQuantCall.cache.offset
+
+
+def _quant_call(k, v, prefix, row0, dev):
+    c = QuantCall()
+    if _marshal is None or not _marshal.quant(C.addressof(c), k, v, prefix, row0, dev):
+        c.cache = _quant_cache(prefix)
+        c.rows = _quant_rows(k, v, c.cache, row0)
+    return c
+
+
 def fdd_prefix_quantize(k, v, prefix, row0=0, stream=None):
     """The rows k, v [rows,Hkv,D] (bf16 or fp32; rows may lie apart) become rows [row0, row0 + rows) of the cache
     ``prefix``, which then ends with them (in place); returns row0 + rows, the number of rows it holds."""
     lib = load_library()
-    cache = _quant_cache(prefix)
-    r = _quant_rows(k, v, cache, int(row0))
-    _check(lib.fdd_prefix_quantize(C.byref(cache), int(row0), C.byref(r), _stream_ptr(stream)))
-    return int(row0) + r.rows
+    row0 = int(row0)
+    dev, handle = _device_and_stream(stream)
+    c = _quant_call(k, v, prefix, row0, dev)
+    _check(lib.fdd_prefix_quantize(C.addressof(c), row0, C.addressof(c) + _ROWS_AT, handle))
+    return row0 + c.rows.rows
 
 
 def fdd_prefix_dequantize(prefix, rows, row0=0, dtype=None, k=None, v=None, stream=None):
     """Rows [row0, row0 + rows) of the cache as (k, v) [rows,Hkv,D], exactly; ``dtype`` bf16 (default) or fp32, or into
     the given k and v."""
     lib = load_library()
-    cache = _quant_cache(prefix)
     if (k is None) != (v is None):
         raise ValueError("give both k and v, or neither")
     rows, row0 = int(rows), int(row0)
-    if rows < 0 or not 0 <= row0 <= cache.capacity - rows:
-        raise ValueError(f"rows [{row0}, {row0 + rows}) do not fit a cache of {cache.capacity}")
     if k is None:
-        dev = prefix.k.device
-        new = torch.empty if stream is None else _maker(stream, dev, torch.empty)
-        k, v = (new((rows, cache.Hkv, cache.D), dtype=torch.bfloat16 if dtype is None else dtype, device=dev) for _ in range(2))
+        cache = _quant_cache(prefix)
+        if rows < 0 or not 0 <= row0 <= cache.capacity - rows:
+            raise ValueError(f"rows [{row0}, {row0 + rows}) do not fit a cache of {cache.capacity}")
+        device = prefix.k.device
+        new = torch.empty if stream is None else _maker(stream, device, torch.empty)
+        k, v = (new((rows, cache.Hkv, cache.D), dtype=torch.bfloat16 if dtype is None else dtype, device=device) for _ in range(2))
     elif k.dim() != 3 or k.shape[0] != rows or (dtype is not None and k.dtype != dtype):
         raise ValueError("k / v must be [rows,Hkv,D] of the requested type")
-    r = _quant_rows(k, v, cache, row0)
-    _check(lib.fdd_prefix_dequantize(C.byref(cache), row0, C.byref(r), _stream_ptr(stream)))
+    dev, handle = _device_and_stream(stream)
+    c = _quant_call(k, v, prefix, row0, dev)
+    _check(lib.fdd_prefix_dequantize(C.addressof(c), row0, C.addressof(c) + _ROWS_AT, handle))
     return k, v
 
 
@@ -536,15 +569,22 @@ def fdd_block_attn_quant(q, prefix, L, block_k, block_v, scaffold_mask=None, out
     lib = load_library()
     if out is None:
         out = (torch.empty_like if stream is None else _maker(stream, q.device, torch.empty_like))(q)
-    p, cache = _quant_attn_params(q, prefix, L, block_k, block_v, scaffold_mask, out, scale, splits, causal_block, ext_k, ext_v, E)
-    if q_positions is not None:
-        _on_current_device(q_positions)
-        _set_q_positions(p, q_positions)
-        if p.n_q_positions == 0:      # (0 stands for all positions in the library)
-            return out
+    dev, handle = _device_and_stream(stream)
+    c = AttnQuantCall()
+    if _marshal is None or prefix is None or not _marshal.attn_quant(C.addressof(c), q, prefix, L, block_k, block_v, scaffold_mask, out, ext_k, ext_v,
+                                                                    q_positions, E, causal_block, splits, scale, dev):
+        c.p, cache = _quant_attn_params(q, prefix, L, block_k, block_v, scaffold_mask, out, scale, splits, causal_block, ext_k, ext_v, E)
+        if cache is not None:
+            c.cache = cache
+        if q_positions is not None:
+            _on_current_device(q_positions)
+            _set_q_positions(c.p, q_positions)
+            if c.p.n_q_positions == 0:      # (0 stands for all positions in the library)
+                return out
+    p = c.p
     ws = _set_workspace(p, workspace, lib.fdd_block_attn_quant_workspace, q.device, stream)  # noqa: F841
-    p.stream = _stream_ptr(stream)
-    _check(lib.fdd_block_attn_quant(C.byref(p), None if cache is None else C.byref(cache)))
+    p.stream = handle
+    _check(lib.fdd_block_attn_quant(C.addressof(c), None if prefix is None else C.addressof(c) + _CACHE_AT))
     return out
 
 
@@ -593,14 +633,7 @@ def fdd_token_logprobs_workspace(logits, top=0) -> int:
     return load_library().fdd_token_logprobs_workspace(C.byref(p))
 
 
-def fdd_token_logprobs(logits, tokens, mask=None, top=0, temperature=1.0, logprobs=None, entropy=None, top_ids=None, top_logprobs=None,
-                       workspace=None, stream=None):
-    """Log probabilities of ``tokens`` [N,B] under softmax(logits [N,B,V] / temperature), the entropy of every row and
-    its ``top`` most probable tokens (see include/fdd.h).  ``mask`` (uint8 [N,B]): only positions where it is 1;
-    the others' outputs stay as they were (0, and ids -1, in outputs that are allocated here).
-
-    Returns (logprobs [N,B], entropy [N,B], top_ids [N,B,top], top_logprobs [N,B,top])."""
-    lib = load_library()
+def _logprob_arguments(logits, tokens, mask, top, temperature, logprobs, entropy, top_ids, top_logprobs, stream):
     N, B, V = logits.shape
     if tokens.dtype != torch.int32 or tokens.shape != (N, B):
         raise TypeError("tokens must be torch.int32 [N,B]")
@@ -628,10 +661,27 @@ def fdd_token_logprobs(logits, tokens, mask=None, top=0, temperature=1.0, logpro
     p.logprobs, p.entropy = _dev(outs[0], "logprobs"), _dev(outs[1], "entropy")
     if p.top:
         p.top_ids, p.top_logprobs = _dev(outs[2], "top_ids"), _dev(outs[3], "top_logprobs")
-    ws = _set_workspace(p, workspace, lib.fdd_token_logprobs_workspace, dev, stream)  # noqa: F841
-    p.stream = _stream_ptr(stream)
-    _check(lib.fdd_token_logprobs(C.byref(p)))
-    return tuple(outs)
+    return (p, *outs)
+
+
+def fdd_token_logprobs(logits, tokens, mask=None, top=0, temperature=1.0, logprobs=None, entropy=None, top_ids=None, top_logprobs=None,
+                       workspace=None, stream=None):
+    """Log probabilities of ``tokens`` [N,B] under softmax(logits [N,B,V] / temperature), the entropy of every row and
+    its ``top`` most probable tokens (see include/fdd.h).  ``mask`` (uint8 [N,B]): only positions where it is 1;
+    the others' outputs stay as they were (0, and ids -1, in outputs that are allocated here).
+
+    Returns (logprobs [N,B], entropy [N,B], top_ids [N,B,top], top_logprobs [N,B,top])."""
+    lib = load_library()
+    dev, handle = _device_and_stream(stream)
+    p = LogprobParams()
+    if logprobs is None or entropy is None or top_ids is None or top_logprobs is None or _marshal is None or not _marshal.logprobs(
+            C.addressof(p), logits, tokens, mask, top, temperature, logprobs, entropy, top_ids, top_logprobs, dev):
+        p, logprobs, entropy, top_ids, top_logprobs = _logprob_arguments(logits, tokens, mask, top, temperature, logprobs, entropy, top_ids,
+                                                                        top_logprobs, stream)
+    ws = _set_workspace(p, workspace, lib.fdd_token_logprobs_workspace, logits.device, stream)  # noqa: F841
+    p.stream = handle
+    _check(lib.fdd_token_logprobs(C.addressof(p)))
+    return logprobs, entropy, top_ids, top_logprobs
 
 
 def _unmask_params(logits, mask, scaffold_mask, tokens, tau, confidences, n_unmasked, committed, refresh=None):

@@ -1,6 +1,7 @@
-// Arguments of the two calls of a denoise step, and of a fork, from tensors to the C structs of fdd.h.
+// Arguments of the two calls of a denoise step, of a fork, and of the calls on a prefix cache in 8 bits and on log probabilities,
+// from tensors to the C structs of fdd.h.
 //
-// Host code, a CPython module: `attn` and `unmask` check shapes, types and placement as binding.py does and fill the
+// Host code, a CPython module: `attn`, `unmask`, `quant`, `attn_quant` and `logprobs` check shapes, types and placement as binding.py does and fill the
 // struct at the given address.  They return True, or False (and set no exception) for anything that is not the ordinary
 // case - a wrong shape, a tensor subclass, an active torch function mode - and binding.py's own checks then accept it or
 // raise their errors.  Nothing is kept between calls.  In Python a tensor property costs about 0.1 us, and a call reads
@@ -145,6 +146,127 @@ void fill_unmask(fdd_unmask_params* p, PyObject* const* a)
     }
 }
 
+struct QuantCall {
+    fdd_quant_cache cache;
+    fdd_quant_rows rows;
+};
+
+struct AttnQuantCall {
+    fdd_attn_params p;
+    fdd_quant_cache cache;
+};
+
+// the tensors of these calls have to be on the current device, which Python names
+struct OnDevice {
+    int64_t device;
+    const at::Tensor& operator()(PyObject* o) const
+    {
+        const at::Tensor& t = tensor(o);
+        need(t.is_cuda() && t.get_device() == device);
+        return t;
+    }
+    void* or_null(PyObject* o) const { return o == Py_None ? nullptr : pointer((*this)(o)); }
+};
+
+void fill_cache(fdd_quant_cache* c, PyObject* o, const OnDevice& on)
+{
+    need(PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 4);
+    const at::Tensor &k = on(PyTuple_GET_ITEM(o, 0)), &v = on(PyTuple_GET_ITEM(o, 1)), &ks = on(PyTuple_GET_ITEM(o, 2)), &vs = on(PyTuple_GET_ITEM(o, 3));
+    need(k.dim() == 3 && v.sizes() == k.sizes() && k.size(1) % FDD_QUANT_BLOCK == 0);
+    need(ks.dim() == 2 && ks.size(0) == k.size(0) && ks.size(1) == k.size(1) / FDD_QUANT_BLOCK && vs.sizes() == ks.sizes());
+    need(k.scalar_type() == at::kFloat8_e4m3fn && v.scalar_type() == at::kFloat8_e4m3fn && ks.scalar_type() == at::kFloat && vs.scalar_type() == at::kFloat);
+    c->k = pointer(k); c->v = pointer(v);
+    c->k_scale = (float*)pointer(ks); c->v_scale = (float*)pointer(vs);
+    c->Hkv = int32_of(k.size(0)); c->capacity = int32_of(k.size(1)); c->D = int32_of(k.size(2));
+}
+
+// k, v, prefix, row0, device
+void fill_quant(QuantCall* c, PyObject* const* a)
+{
+    const OnDevice on{int32_of(a[4])};
+    const at::Tensor &k = on(a[0]), &v = on(a[1]);
+    fill_cache(&c->cache, a[2], on);
+    need(k.dim() == 3 && v.sizes() == k.sizes() && k.size(1) == c->cache.Hkv && k.size(2) == c->cache.D && v.scalar_type() == k.scalar_type());
+    need(k.is_contiguous() && v.is_contiguous());      // (rows that lie apart are looked at in Python)
+    c->rows.rows = int32_of(k.size(0));
+    c->rows.dtype = (decltype(c->rows.dtype))dtype_code(k);
+    const int32_t row0 = int32_of(a[3]);
+    need(row0 >= 0 && row0 <= c->cache.capacity - c->rows.rows);
+    c->rows.k = k.data_ptr(); c->rows.v = v.data_ptr();
+    if (c->rows.rows > 1) { c->rows.k_row_stride = k.stride(0); c->rows.v_row_stride = v.stride(0); }
+}
+
+// q, prefix, L, block_k, block_v, scaffold_mask, out, ext_k, ext_v, q_positions, E, causal_block, splits, scale, device
+void fill_attn_quant(AttnQuantCall* c, PyObject* const* a)
+{
+    const OnDevice on{int32_of(a[14])};
+    const at::Tensor &q = on(a[0]), &bk = on(a[3]), &bv = on(a[4]);
+    fill_cache(&c->cache, a[1], on);
+    need(q.dim() == 4 && bk.dim() == 4);
+    const int64_t N = q.size(0), B = q.size(1), Hkv = bk.size(2), D = q.size(3);
+    need(bk.size(0) == N && bk.size(1) == B && bk.size(3) == D && bv.sizes() == bk.sizes());
+    need(c->cache.Hkv == Hkv && c->cache.D == D);
+    const auto type = q.scalar_type();
+    need(bk.scalar_type() == type && bv.scalar_type() == type);
+    fdd_attn_params* const p = &c->p;
+    p->N = int32_of(N); p->B = int32_of(B); p->L = int32_of(a[2]);
+    need(p->L >= 0 && p->L <= c->cache.capacity);
+    p->Hq = int32_of(q.size(2)); p->Hkv = int32_of(Hkv); p->D = int32_of(D);
+    p->dtype = (decltype(p->dtype))dtype_code(q);
+    p->scale = a[13] == Py_None ? 0.f : float_of(a[13]);
+    p->q = pointer(q);
+    p->block_k = pointer(bk); p->block_v = pointer(bv);
+    p->scaffold_mask = (decltype(p->scaffold_mask))on.or_null(a[5]);
+    p->out = pointer(on(a[6]));
+    if (a[7] != Py_None) {
+        const at::Tensor &ek = on(a[7]), &ev = on(a[8]);
+        need(ek.dim() == 4 && ek.size(0) == N && ek.size(2) == Hkv && ek.size(3) == D && ev.sizes() == ek.sizes());
+        need(ek.scalar_type() == type && ev.scalar_type() == type);
+        p->ext_k = pointer(ek); p->ext_v = pointer(ev); p->ext_capacity = int32_of(ek.size(1));
+    }
+    if (a[9] != Py_None) {
+        const at::Tensor& qp = on(a[9]);
+        need(qp.scalar_type() == at::kInt && qp.dim() == 1 && qp.numel() > 0);
+        p->q_positions = (decltype(p->q_positions))pointer(qp);
+        p->n_q_positions = int32_of(qp.numel());
+    }
+    p->E = int32_of(a[10]);
+    const int causal = PyObject_IsTrue(a[11]);
+    need(causal >= 0);
+    p->flags = causal ? FDD_ATTN_CAUSAL_BLOCK : 0;
+    p->splits = int32_of(a[12]);
+}
+
+// logits, tokens, mask, top, temperature, logprobs, entropy, top_ids, top_logprobs, device
+void fill_logprobs(fdd_logprob_params* p, PyObject* const* a)
+{
+    const OnDevice on{int32_of(a[9])};
+    const at::Tensor &x = on(a[0]);
+    need(x.dim() == 3);
+    const int64_t N = x.size(0), B = x.size(1);
+    p->N = int32_of(N); p->B = int32_of(B); p->V = x.size(2);
+    p->dtype = (decltype(p->dtype))dtype_code(x);
+    p->top = int32_of(a[3]);
+    need(p->top >= 0 && p->top <= FDD_LOGPROBS_MAX_TOP);
+    p->temperature = float_of(a[4]);
+    auto per_position = [&](PyObject* o, at::ScalarType type, bool top) {
+        const at::Tensor& t = on(o);
+        need(t.scalar_type() == type && t.dim() == (top ? 3 : 2) && t.size(0) == N && t.size(1) == B && (!top || t.size(2) == p->top));
+        return pointer(t);
+    };
+    p->logits = pointer(x);
+    p->tokens = (decltype(p->tokens))per_position(a[1], at::kInt, false);
+    if (a[2] != Py_None) p->row_mask = (decltype(p->row_mask))per_position(a[2], at::kByte, false);
+    p->logprobs = (float*)per_position(a[5], at::kFloat, false);
+    p->entropy = (float*)per_position(a[6], at::kFloat, false);
+    void* const ids = per_position(a[7], at::kInt, true);
+    void* const top = per_position(a[8], at::kFloat, true);
+    if (p->top > 0) {
+        p->top_ids = (decltype(p->top_ids))ids;
+        p->top_logprobs = (float*)top;
+    }
+}
+
 // address of a zeroed struct, then the arguments
 template <typename P, int ARGS, void (*FILL)(P*, PyObject* const*)>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n)
@@ -196,6 +318,9 @@ PyMethodDef methods[] = {
     {"fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&fork)), METH_FASTCALL, "arguments of fdd_fork_block"},
     {"attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<fdd_attn_params, 15, fill_attn>)), METH_FASTCALL, "fill an fdd_attn_params"},
     {"unmask", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<fdd_unmask_params, 9, fill_unmask>)), METH_FASTCALL, "fill an fdd_unmask_params"},
+    {"quant", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<QuantCall, 5, fill_quant>)), METH_FASTCALL, "fill an fdd_quant_cache and the fdd_quant_rows behind it"},
+    {"attn_quant", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<AttnQuantCall, 15, fill_attn_quant>)), METH_FASTCALL, "fill an fdd_attn_params and the fdd_quant_cache behind it"},
+    {"logprobs", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<fdd_logprob_params, 10, fill_logprobs>)), METH_FASTCALL, "fill an fdd_logprob_params"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -207,7 +332,10 @@ PyMODINIT_FUNC PyInit__marshal()
     PyObject* m = PyModule_Create(&module);
     if (m && (PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0 ||
               PyModule_AddIntConstant(m, "attn_bytes", sizeof(fdd_attn_params)) < 0 ||
-              PyModule_AddIntConstant(m, "unmask_bytes", sizeof(fdd_unmask_params)) < 0)) {
+              PyModule_AddIntConstant(m, "unmask_bytes", sizeof(fdd_unmask_params)) < 0 ||
+              PyModule_AddIntConstant(m, "quant_bytes", sizeof(QuantCall)) < 0 ||
+              PyModule_AddIntConstant(m, "attn_quant_bytes", sizeof(AttnQuantCall)) < 0 ||
+              PyModule_AddIntConstant(m, "logprobs_bytes", sizeof(fdd_logprob_params)) < 0)) {
         Py_DECREF(m);
         return nullptr;
     }
