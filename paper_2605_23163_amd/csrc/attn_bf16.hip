@@ -559,8 +559,6 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                 q_k0 = qks[t0];
                 q_v0 = qvs[t0];
                 q_k1 = qks[min(t0 + 1, a.TP - 1)];
-                q_scales(0);
-                q_scales(64);
                 if constexpr (Q::HALF) {
                     q_request(q_v, 0, 0, p_0);
                     if (!q_v) q_request(false, 1, 1, p_0);
@@ -572,6 +570,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                     for_slots(second, std::make_integer_sequence<int, Q::NP>());
                     for_slots(third, std::make_integer_sequence<int, Q::NP>());
                 }
+                q_scales(0);
+                if (F > 62) q_scales(64);      // (not counted in the waits below: they wait for one more load each then)
             }
         } else {
             fetch_k(0, 0);
@@ -833,7 +833,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
             const std::integral_constant<int, 2 * C::NI> first;
             const std::integral_constant<int, (NB - 2) * 2 * C::NI> rest;
             if constexpr (Q8) {
-                wait_vm<Q::HALF ? 0 : 2 * Q::NP>();      // Q, scales, K0
+                wait_vm<Q::HALF ? 0 : 2 * Q::NP + 2>();      // Q, K0
                 if (!q_v) q_convert(false, 0, 0, q_k0);
                 wg_barrier_written();
             } else {
@@ -842,7 +842,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
             }
             // Q8: V0 and K1, once the first AHEAD steps' codes have been requested
             auto q_first = [&] {
-                wait_vm<Q::AHEAD * Q::LOADS>();
+                wait_vm<Q::AHEAD * Q::LOADS + 2>();
                 if (!Q::HALF || q_v) q_convert(true, 0, 0, q_v0);
                 if (!Q::HALF || !q_v) q_convert(false, 1, 1, q_k1);
                 wg_barrier_written();

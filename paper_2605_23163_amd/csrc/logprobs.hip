@@ -456,33 +456,36 @@ __device__ __forceinline__ double wave_sum(double x)
 }
 
 // The pieces of a row joined, sums in their order; one workgroup per row.  Latency is all it takes: what is read is requested at
-// once, wavefront 0 works out the sums while the others look for the top entries among those of the pieces.
+// once, and the last wavefront works out the sums while the first ranks the top entries.
 template <typename T>
 __global__ __launch_bounds__(THREADS) void logprobs_join_kernel(Args a)
 {
-    constexpr int BATCH = 2 * THREADS;            // keys at a time
     const size_t row = wg_id_x();
     const int tid = thread_id_x(), lane = tid & 63, wave = tid >> 6;
     const Partial* const parts = a.parts + row * a.pieces;
     const uint64_t* const keys = a.keys + row * (size_t)a.pieces * a.top;
-    const long long all = (long long)a.pieces * a.top;
-    __shared__ __align__(16) uint64_t list[BATCH + 8];
-    __shared__ uint64_t best[MAX_TOP];
+    const int batch = a.top > 0 ? 2 * THREADS / a.top : 1, all = min(a.pieces, batch) * a.top;     // pieces at a time, keys of the first ones
+    __shared__ __align__(16) uint64_t list[2 * THREADS + MAX_TOP + 8];
+    __shared__ uint64_t best[MAX_TOP], bound;
+    __shared__ int listed;
     __shared__ RowSum sum;
     const uint8_t selected = a.mask ? a.mask[row] : 1;
     uint64_t mine[2] = {tid < all ? keys[tid] : 0, THREADS + tid < all ? keys[THREADS + tid] : 0};
+    const Partial none = {-INFINITY, 0.f, 0.f, 0.f};
+    Partial x = none;
+    if (wave == WAVES - 1 && lane < a.pieces) x = parts[lane];
     if (selected != 1) return;
 
-    if (wave == 0) {
-        float m = -INFINITY;
-        for (int p = lane; p < a.pieces; p += 64) m = fmaxf(m, parts[p].m);
+    auto sums = [&] {
+        float m = x.m;
+        for (int p = 64 + lane; p < a.pieces; p += 64) m = fmaxf(m, parts[p].m);
         m = wave_max(m);
         // the first piece that has the largest entry leaves it out
         int owner = 0x7fffffff;
         double s = 0.0, u = 0.0;
         for (int p0 = 0; p0 < a.pieces; p0 += 64) {
             const int p = p0 + lane;
-            const Partial x = p < a.pieces ? parts[p] : Partial{-INFINITY, 0.f, 0.f, 0.f};
+            if (p0 > 0) x = p < a.pieces ? parts[p] : none;
             const uint64_t has = __builtin_amdgcn_ballot_w64(x.m == m);
             if (owner == 0x7fffffff && has) owner = p0 + __builtin_ctzll(has);
             if (x.m != -INFINITY) {
@@ -496,36 +499,51 @@ __global__ __launch_bounds__(THREADS) void logprobs_join_kernel(Args a)
             sum = r;
             write_row<T>(a, row, r);
         }
-    }
-    // the keys, batch by batch; from the second on the best ones so far are among them
+    };
+    // The keys of as many pieces at a time as there is room for, with the best ones of the pieces before.  With n pieces and
+    // t = ceil(top / n), the smallest of their t-th keys is one that n t >= top keys reach: only those from it on are ranked.
     if (tid < MAX_TOP) best[tid] = 0;
-    int carried = 0;
-    for (long long k0 = 0; k0 < all;) {
-        const int n = (int)min((long long)(BATCH - carried), all - k0);
+    for (int p0 = 0; p0 < a.pieces && a.top > 0; p0 += batch) {
+        const int n = min(batch, a.pieces - p0), t = (a.top + n - 1) / n;
+        if (tid == 0) {
+            bound = ~0ull;
+            listed = 0;
+        }
+        __syncthreads();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int i = h * THREADS + tid;
-            if (k0 > 0) mine[h] = i < carried ? best[i] : i - carried < n ? keys[k0 + i - carried] : 0;
-            list[i] = mine[h];
+            if (p0 > 0) mine[h] = i < n * a.top ? keys[(size_t)p0 * a.top + i] : 0;
+            if (i < n * a.top && i % a.top == t - 1) atomicMin(&bound, mine[h]);
         }
-        if (tid < 8) list[BATCH + tid] = 0;
         __syncthreads();
-        int place[2] = {0, 0};
-        for (int j = 0; j < carried + n; j += 8)
+        auto offer = [&](uint64_t k) {
+            const uint64_t taken = __builtin_amdgcn_ballot_w64(k != 0 && k >= bound);
+            if (taken == 0) return;
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&listed, (int)__builtin_popcountll(taken));
+            at = __builtin_amdgcn_readfirstlane(at) + (int)__builtin_popcountll(taken & ((1ull << lane) - 1));
+            if (taken >> lane & 1) list[at] = k;
+        };
+        offer(mine[0]);
+        offer(mine[1]);
+        if (wave == 0) offer(lane < MAX_TOP ? best[lane] : 0);
+        __syncthreads();
+        const int m = listed;
+        if (tid < 8) list[m + tid] = 0;
+        __syncthreads();
+        if (wave == WAVES - 1 && p0 + batch >= a.pieces) sums();      // (beside the ranks, which wavefront 0 mostly works out alone)
+        for (int i = tid; i < m; i += THREADS) {
+            const uint64_t k = list[i];
+            int place = 0;
+            for (int j = 0; j < m; j += 8)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint64_t o = list[j + e];
-                place[0] += o > mine[0] ? 1 : 0;
-                place[1] += o > mine[1] ? 1 : 0;
-            }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (mine[h] != 0 && place[h] < a.top) best[place[h]] = mine[h];
-        carried = a.top;
-        k0 += n;
+                for (int e = 0; e < 8; ++e) place += list[j + e] > k ? 1 : 0;
+            if (place < a.top) best[place] = k;
+        }
         __syncthreads();
     }
-    if (a.top == 0) return;
+    if (wave == WAVES - 1 && a.top == 0) sums();
     if (tid < a.top) write_top(a, row, tid, best[tid], sum);
 }
 
