@@ -240,8 +240,10 @@ def _stream_ptr(stream):
 
 
 def _device_and_stream(stream):
-    """The current device's index, and the handle of the call's stream."""
-    dev = torch.cuda.current_device() if torch.cuda.is_initialized() else -1
+    """The current device's index (-1 where the GPU has not been used), and the handle of the call's stream."""
+    # (without the checks around it 0.1 us instead of 0.6, where this torch has that)
+    get = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    dev = get() if torch.cuda.is_initialized() else -1
     if stream is not None:
         return dev, stream.cuda_stream
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)

@@ -306,6 +306,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
         asm volatile("" ::"s"(h0), "s"(h1), "s"(h2), "s"(h3), "s"(h4), "s"(h5), "s"(h6), "s"(h7), "s"(h8), "s"(h9), "s"(h10),
                      "s"(h11), "s"(h12), "s"(h13), "s"(h14), "s"(h15), "s"(d0), "s"(d1), "s"(d2), "s"(d3), "s"(d4), "s"(d5),
                      "s"(d6), "s"(d7), "s"(d8), "s"(d9), "s"(p0), "s"(p1), "s"(p2));
+        if constexpr (Q8) asm volatile("" ::"s"(a.ks), "s"(a.vs), "s"(a.s_bs), "s"(a.head_bytes), "s"(a.head_scales));
         // the fields of the Q load, and a first touch of every other 64-byte line of the block (what is read
         // from those later then comes from the scalar cache)
         const uint16_t* q0 = a.q;
