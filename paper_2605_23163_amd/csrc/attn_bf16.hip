@@ -207,6 +207,14 @@ __device__ __forceinline__ void wait_vm()
     __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
+// The same before this wavefront reads what it had moved into LDS itself: no read is moved ahead of the wait.
+template <int N>
+__device__ __forceinline__ void wait_own()
+{
+    wait_vm<N>();
+    asm volatile("" ::: "memory");
+}
+
 // Workgroup barrier that orders LDS traffic only.  (__syncthreads() also
 // fences global memory, which makes the compiler drain every tile still on
 // its way into the ring.)  No memory access is moved across it.
@@ -834,7 +842,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
             const std::integral_constant<int, 2 * C::NI> first;
             const std::integral_constant<int, (NB - 2) * 2 * C::NI> rest;
             if constexpr (Q8) {
-                wait_vm<Q::HALF ? 0 : 2 * Q::NP + 2>();      // Q, K0
+                wait_own<Q::HALF ? 0 : 2 * Q::NP + 2>();     // Q, K0
                 if (!q_v) q_convert(false, 0, 0, q_k0);
                 wg_barrier_written();
             } else {
@@ -843,7 +851,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
             }
             // Q8: V0 and K1, once the first AHEAD steps' codes have been requested
             auto q_first = [&] {
-                wait_vm<Q::AHEAD * Q::LOADS + 2>();
+                wait_own<Q::AHEAD * Q::LOADS + 2>();
                 if (!Q::HALF || q_v) q_convert(true, 0, 0, q_v0);
                 if (!Q::HALF || !q_v) q_convert(false, 1, 1, q_k1);
                 wg_barrier_written();
@@ -863,7 +871,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                     q_first();
                     for (int i = 0; i < F; ++i) {
                         if ((i & 63) == 0 && i > 0) q_scales(i + 64);
-                        wait_vm<(Q::AHEAD - 1) * Q::LOADS>();
+                        wait_own<(Q::AHEAD - 1) * Q::LOADS>();
                         if (!Q::HALF || !q_v) q_convert(false, (i + 2) & 3, i & 1, q_scale(false, i));
                         if (!Q::HALF || q_v) q_convert(true, (i + 1) & 3, (i + 1) & 1, q_scale(true, i));
                         q_request_step(i + 1 + Q::AHEAD);
@@ -993,7 +1001,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                         const std::integral_constant<int, e / 4 % Q::NP> piece;
                         const bool v = Q::HALF ? q_v : e / 4 / Q::NP == 1;
                         if constexpr (e % 4 == 0) {
-                            if constexpr (e == 0) wait_vm<(Q::AHEAD - 1) * Q::LOADS>();
+                            if constexpr (e == 0) wait_own<(Q::AHEAD - 1) * Q::LOADS>();
                             codes = q_read(v, v ? (P + 1) % 4 : (P + 2) % 4, piece);
                             if constexpr (e % (4 * Q::NP) == 0) code_scale = q_scale(v, i);
                         } else if constexpr (e % 4 < 3) {

@@ -237,6 +237,27 @@ def test_scales_of_blocks_differ(F, oracle, spread):
     check(F, oracle, {k: W.to_storage(v, W.BF16) for k, v in f.items()}, W.BF16)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("N,splits", [(1, 1), (1, 2), (4, 1), (4, 3)])
+def test_long_runs_of_tiles(F, oracle, D, N, splits):
+    """One workgroup walks 203 tiles (more than the ring of scales holds), 102 or 68, every tile with scales of its own; M-tiles of 128
+    rows (N = 1) and of 256."""
+    print_case(test="quant_attn_long", D=D, N=N, splits=splits)
+    rng = np.random.default_rng([D, N, splits])
+    B, L, Hq, Hkv = 32, 64 * 202 + 17, 24, 4
+    d = rand_attn(rng, N, B, L, Hq, Hkv, D, W.BF16)
+    f = {k: W.widen(d[k], W.BF16) for k in ("prefix_k", "prefix_v")}
+    f["prefix_k"] *= np.exp2(rng.integers(-2, 2, size=(203, Hkv))).repeat(64, 0)[:L, :, None]
+    f["prefix_v"] *= np.exp2(rng.integers(-3, 4, size=(203, Hkv))).repeat(64, 0)[:L, :, None]
+    d.update({k: W.to_storage(v, W.BF16) for k, v in f.items()})
+    p, d = cached(F, d, W.BF16)
+    dev = {k: to_dev(v) for k, v in d.items()}
+    out = to_f64(F.fdd_block_attn_quant(dev["q"], p, L, dev["block_k"], dev["block_v"], splits=splits))
+    rows = np.stack([rng.integers(0, n, 48) for n in (N, B, Hq)], axis=1)
+    ref = oracle.block_attn(d["q"], d["prefix_k"], d["prefix_v"], d["block_k"], d["block_v"], rows=rows)
+    assert row_error(out[tuple(rows.T)], ref) <= ROW_TOL
+
+
 def test_rows_behind_the_prefix_are_not_used(F):
     """A cache holds more rows than the call says, NaN among them: the result is that of a cache that ends there."""
     print_case(test="quant_attn_behind")
