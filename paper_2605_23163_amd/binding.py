@@ -559,9 +559,10 @@ def _set_q_positions(p, q_positions):
 
 def fdd_block_attn_quant_workspace(q, prefix, L, block_k, block_v, splits=0, ext_k=None, ext_v=None, E=0, n_q_positions=0) -> int:
     """Workspace bytes of the fdd_block_attn_quant call with these arguments."""
+    lib = load_library()
     p, _ = _quant_attn_params(q, prefix, L, block_k, block_v, None, None, None, splits, False, ext_k, ext_v, E)
     p.n_q_positions = int(n_q_positions)
-    return load_library().fdd_block_attn_quant_workspace(C.byref(p))
+    return lib.fdd_block_attn_quant_workspace(C.byref(p))
 
 
 def fdd_block_attn_quant(q, prefix, L, block_k, block_v, scaffold_mask=None, out=None, scale=None, workspace=None, stream=None,
@@ -603,8 +604,9 @@ def _batched_quant_params(q, prefix, L, block_k, block_v, out, scale, splits, ca
 
 
 def fdd_block_attn_quant_batched_workspace(q, prefix, L, block_k, block_v, splits=0, ext_k=None, ext_v=None, E=0) -> int:
+    lib = load_library()
     p, _ = _batched_quant_params(q, prefix, L, block_k, block_v, None, None, splits, False, ext_k, ext_v, E)
-    return load_library().fdd_block_attn_quant_workspace(C.byref(p))
+    return lib.fdd_block_attn_quant_workspace(C.byref(p))
 
 
 def fdd_block_attn_quant_batched(q, prefix, L, block_k, block_v, out=None, scale=None, workspace=None, stream=None, splits=0,
@@ -631,8 +633,9 @@ def _logprob_params(logits, top, temperature):
 
 
 def fdd_token_logprobs_workspace(logits, top=0) -> int:
+    lib = load_library()
     p = _logprob_params(logits, top, 1.0)
-    return load_library().fdd_token_logprobs_workspace(C.byref(p))
+    return lib.fdd_token_logprobs_workspace(C.byref(p))
 
 
 def _logprob_arguments(logits, tokens, mask, top, temperature, logprobs, entropy, top_ids, top_logprobs, stream):

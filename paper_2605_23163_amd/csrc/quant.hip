@@ -8,11 +8,13 @@
 // value has four significant bits, so it is a bf16 number (2^-9 * 2^-117 is the smallest bf16 normal one), codes can
 // move to a larger scale, and attention multiplies the values that are read back here.
 //
-// Both kernels are bound by the bytes that they move; a thread takes 16 elements at a time (16 bytes of codes).
+// Both kernels are bound by the bytes that they move.  A thread takes as many elements at a time as 16 bytes of the rows hold (8
+// bf16, 4 fp32), so that neighbouring lanes load or store neighbouring pieces.
 //   quantize    one workgroup per (block of 64 rows, KV head, K or V): it holds the block in registers between the
 //               maximum and the rounding, so a row is read once.
-//   dequantize  one thread per 16 elements in the order of the destination.
+//   dequantize  threads in the order of the destination.
 #include <cmath>
+#include <type_traits>
 
 #include "fdd_internal.h"
 #include "wave.h"
@@ -25,7 +27,6 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int QB = FDD_QUANT_BLOCK;
 constexpr int THREADS = 256;
-constexpr int CHUNK = 16;       // elements a thread takes at a time
 
 // one of K and V
 struct Side {
@@ -47,34 +48,57 @@ struct DequantArgs {
     long long code_bs, scale_bs, rows_bs;    // batch: elements from one problem to the next
 };
 
-__device__ __forceinline__ void load16(const uint16_t* p, float (&x)[CHUNK])
+// 16 bytes of rows as fp32 and back
+__device__ __forceinline__ void widen(const u32x4& w, float (&x)[8])
 {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const u32x4 w = reinterpret_cast<const u32x4*>(p)[i];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-            x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        }
+    for (int j = 0; j < 4; ++j) {
+        x[2 * j] = __uint_as_float(w[j] << 16);
+        x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
     }
 }
-
-__device__ __forceinline__ void load16(const float* p, float (&x)[CHUNK])
+__device__ __forceinline__ void widen(const u32x4& w, float (&x)[4])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const u32x4 w = reinterpret_cast<const u32x4*>(p)[i];
+    for (int j = 0; j < 4; ++j) x[j] = __uint_as_float(w[j]);
+}
+__device__ __forceinline__ u32x4 narrow(const float (&x)[8])
+{
+    u32x4 w;
+    // (four significant bits: the upper half of the word is the value)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[4 * i + j] = __uint_as_float(w[j]);
-    }
+    for (int j = 0; j < 4; ++j) w[j] = (__float_as_uint(x[2 * j]) >> 16) | (__float_as_uint(x[2 * j + 1]) & 0xffff0000u);
+    return w;
+}
+__device__ __forceinline__ u32x4 narrow(const float (&x)[4])
+{
+    return u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
 }
 
-__device__ __forceinline__ void decode16(const u32x4& codes, float scale, float (&x)[CHUNK])
+// the codes that belong to them
+template <int VEC>
+struct Codes {
+    uint32_t w[VEC / 4];
+};
+template <int VEC>
+__device__ __forceinline__ Codes<VEC> load_codes(const uint8_t* p)
+{
+    Codes<VEC> c;
+    __builtin_memcpy(&c, __builtin_assume_aligned(p, VEC), VEC);
+    return c;
+}
+template <int VEC>
+__device__ __forceinline__ void store_codes(uint8_t* p, const Codes<VEC>& c)
+{
+    __builtin_memcpy(__builtin_assume_aligned(p, VEC), &c, VEC);
+}
+
+template <int VEC>
+__device__ __forceinline__ void decode(const Codes<VEC>& c, float scale, float (&x)[VEC])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[i], true);
+    for (int i = 0; i < VEC / 4; ++i) {
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.w[i], true);
         x[4 * i] = lo[0] * scale;
         x[4 * i + 1] = lo[1] * scale;
         x[4 * i + 2] = hi[0] * scale;
@@ -82,52 +106,31 @@ __device__ __forceinline__ void decode16(const u32x4& codes, float scale, float 
     }
 }
 
-__device__ __forceinline__ u32x4 encode16(const float (&x)[CHUNK], float inv)
+template <int VEC>
+__device__ __forceinline__ Codes<VEC> encode(const float (&x)[VEC], float inv)
 {
-    float y[CHUNK];
+    float y[VEC];
 #pragma unroll
-    for (int i = 0; i < CHUNK; ++i) {
+    for (int i = 0; i < VEC; ++i) {
         const float t = x[i] * inv;
         y[i] = t != t ? t : fminf(fmaxf(t, -448.f), 448.f);     // (the conversion makes NaN of what is too large)
     }
-    u32x4 c;
+    Codes<VEC> c;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i], y[4 * i + 1], 0, false);
-        c[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], w, true);
+    for (int i = 0; i < VEC / 4; ++i) {
+        const int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i], y[4 * i + 1], 0, false);
+        c.w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], w, true);
     }
     return c;
 }
 
-__device__ __forceinline__ void store16(uint16_t* p, const float (&x)[CHUNK])
-{
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        u32x4 w;
-        // (four significant bits: the upper half of the word is the value)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = (__float_as_uint(x[8 * i + 2 * j]) >> 16) | (__float_as_uint(x[8 * i + 2 * j + 1]) & 0xffff0000u);
-        reinterpret_cast<u32x4*>(p)[i] = w;
-    }
-}
-
-__device__ __forceinline__ void store16(float* p, const float (&x)[CHUNK])
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        u32x4 w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(x[4 * i + j]);
-        reinterpret_cast<u32x4*>(p)[i] = w;
-    }
-}
-
 // grid (blocks of the cache that the rows touch, Hkv, K and V)
 template <int D, typename T>
-__global__ __launch_bounds__(THREADS) void quantize_kernel(QuantArgs a)
+__global__ __launch_bounds__(THREADS, 6) void quantize_kernel(QuantArgs a)
 {
-    constexpr int CPR = D / CHUNK;                    // chunks of a row
-    constexpr int NC = QB * CPR / THREADS;            // chunks of a thread
+    constexpr int VEC = 16 / sizeof(T);
+    constexpr int CPR = D / VEC;                      // pieces of a row
+    constexpr int ROWS = THREADS / CPR, NC = QB / ROWS;   // rows a step; steps: pieces of a thread
     const Side& s = a.side[blockIdx.z];
     const int h = blockIdx.y, tid = threadIdx.x, block = a.row0 / QB + (int)blockIdx.x;
     const int lead = max(a.row0 - block * QB, 0);     // rows of the block that are there already
@@ -135,21 +138,25 @@ __global__ __launch_bounds__(THREADS) void quantize_kernel(QuantArgs a)
     uint8_t* const codes = s.codes + ((size_t)h * a.capacity + (size_t)block * QB) * D;
     float* const scale_at = s.scale + (size_t)h * (a.capacity / QB) + block;
 
-    float x[NC][CHUNK];
-    uint32_t top = 0;
     const float old = lead > 0 ? *scale_at : 0.f;
+    const int r0 = tid / CPR, col = tid % CPR;
+    const T* const src = static_cast<const T*>(s.rows) + ((long long)block * QB - a.row0 + r0) * s.row_stride + h * D + col * VEC;   // (used from row `lead` on)
+    u32x4 raw[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int i = tid + c * THREADS, r = i / CPR, col = i % CPR;
-        if (r < lead) {
-            decode16(*reinterpret_cast<const u32x4*>(codes + (size_t)i * CHUNK), old, x[c]);
-        } else if (r < end) {
-            load16(static_cast<const T*>(s.rows) + (size_t)(block * (long long)QB + r - a.row0) * s.row_stride + h * D + col * CHUNK, x[c]);
+        const int r = r0 + c * ROWS;
+        raw[c] = u32x4{0u, 0u, 0u, 0u};
+        if (r >= lead && r < end) raw[c] = *reinterpret_cast<const u32x4*>(src + c * ROWS * s.row_stride);
+    }
+    uint32_t top = 0;
 #pragma unroll
-            for (int j = 0; j < CHUNK; ++j) {
-                const uint32_t b = __float_as_uint(x[c][j]) & 0x7fffffffu;
-                top = max(top, b < 0x7f800000u ? b : 0u);
-            }
+    for (int c = 0; c < NC; ++c) {
+        float x[VEC];
+        widen(raw[c], x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const uint32_t b = __float_as_uint(x[j]) & 0x7fffffffu;
+            top = max(top, b < 0x7f800000u ? b : 0u);
         }
     }
     __shared__ uint32_t part[THREADS / 64];
@@ -162,29 +169,55 @@ __global__ __launch_bounds__(THREADS) void quantize_kernel(QuantArgs a)
     const float scale = fmaxf(__uint_as_float((uint32_t)(e + 127) << 23), old), inv = 1.f / scale;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-        const int i = tid + c * THREADS, r = i / CPR;
-        if (r < end && (r >= lead || scale != old)) *reinterpret_cast<u32x4*>(codes + (size_t)i * CHUNK) = encode16(x[c], inv);
+        const int r = r0 + c * ROWS;
+        float x[VEC];
+        widen(raw[c], x);
+        if (r >= lead && r < end) store_codes<VEC>(codes + (size_t)(tid + c * THREADS) * VEC, encode<VEC>(x, inv));
+    }
+    if (lead > 0 && scale != old) {
+#pragma unroll 1
+        for (int r = r0; r < lead; r += ROWS) {
+            uint8_t* const at = codes + r * D + col * VEC;
+            float x[VEC];
+            decode<VEC>(load_codes<VEC>(at), old, x);
+            store_codes<VEC>(at, encode<VEC>(x, inv));
+        }
     }
     if (tid == 0) *scale_at = scale;
 }
 
-// grid (chunks / THREADS, K and V, problems)
-template <int D, typename T>
+// grid (pieces / (THREADS U), K and V, problems); U: pieces of a thread, all requested before the first is stored
+template <int D, typename T, int U>
 __global__ __launch_bounds__(THREADS) void dequantize_kernel(DequantArgs a)
 {
-    constexpr int CPR = D / CHUNK;
+    constexpr int VEC = 16 / sizeof(T), CPR = D / VEC;
     const Side& s = a.side[blockIdx.y];
-    const size_t i = (size_t)blockIdx.x * THREADS + threadIdx.x;      // chunk of the destination: (row, head, column)
-    if (i >= (size_t)a.rows * a.Hkv * CPR) return;
-    const int rh = (int)(i / CPR), col = (int)(i % CPR);
-    const int r = fast_div(rh, a.dHkv), h = rh - r * a.Hkv;
-    const size_t row = (size_t)a.row0 + r;
     const uint8_t* const codes = s.codes + blockIdx.z * a.code_bs;
     const float* const scales = s.scale + blockIdx.z * a.scale_bs;
-    float x[CHUNK];
-    decode16(*reinterpret_cast<const u32x4*>(codes + ((size_t)h * a.capacity + row) * D + col * CHUNK),
-             scales[(size_t)h * (a.capacity / QB) + row / QB], x);
-    store16(static_cast<T*>(s.rows) + blockIdx.z * a.rows_bs + (size_t)r * s.row_stride + h * D + col * CHUNK, x);
+    T* const out = static_cast<T*>(s.rows) + blockIdx.z * a.rows_bs;
+    const size_t i0 = (size_t)blockIdx.x * (THREADS * U) + threadIdx.x, all = (size_t)a.rows * a.Hkv * CPR;
+    Codes<VEC> c[U];
+    float scale[U];
+    size_t to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const size_t i = i0 + u * THREADS;             // piece of the destination: (row, head, column)
+        to[u] = ~(size_t)0;
+        if (i >= all) continue;
+        const int rh = (int)(i / CPR), col = (int)(i % CPR);
+        const int r = fast_div(rh, a.dHkv), h = rh - r * a.Hkv;
+        const size_t row = (size_t)a.row0 + r;
+        c[u] = load_codes<VEC>(codes + ((size_t)h * a.capacity + row) * D + col * VEC);
+        scale[u] = scales[(size_t)h * (a.capacity / QB) + row / QB];
+        to[u] = (size_t)r * s.row_stride + h * D + col * VEC;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (to[u] == ~(size_t)0) continue;
+        float x[VEC];
+        decode<VEC>(c[u], scale[u], x);
+        *reinterpret_cast<u32x4*>(out + to[u]) = narrow(x);
+    }
 }
 
 long long row_stride(const fdd_quant_cache& c, long long stride) { return stride ? stride : (long long)c.Hkv * c.D; }
@@ -225,14 +258,25 @@ hipError_t launch_dequantize(const fdd_quant_cache& c, int row0, const fdd_quant
     a.code_bs = c.batch_stride;
     a.scale_bs = c.scale_batch_stride;
     a.rows_bs = batch_stride;
-    const long long chunks = (long long)dst.rows * c.Hkv * (c.D / CHUNK);
-    const dim3 grid((unsigned)((chunks + THREADS - 1) / THREADS), 2, (unsigned)batch);
+    const long long pieces = (long long)dst.rows * c.Hkv * (c.D / (dst.dtype == FDD_BF16 ? 8 : 4));
+    // four pieces a thread where they are enough for every compute unit all the same
+    const bool many = pieces * batch >= 4ll * kNumCU * 4 * THREADS;
+    const long long per = THREADS * (many ? 4 : 1);
+    const dim3 grid((unsigned)((pieces + per - 1) / per), 2, (unsigned)batch);
+    auto go = [&](auto d, auto t) {
+        constexpr int D = decltype(d)::value;
+        typedef decltype(t) T;
+        if (many) hipLaunchKernelGGL((dequantize_kernel<D, T, 4>), grid, dim3(THREADS), 0, s, a);
+        else hipLaunchKernelGGL((dequantize_kernel<D, T, 1>), grid, dim3(THREADS), 0, s, a);
+    };
+    const std::integral_constant<int, 64> d64;
+    const std::integral_constant<int, 128> d128;
     if (dst.dtype == FDD_BF16) {
-        if (c.D == 128) hipLaunchKernelGGL((dequantize_kernel<128, uint16_t>), grid, dim3(THREADS), 0, s, a);
-        else hipLaunchKernelGGL((dequantize_kernel<64, uint16_t>), grid, dim3(THREADS), 0, s, a);
+        if (c.D == 128) go(d128, uint16_t());
+        else go(d64, uint16_t());
     } else {
-        if (c.D == 128) hipLaunchKernelGGL((dequantize_kernel<128, float>), grid, dim3(THREADS), 0, s, a);
-        else hipLaunchKernelGGL((dequantize_kernel<64, float>), grid, dim3(THREADS), 0, s, a);
+        if (c.D == 128) go(d128, float());
+        else go(d64, float());
     }
     return hipGetLastError();
 }

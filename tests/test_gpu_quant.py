@@ -258,6 +258,31 @@ def test_long_runs_of_tiles(F, oracle, D, N, splits):
     assert row_error(out[tuple(rows.T)], ref) <= ROW_TOL
 
 
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_random_shapes(F, oracle, seed):
+    """Shapes that the cases above do not list, every form of the call among them."""
+    rng = np.random.default_rng([seed, 77])
+    for case in range(24):
+        dtype = W.BF16 if case % 4 else W.F32
+        D, Hkv, G = int(rng.choice([64, 128])), int(rng.choice([1, 2, 4, 8])), int(rng.choice([1, 2, 3, 7]))
+        N, B = int(rng.integers(1, 20)), int(rng.choice([1, 2, 5, 16, 31, 32, 33, 40, 64, 65, 100]))
+        L = int(rng.choice([0, 1, 63, 64, 65, 127, 128, 200, 777, 1024, 1500, 4096, 5000]))
+        E = int(rng.choice([0, 0, 1, 7, 64, 90]))
+        if N * B * Hkv * G * (L + E + B) * D > (2e8 if dtype == W.F32 else 2e9):
+            N, L = max(1, N // 5), min(L, 1500)
+        kw = dict(causal=bool(rng.integers(0, 2)), splits=int(rng.choice([0, 0, 0, 1, 2, 3, 5, 9])), extra=int(rng.choice([0, 0, 130])))
+        if E:
+            cap = E + int(rng.integers(0, 5))
+            kw.update(E=E, ext=[W.to_storage(rng.standard_normal((N, cap, Hkv, D)), dtype) for _ in range(2)])
+        if rng.integers(0, 3) == 0:
+            keep = rng.random(N * B) < rng.choice([0.1, 0.5, 0.9])
+            keep[rng.integers(N * B)] = True
+            kw["positions"] = np.flatnonzero(keep).tolist()
+        print_case(test="quant_attn_sweep", seed=seed, case=case, dtype=dtype, N=N, B=B, L=L, Hq=Hkv * G, Hkv=Hkv, D=D, E=E, causal=kw["causal"],
+                   splits=kw["splits"], listed="positions" in kw)
+        check(F, oracle, rand_attn(rng, N, B, L, Hkv * G, Hkv, D, dtype), dtype, **kw)
+
+
 def test_rows_behind_the_prefix_are_not_used(F):
     """A cache holds more rows than the call says, NaN among them: the result is that of a cache that ends there."""
     print_case(test="quant_attn_behind")

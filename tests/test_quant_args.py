@@ -2,6 +2,8 @@
 status code or an exception and nothing is launched; and the reference in 64 bits against cases worked out by hand."""
 import ctypes as C
 import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -139,6 +141,39 @@ def test_binding_refuses(lib):
         bd.fdd_token_logprobs(logits, tok, top=2, top_ids=torch.zeros(1, 2, 3, dtype=torch.int32))
     with pytest.raises(ValueError, match="GPU memory"):
         bd.fdd_token_logprobs(logits, tok)
+
+
+FIRST_CALLS = {
+    "fdd_block_attn_quant_workspace": "F.fdd_block_attn_quant_workspace(q, p, 1, b, b)",
+    "fdd_block_attn_quant_batched_workspace": "F.fdd_block_attn_quant_batched_workspace(q[None], P, 1, b[None], b[None])",
+    "fdd_token_logprobs_workspace": "F.fdd_token_logprobs_workspace(b.float()[0])",
+    "fdd_block_attn_quant": "F.fdd_block_attn_quant(q, p, 1, b, b)",
+    "fdd_block_attn_quant_batched": "F.fdd_block_attn_quant_batched(q[None], P, 1, b[None], b[None])",
+    "fdd_prefix_quantize": "F.fdd_prefix_quantize(b[0], b[0], p)",
+    "fdd_prefix_dequantize": "F.fdd_prefix_dequantize(p, 4, k=b[0], v=b[0])",
+    "fdd_token_logprobs": "F.fdd_token_logprobs(b.float()[0], torch.zeros(4, 2, dtype=torch.int32))",
+    "fdd_quant_prefix": "F.fdd_quant_prefix(100, 2, 64, device='cpu')",
+}
+
+
+@pytest.mark.parametrize("name", sorted(FIRST_CALLS))
+def test_any_call_may_be_the_first(name):
+    """The library and torch are loaded by the first call, whichever it is; host tensors are refused as such."""
+    code = f"""
+import torch
+import paper_2605_23163_amd as F
+q, b = torch.zeros(1, 4, 4, 64, dtype=torch.bfloat16), torch.zeros(1, 4, 2, 64, dtype=torch.bfloat16)
+p = F.QuantPrefix(*(torch.zeros(2, 64, 64).to(torch.float8_e4m3fn) for _ in range(2)), *(torch.ones(2, 1) for _ in range(2)))
+P = F.QuantPrefix(*(t[None] for t in p))
+try:
+    {FIRST_CALLS[name]}
+    print("returned")
+except ValueError as e:
+    print("refused", "GPU memory" in str(e))
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    assert r.stdout.strip() in (("returned",) if name in ("fdd_quant_prefix", "fdd_token_logprobs_workspace") else ("refused True",)), r.stdout
 
 
 class Elsewhere:
