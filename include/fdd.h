@@ -212,7 +212,8 @@ typedef struct fdd_quant_rows {
  * prompt (row0 = 0), or a finished block behind the rows that are there (row0 = their number).  Where row0
  * lies inside a block of the cache, the block's scale may grow: the rows in front are then rounded again,
  * to the codes of the new scale (exact, except for codes that fall below 2^-6), else they are left as they
- * are.  It does not shrink.  Codes behind row0 + rows and scales of later blocks are left as they were.
+ * are.  It does not shrink.  (All rows of that block in front of row0 and its scale have to be there: a scale is a power of two from
+ * 2^-117 to 2^119, also in a cache that was filled by other means.)  Codes behind row0 + rows and scales of later blocks are left as they were.
  * Values: an infinity or a magnitude above 448 * 2^119 is stored as the largest code, a NaN as a NaN;
  * infinities and NaN have no part in the scale.  The source must not overlap the cache.
  *
@@ -225,9 +226,9 @@ fdd_status fdd_prefix_dequantize(const fdd_quant_cache *cache, int32_t row0, con
  * are ignored): the L keys and values of the prefix are rows [0, L) of `cache`, L <= cache->capacity,
  * converted without an error.  Queries, blocks, extensions and outputs are of type p->dtype.  The result is
  * that of fdd_block_attn on the rows as fdd_prefix_dequantize returns them, up to the order of sums.
- * `cache` may be NULL iff L == 0.  The workspace is fdd_block_attn_quant_workspace(p): more than that of
- * fdd_block_attn where the call converts the prefix once, for all of its workgroups, instead of tile by
- * tile.  Values and q_positions as with fdd_block_attn; a NaN in the cache is a NaN. */
+ * `cache` may be NULL iff L == 0.  The workspace is fdd_block_attn_quant_workspace(p): a bf16 call converts the
+ * prefix tile by tile on its way to the matrix pipe and needs no room for it; an fp32 call converts it first and
+ * needs room for its K and V in fp32.  Values and q_positions as with fdd_block_attn; a NaN in the cache is a NaN. */
 size_t fdd_block_attn_quant_workspace(const fdd_attn_params *p);
 fdd_status fdd_block_attn_quant(const fdd_attn_params *p, const fdd_quant_cache *cache);
 
@@ -391,7 +392,7 @@ typedef struct fdd_logprob_params {
     int64_t V;
     int32_t dtype;                 /* fdd_dtype of logits */
     int32_t top;                   /* 0 .. min(V, FDD_LOGPROBS_MAX_TOP) */
-    float temperature;             /* positive and finite */
+    float temperature;             /* positive and finite, and so is 1.5 / temperature */
     int32_t reserved;              /* must be 0 */
     const void *logits;            /* [N,B,V] */
     const int32_t *tokens;         /* [N,B]; may be NULL iff logprobs is */

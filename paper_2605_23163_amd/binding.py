@@ -527,7 +527,7 @@ def fdd_prefix_dequantize(prefix, rows, row0=0, dtype=None, k=None, v=None, stre
         cache = _quant_cache(prefix)
         if rows < 0 or not 0 <= row0 <= cache.capacity - rows:
             raise ValueError(f"rows [{row0}, {row0 + rows}) do not fit a cache of {cache.capacity}")
-        device = prefix.k.device
+        device = prefix[0].device
         new = torch.empty if stream is None else _maker(stream, device, torch.empty)
         k, v = (new((rows, cache.Hkv, cache.D), dtype=torch.bfloat16 if dtype is None else dtype, device=device) for _ in range(2))
     elif k.dim() != 3 or k.shape[0] != rows or (dtype is not None and k.dtype != dtype):

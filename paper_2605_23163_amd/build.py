@@ -26,7 +26,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + os.path.j
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
 # The bf16 attention and vocabulary kernels produce no NaN from finite inputs (masked
 # scores are -inf and every inf - inf is avoided by construction), so max/min need no NaN
-# quieting there; the kernels of log probabilities write the NaN of a row without entries as bits.  The fp32 attention kernel passes the caller's NaN and infinities on.
+# quieting there; the kernels of log probabilities write the NaN of a row
+# without entries as bits.  The fp32 attention kernel passes the caller's NaN and infinities on.
 EXTRA = {"attn_bf16.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
          "logprobs.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
          "unmask.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"]}

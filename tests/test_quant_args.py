@@ -104,6 +104,12 @@ def test_logprobs_are_checked(lib):
     assert lib.fdd_token_logprobs_workspace(C.byref(logp(V=0))) == 0
 
 
+def test_smallest_temperature(lib):
+    """1 / 4e-39 is an fp32 number, log2(e) / 4e-39 is none."""
+    assert lib.fdd_token_logprobs(C.byref(logp(temperature=4e-39))) == 4
+    assert "temperature" in lib.fdd_last_error().decode()
+
+
 def host_prefix(cap=128, Hkv=2, D=64, **kw):
     d = dict(k=torch.zeros(Hkv, cap, D).to(torch.float8_e4m3fn), v=torch.zeros(Hkv, cap, D).to(torch.float8_e4m3fn),
              k_scale=torch.ones(Hkv, cap // 64), v_scale=torch.ones(Hkv, cap // 64))
