@@ -1201,6 +1201,22 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                 // L=16384: 723 -> 696 us; N=8, L=4096: 28.9 -> 27.7; plain, non-temporal and both measured).
                 const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
                 const size_t pseg = (size_t)M * a.max_seg + __builtin_amdgcn_readfirstlane(seg);
+                // Q8: in fp16, times the power of two that brings the row's largest one to 2^14 .. 2^15: 11 bits instead of 8 in as many
+                // bytes, so that a call in several pieces is as exact as one in a single piece (error of a result in norm 2.9e-3 -> 2.3e-3
+                // at N=8, L=4096, time within 2 %; averages in fp32 took 5 to 10 % more).
+                typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+                float to_f16 = 0.f, from_f16 = 0.f;
+                if constexpr (Q8) {
+                    float top = 0.f;
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) top = fmaxf(top, __builtin_fabsf(o[db][v]));
+                    top = fmaxf(top, other_half(top)) * inv;
+                    const uint32_t e = max(__float_as_uint(top) >> 23 & 255u, 40u);      // (with l near 1 or more no factor overflows)
+                    to_f16 = inv * __uint_as_float((127 + 14 + 127 - e) << 23);
+                    from_f16 = __uint_as_float((e - 14) << 23);
+                }
                 const __amdgpu_buffer_rsrc_t o_rsrc = __builtin_amdgcn_make_buffer_rsrc(
                     static_cast<unsigned char*>(a.ws_o) + pseg * (size_t)(MROWS * D * 2), 0, MROWS * D * 2, RSRC_FLAGS);
                 const uint32_t o_off = (uint32_t)(wave * (2 * DB * 64) + lane) * 16;
@@ -1208,6 +1224,13 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                 for (int db = 0; db < DB; ++db)
 #pragma unroll
                     for (int v2 = 0; v2 < 2; ++v2) {
+                        if constexpr (Q8) {
+                            f16x8 w;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) w[j] = (_Float16)(o[db][v2 * 8 + j] * to_f16);
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w), o_rsrc, o_off + (db * 2 + v2) * 1024, 0, 16);
+                            continue;
+                        }
                         bf16x8 w;
 #pragma unroll
                         for (int j = 0; j < 8; ++j) w[j] = (__bf16)(o[db][v2 * 8 + j] * inv);
@@ -1215,9 +1238,10 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 1 : 2) void attn_bf16_kern
                     }
                 if (half == 0) {
                     const size_t prow = pseg * MROWS + (wave * 32 + l32);
-                    float* const ml = a.ws_ml + prow * 2;
+                    float* const ml = a.ws_ml + prow * (Q8 ? 4 : 2);
                     ml[0] = m_run;
                     ml[1] = l_tot;
+                    if constexpr (Q8) ml[2] = from_f16;
                 }
             }
         }
@@ -1317,9 +1341,11 @@ __device__ __forceinline__ float reduce_groups(float v, Op op)
     return __uint_as_float(x);
 }
 
-template <int D, int WAVES, int SG, int UX>
+// Q8: averages in fp16 times a factor, which is the third of four numbers beside m and l.
+template <int D, int WAVES, int SG, int UX, bool Q8>
 __global__ __launch_bounds__(256) void attn_merge_bf16_kernel(MergeArgs a)
 {
+    constexpr int ML = Q8 ? 4 : 2;
     constexpr int DB = D / 32;
     constexpr int CPW = 2 * DB * 64;          // 16-byte chunks per wavefront of the attention kernel
     constexpr int CH = WAVES * CPW;           // chunks per M-tile and segment
@@ -1343,7 +1369,7 @@ __global__ __launch_bounds__(256) void attn_merge_bf16_kernel(MergeArgs a)
     const int r = cidx & 31, half = (cidx >> 5) & 1, i2 = (cidx >> 6) % (2 * DB);
     const bool live = row0 + r < a.R;
     const u32x4* src = a.ws_o + (size_t)M * a.max_seg * CH + cidx;
-    const float* ml = a.ws_ml + ((size_t)M * a.max_seg * MROWS + wave * 32 + r) * 2;
+    const float* ml = a.ws_ml + ((size_t)M * a.max_seg * MROWS + wave * 32 + r) * ML;
 
     float m = -INFINITY, sum = 0.f;           // this thread's segments: largest m, sum of weights against it
     float acc[8];                             // and their weighted average
@@ -1351,11 +1377,21 @@ __global__ __launch_bounds__(256) void attn_merge_bf16_kernel(MergeArgs a)
     for (int j = 0; j < 8; ++j) acc[j] = 0.f;
     for (int s0 = 0; s0 < n_seg; s0 += SG * UX) {
         float2 y[UX];
+        float z[UX];
         u32x4 x[UX];
 #pragma unroll
         for (int u = 0; u < UX; ++u) {
             const int s = s0 + sg + u * SG;
             y[u] = make_float2(-INFINITY, 0.f);
+            if constexpr (Q8) {
+                // (no branch: what is missing is the last segment once more, without a weight; rows beyond the last are not stored)
+                const int t = min(s, n_seg - 1);
+                const float4 of = *reinterpret_cast<const float4*>(ml + (size_t)t * (ML * MROWS));
+                y[u] = make_float2(of.x, s < n_seg ? of.y : 0.f);
+                z[u] = of.z;
+                x[u] = src[(size_t)t * CH];
+                continue;
+            }
             x[u] = u32x4{0u, 0u, 0u, 0u};
             if (live && s < n_seg) {
                 y[u] = *reinterpret_cast<const float2*>(ml + (size_t)s * (2 * MROWS));
@@ -1388,6 +1424,13 @@ __global__ __launch_bounds__(256) void attn_merge_bf16_kernel(MergeArgs a)
 #pragma unroll
         for (int u = 0; u < UX; ++u) {
             const float w = y[u].y * inv;
+            if constexpr (Q8) {
+                typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+                const f16x8 of = __builtin_bit_cast(f16x8, x[u]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] = fmaf((float)of[j], w * z[u], acc[j]);
+                continue;
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 acc[2 * j] = fmaf(__uint_as_float(x[u][j] << 16), w, acc[2 * j]);
@@ -1546,7 +1589,7 @@ hipError_t launch_attn_quant(const fdd_attn_params& p, const fdd_quant_cache* ca
     return hipErrorInvalidValue;
 }
 
-hipError_t launch_attn_merge_bf16(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s)
+static hipError_t launch_merge(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s, bool quant)
 {
     MergeArgs a;
     a.ws_o = static_cast<const u32x4*>(p.workspace);
@@ -1570,8 +1613,13 @@ hipError_t launch_attn_merge_bf16(const fdd_attn_params& p, const AttnPlan& plan
     auto go = [&](auto d, auto sgc, auto ux) {
         constexpr int D = decltype(d)::value, SG = decltype(sgc)::value, UX = decltype(ux)::value;
         const dim3 grid((unsigned)(p.Hkv * batch * plan.MT), (unsigned)(plan.mtile_rows / 32 * 2 * (D / 32) * SG / 4));
-        if (plan.mtile_rows == 256) hipLaunchKernelGGL((attn_merge_bf16_kernel<D, 8, SG, UX>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((attn_merge_bf16_kernel<D, 4, SG, UX>), grid, dim3(256), 0, s, a);
+        auto kernel = [&](auto w) {
+            constexpr bool Q8 = decltype(w)::value;
+            if (plan.mtile_rows == 256) hipLaunchKernelGGL((attn_merge_bf16_kernel<D, 8, SG, UX, Q8>), grid, dim3(256), 0, s, a);
+            else hipLaunchKernelGGL((attn_merge_bf16_kernel<D, 4, SG, UX, Q8>), grid, dim3(256), 0, s, a);
+        };
+        if (quant) kernel(std::true_type());
+        else kernel(std::false_type());
     };
     auto sized = [&](auto d) {
         const std::integral_constant<int, 1> i1;
@@ -1588,6 +1636,9 @@ hipError_t launch_attn_merge_bf16(const fdd_attn_params& p, const AttnPlan& plan
     else sized(std::integral_constant<int, 64>());
     return hipGetLastError();
 }
+
+hipError_t launch_attn_merge_bf16(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s) { return launch_merge(p, plan, scale, s, false); }
+hipError_t launch_attn_merge_quant(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s) { return launch_merge(p, plan, scale, s, true); }
 
 hipError_t launch_prefix_pack(const void* prefix_v, int L, int Hkv, int D, void* packed, hipStream_t s)
 {

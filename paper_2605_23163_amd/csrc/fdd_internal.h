@@ -177,6 +177,7 @@ __host__ __device__ inline int unit_begin(int w, int base, int rem) { return w *
 hipError_t launch_attn_bf16(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s, hipEvent_t before_main);
 // the same with the prefix in a cache of 8 bits (nullptr: no prefix); p's own prefix is not used
 hipError_t launch_attn_quant(const fdd_attn_params& p, const fdd_quant_cache* cache, const AttnPlan& plan, float scale, hipStream_t s, hipEvent_t before_main);
+hipError_t launch_attn_merge_quant(const fdd_attn_params& p, const AttnPlan& plan, float scale, hipStream_t s);  // averages of launch_attn_quant
 hipError_t launch_prefix_pack(const void* prefix_v, int L, int Hkv, int D, void* packed, hipStream_t s);
 // K and V of the first `rows` rows of a cache of 8 bits, [batch][rows,Hkv,D] of type `dtype`, problems batch_stride elements apart
 hipError_t launch_dequantize(const fdd_quant_cache& c, int row0, const fdd_quant_rows& dst, int batch, long long batch_stride, hipStream_t s);

@@ -371,6 +371,7 @@ bool plan_by_tile(const fdd_attn_params& p, AttnPlan* plan)
     make_attn_plan(p, plan);
     plan->packed = false;
     plan->ws_vt_bytes = 0;
+    plan->ws_ml_bytes *= 2;       // (with a factor of the row's averages beside m and l)
     return true;
 }
 
@@ -439,7 +440,7 @@ fdd_status fdd_block_attn_quant(const fdd_attn_params* p, const fdd_quant_cache*
         attn_events(&start, &stop);
         hipError_t e = launch_attn_quant(*p, cache, plan, scale, stream, start);
         if (e == hipSuccess && stop) e = hipEventRecord(stop, stream);
-        if (e == hipSuccess && plan.ws_o_bytes > 0) e = launch_attn_merge_bf16(*p, plan, scale, stream);
+        if (e == hipSuccess && plan.ws_o_bytes > 0) e = launch_attn_merge_quant(*p, plan, scale, stream);
         if (e != hipSuccess) return fail(FDD_ERR_LAUNCH, "%s: launch failed: %s", kAttn, hipGetErrorString(e));
         return FDD_OK;
     }

@@ -258,6 +258,30 @@ def test_long_runs_of_tiles(F, oracle, D, N, splits):
     assert row_error(out[tuple(rows.T)], ref) <= ROW_TOL
 
 
+@pytest.mark.parametrize("spread", [0, 100, -80])
+@pytest.mark.parametrize("D,N", [(64, 1), (128, 1), (128, 12)])
+def test_segments_that_cancel(F, D, N, spread):
+    """Two pieces of the keys whose averages nearly cancel.  Scores are all 0, so that every probability is 1 and an output is the mean of
+    n values: fp32 sums n 2^-24 of the largest one; a piece's averages in 11 bits of the largest one, 2^-11 of it at most; the
+    output in bf16, 2^-8 of itself.  (Averages in bf16 would be off by 2^-9 of themselves and more.)"""
+    print_case(test="quant_attn_cancel", D=D, N=N, spread=spread)
+    rng = np.random.default_rng([D, N, spread + 100])
+    B, L, Hq, Hkv = 8, 512, 8, 2
+    d = rand_attn(rng, N, B, L, Hq, Hkv, D, W.BF16)
+    v = rng.uniform(1.0, 2.0, (L, Hkv, D))
+    v[L // 2:] *= -1.0
+    d["prefix_v"] = W.to_storage(np.ldexp(v, spread), W.BF16)
+    d["block_v"] = W.to_storage(np.ldexp(rng.uniform(-1.0, 1.0, (N, B, Hkv, D)), spread), W.BF16)
+    p, d = cached(F, d, W.BF16)
+    dev = {k: to_dev(x) for k, x in d.items()}
+    out = to_f64(F.fdd_block_attn_quant(torch.zeros_like(dev["q"]), p, L, dev["block_k"], dev["block_v"], splits=2))
+    pv, bv = (W.widen(d[k], W.BF16).astype(np.float64) for k in ("prefix_v", "block_v"))
+    ref = (pv.sum(0) + bv.sum(1, keepdims=True)) / (L + B)                 # [N,1,Hkv,D], one for all queries
+    ref = np.repeat(ref, Hq // Hkv, axis=2)
+    top = np.abs(pv).max()
+    assert (np.abs(out - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -11 + (L + B) * 2.0 ** -24) * top).all()
+
+
 @pytest.mark.parametrize("seed", [1, 2, 3])
 def test_random_shapes(F, oracle, seed):
     """Shapes that the cases above do not list, every form of the call among them."""
