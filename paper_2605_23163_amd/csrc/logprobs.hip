@@ -6,7 +6,9 @@
 //     ln p_v = y_v - ln(1 + S),   entropy = -sum p ln p = ln(1 + S) - U / (1 + S).
 // Both terms of the entropy are >= 0, and S without the largest term keeps its digits where the row is nearly certain.
 //
-// Bound by the bytes of the logits, which are read once, and close behind by the vector ALUs.  A row is cut into pieces, a
+// Bound by the bytes of the logits, which are read once, and close behind by the vector ALUs (13 instructions an entry, an exponential
+// among them).  N=16, B=64, V=152064 bf16, top 5 77 us (4.0 TB/s); N=8, B=32 25, half of the rows selected 18.7, top 0 14.9; N=1, B=32 11.7; one
+// piece (V=512) 5.1.  A row is cut into pieces, a
 // workgroup each; a thread requests its part together and takes its sums as the vectors come, against a number near its largest
 // entry, before it meets the others.  Entry a is left out in the end: the one thread that has it has its sums taken again, an
 // entry a lane.
@@ -29,7 +31,9 @@ namespace fdd {
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
-constexpr int NV = 8;                        // 16-byte vectors a thread holds at most
+// 16-byte vectors a thread holds at most, of 4, 6, 8, 12, 16: fastest with 8 at up to 256 rows of 152064; 12 and 16 are up to a
+// tenth faster at 1024 rows and slower at 32.
+constexpr int NV = 8;
 constexpr int MAX_TOP = FDD_LOGPROBS_MAX_TOP;
 constexpr int NEAR = 128;                    // vectors of a wavefront that may hold top entries
 constexpr int LIST = 1024;                   // candidates for the top entries of a piece
@@ -553,14 +557,16 @@ struct LogprobPlan {
 };
 
 // A row that a workgroup can hold is one piece: one launch.  Others are cut into equal pieces, as few as hold them, or
-// more where there are few rows: up to four workgroups a compute unit, of a quarter of what they can hold at least.
+// more where there are few rows: up to two workgroups a compute unit, of a quarter of what they can hold at least.  us with none
+// finer, one, two, four, eight workgroups a compute unit: N=1, B=32, V=152064, top 5 12.4, 12.4, 11.7, 13.0, 13.6; V=50001, top 20 10.9, 10.1,
+// 10.5, 10.5, 10.5; N=8, V=32768 12.5, 12.5, 12.4, 12.7, 13.9; pieces down to an eighth cost N=1, B=4 8 us (the join takes them in rounds).
 LogprobPlan make_logprob_plan(const fdd_logprob_params& p)
 {
     const long long vec = p.dtype == FDD_BF16 ? 8 : 4, rows = (long long)p.N * p.B;
     const long long vecs = std::max(p.V / vec, 1ll);            // (the entries in front of a row's first vector may take one from this)
     long long pieces = (vecs + NV * THREADS - 1) / (NV * THREADS);
     if (pieces > 1) {
-        const long long finer = std::min(4ll * kNumCU / rows, (vecs + 2 * THREADS - 1) / (2 * THREADS));
+        const long long finer = std::min(2ll * kNumCU / rows, (vecs + 2 * THREADS - 1) / (2 * THREADS));
         pieces = std::max(pieces, finer);
     }
     LogprobPlan l;
@@ -595,7 +601,7 @@ hipError_t launch_logprobs(const fdd_logprob_params& p, hipStream_t s)
     a.inv_t = 1.f / p.temperature;
     a.c = LOG2E * a.inv_t;
     const dim3 rows((unsigned)a.rows), units((unsigned)a.rows * (unsigned)plan.pieces), block(THREADS);
-    const bool bf16 = p.dtype == FDD_BF16, one = plan.pieces == 1, compact = a.mask && a.rows >= 16 && a.rows <= LIVE_ROWS;
+    const bool bf16 = p.dtype == FDD_BF16, one = plan.pieces == 1, compact = a.mask && a.rows >= 16 && a.rows <= LIVE_ROWS;   // (as many as eligible_row takes; N=8, B=32, half of the rows: 18.9 us, else 21.1)
     auto go = [&](auto is_one, auto is_compact) {
         constexpr bool ONE = decltype(is_one)::value, COMPACT = decltype(is_compact)::value;
         if (bf16) hipLaunchKernelGGL((logprobs_kernel<uint16_t, ONE, COMPACT>), units, block, 0, s, a);
