@@ -77,6 +77,19 @@
 //     Diffusion") go through a simpler masked path out of the same ring: rows
 //     of other rollouts are masked to -inf, and in the verify pass of scaffold
 //     speculative decoding the block keys after the query's own position too.
+//
+// The prefix in 8 bits (Q8 kernels: e4m3 codes, a power of two per tile and head)
+//   * A code times its scale is a bf16 number, so the same products are taken:
+//     tiles of codes go straight into a ring of their own in LDS, and the
+//     wavefront that moved them converts them into two bf16 slots beside the
+//     matrix instructions of the step before.  Half the bytes come from memory;
+//     a step has 8 conversions, 2 reads and 4 writes of 16 bytes of LDS a lane
+//     more (8 wavefronts).
+//   * us per call, 8-bit and bf16 prefix, Hq = 28, Hkv = 4, D = 128: N=16, B=64,
+//     L=16384 217 and 213 (1110 TFLOP/s); N=8, B=32, L=4096 26.9 and 24.5; N=1,
+//     B=32, L=16384 19.6 and 20.1, L=2048 11.3 and 10.7; 8 heads, B=1, L=8000
+//     14.4 and 15.8.  Bound by the same as there; 2 % of the large calls and 1 to
+//     2 us of the short ones are the conversion.
 #include <atomic>
 #include <type_traits>
 #include <utility>
