@@ -216,3 +216,28 @@ def test_unaligned_workspace_and_missing_outputs(F):
         for n, t in zip(("logprobs", "entropy", "top_ids", "top_logprobs"), ref):
             if n in outs:
                 assert torch.equal(outs[n].view(torch.int32), t.view(torch.int32))
+
+
+@pytest.mark.parametrize("seed", [1, 2, 3, 4])
+def test_random_calls(F, seed):
+    """Sizes, types, selected positions and values drawn: few or many entries that can be chosen, few different values, large offsets."""
+    rng = np.random.default_rng([77, seed])
+    for i in range(16):
+        N, B = int(rng.integers(1, 9)), int(rng.integers(1, 41))
+        V = int(np.exp(rng.uniform(0, np.log(60000))))
+        V = max(1, min(V, 2000000 // (N * B)))
+        dtype, top = (W.BF16, W.F32)[rng.integers(2)], int(rng.integers(0, min(V, 32) + 1))
+        kind, t = int(rng.integers(0, 4)), float(rng.choice([1.0, 0.3, 2.5, 40.0]))
+        print_case(test="logprobs_random", seed=seed, i=i, N=N, B=B, V=V, dtype=dtype, top=top, kind=kind, t=t)
+        x = W.widen(logits(rng, N, B, V, dtype), dtype).astype(np.float64)
+        if kind == 1:
+            x[rng.random(x.shape) < rng.choice([0.5, 0.99])] = -np.inf
+            np.put_along_axis(x, rng.integers(0, V, (N, B, 1)), 1.0, 2)
+        elif kind == 2:
+            x = np.rint(x * 0.5)
+        elif kind == 3:
+            x[..., : V // 3] += 20.0
+            x -= 100.0
+        mask = None if rng.random() < 0.4 else (rng.random((N, B)) < rng.choice([0.1, 0.5, 1.0])).astype(np.uint8)
+        tokens = rng.integers(-1, V + 1, (N, B)).astype(np.int32)
+        check(F, W.to_storage(x, dtype), tokens, dtype, top, t=t, mask=mask)
