@@ -8,8 +8,7 @@
 //
 // Bound by the bytes of the logits, which are read once, and close behind by the vector ALUs (13 instructions an entry, an exponential
 // among them).  N=16, B=64, V=152064 bf16, top 5 77 us (4.0 TB/s); N=8, B=32 25, half of the rows selected 18.7, top 0 14.9; N=1, B=32 11.7; one
-// piece (V=512) 5.1.  A row is cut into pieces, a
-// workgroup each; a thread requests its part together and takes its sums as the vectors come, against a number near its largest
+// piece (V=512) 4.8.  A row is cut into pieces, a workgroup each; a thread requests its part together and takes its sums as the vectors come, against a number near its largest
 // entry, before it meets the others.  Entry a is left out in the end: the one thread that has it has its sums taken again, an
 // entry a lane.
 // A thread keeps the largest entry of each of its vectors of 16 bytes, from which the top ones are found:
@@ -31,9 +30,12 @@ namespace fdd {
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
-// 16-byte vectors a thread holds at most, of 4, 6, 8, 12, 16: fastest with 8 at up to 256 rows of 152064; 12 and 16 are up to a
-// tenth faster at 1024 rows and slower at 32.
-constexpr int NV = 8;
+// 16-byte vectors a thread holds at most.  Of 4, 6, 8, 12, 16 fastest with 8 at up to 256 rows of 152064; 12 and 16 are 2 to 5 % faster
+// at 1024 rows of bf16 and up to 7 % slower in others.  Pieces of two a thread or fewer have a kernel of their own, without the requests
+// that bring nothing new; us with it and without: N=1, B=8, V=512 fp32 4.8 and 5.1; N=32, B=64, V=512 bf16 8.3 and 8.8; N=8, B=32, V=4001 5.6 and
+// 5.9; N=1, B=32, V=50001, top 20 10.3 and 10.6 (limits of one and four instead of two: within 0.2 of it).
+constexpr int MAX_NV = 8;
+constexpr int FEW_NV = 2;
 constexpr int MAX_TOP = FDD_LOGPROBS_MAX_TOP;
 constexpr int NEAR = 128;                    // vectors of a wavefront that may hold top entries
 constexpr int LIST = 1024;                   // candidates for the top entries of a piece
@@ -167,7 +169,7 @@ struct WaveSum {
 };
 
 // one workgroup per (row, piece); ONE: a row is one piece, and is finished here; COMPACT: workgroups are dealt to selected rows only
-template <typename T, bool ONE, bool COMPACT>
+template <typename T, bool ONE, bool COMPACT, int NV>
 __global__ __launch_bounds__(THREADS) void logprobs_kernel(Args a)
 {
     constexpr int VEC = 16 / sizeof(T);
@@ -564,7 +566,7 @@ LogprobPlan make_logprob_plan(const fdd_logprob_params& p)
 {
     const long long vec = p.dtype == FDD_BF16 ? 8 : 4, rows = (long long)p.N * p.B;
     const long long vecs = std::max(p.V / vec, 1ll);            // (the entries in front of a row's first vector may take one from this)
-    long long pieces = (vecs + NV * THREADS - 1) / (NV * THREADS);
+    long long pieces = (vecs + MAX_NV * THREADS - 1) / (MAX_NV * THREADS);
     if (pieces > 1) {
         const long long finer = std::min(2ll * kNumCU / rows, (vecs + 2 * THREADS - 1) / (2 * THREADS));
         pieces = std::max(pieces, finer);
@@ -602,10 +604,15 @@ hipError_t launch_logprobs(const fdd_logprob_params& p, hipStream_t s)
     a.c = LOG2E * a.inv_t;
     const dim3 rows((unsigned)a.rows), units((unsigned)a.rows * (unsigned)plan.pieces), block(THREADS);
     const bool bf16 = p.dtype == FDD_BF16, one = plan.pieces == 1, compact = a.mask && a.rows >= 16 && a.rows <= LIVE_ROWS;   // (as many as eligible_row takes; N=8, B=32, half of the rows: 18.9 us, else 21.1)
-    auto go = [&](auto is_one, auto is_compact) {
+    auto held = [&](auto is_one, auto is_compact, auto nv) {
         constexpr bool ONE = decltype(is_one)::value, COMPACT = decltype(is_compact)::value;
-        if (bf16) hipLaunchKernelGGL((logprobs_kernel<uint16_t, ONE, COMPACT>), units, block, 0, s, a);
-        else hipLaunchKernelGGL((logprobs_kernel<float, ONE, COMPACT>), units, block, 0, s, a);
+        constexpr int NV = decltype(nv)::value;
+        if (bf16) hipLaunchKernelGGL((logprobs_kernel<uint16_t, ONE, COMPACT, NV>), units, block, 0, s, a);
+        else hipLaunchKernelGGL((logprobs_kernel<float, ONE, COMPACT, NV>), units, block, 0, s, a);
+    };
+    auto go = [&](auto is_one, auto is_compact) {
+        if (plan.per <= FEW_NV * THREADS) held(is_one, is_compact, std::integral_constant<int, FEW_NV>());
+        else held(is_one, is_compact, std::integral_constant<int, MAX_NV>());
     };
     if (one && compact) go(std::true_type(), std::true_type());
     else if (one) go(std::true_type(), std::false_type());
