@@ -382,7 +382,8 @@ fdd_status fdd_verify_step(const fdd_verify_params *p);
  *
  * The sums run in fp32 over pieces of a row, which are joined in fp64; the largest term is kept out of the
  * sum and joins in ln(1 + rest), so that the log probability of a token that is nearly certain keeps its
- * digits.  Logits: finite values, and -inf for entries that can never be chosen.  A row without a
+ * digits.  Logits: finite values, down to the type's lowest number, and -inf for entries that can never be chosen; a
+ * log probability below fp32's lowest number is -inf.  A row without a
  * finite entry has no softmax: its logprobs, entropy and top_logprobs are NaN, its top_ids 0..top-1.  NaN and
  * +inf are not supported: such a row's outputs are undefined (nothing is read or written out of bounds).
  */

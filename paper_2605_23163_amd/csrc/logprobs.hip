@@ -159,7 +159,7 @@ __device__ __forceinline__ RowSum row_sum(float m, double s, double u)
 
 constexpr float FAR = -200.f;       // 2^y is 0 from -150 on; a difference of -inf would make NaN of y 2^y
 
-constexpr float NO_REF = -0x1.8p127f;      // below every reference but those that it may stand for
+constexpr float NO_REF = -0x1.fffffep127f;      // the lowest number: no reference lies above its thread's entries, so that sums are never scaled up to another one
 
 struct WaveSum {
     float m;          // largest entry
