@@ -538,8 +538,18 @@ def fdd_prefix_dequantize(prefix, rows, row0=0, dtype=None, k=None, v=None, stre
     return k, v
 
 
+def _check_out(out, q):
+    """The library writes as many elements as q has, of q's type."""
+    if out is not None:
+        if out.shape != q.shape:
+            raise ValueError(f"out must have the shape of q, {list(q.shape)}")
+        if out.dtype != q.dtype:
+            raise TypeError("out must have the element type of q")
+
+
 def _quant_attn_params(q, prefix, L, block_k, block_v, scaffold_mask, out, scale, splits, causal_block, ext_k, ext_v, E):
     """Parameters of a call (prefix in a cache) and the cache, or None in its place where there is no prefix."""
+    _check_out(out, q)
     cache = None if prefix is None else _quant_cache(prefix)
     L = int(L)
     if not 0 <= L <= (0 if cache is None else cache.capacity):
@@ -568,7 +578,7 @@ def fdd_block_attn_quant_workspace(q, prefix, L, block_k, block_v, splits=0, ext
 def fdd_block_attn_quant(q, prefix, L, block_k, block_v, scaffold_mask=None, out=None, scale=None, workspace=None, stream=None,
                          splits=0, causal_block=False, ext_k=None, ext_v=None, E=0, q_positions=None):
     """``fdd_block_attn`` with the shared prefix in 8 bits: its keys and values are the first L rows of the cache
-    ``prefix`` (a QuantPrefix; may be None iff L == 0).  Everything else is as there."""
+    ``prefix`` (a QuantPrefix; may be None iff L == 0).  ``out`` has q's shape and type.  Everything else is as there."""
     lib = load_library()
     if out is None:
         out = (torch.empty_like if stream is None else _maker(stream, q.device, torch.empty_like))(q)
@@ -592,6 +602,7 @@ def fdd_block_attn_quant(q, prefix, L, block_k, block_v, scaffold_mask=None, out
 
 
 def _batched_quant_params(q, prefix, L, block_k, block_v, out, scale, splits, causal_block, ext_k, ext_v, E):
+    _check_out(out, q)
     P = q.shape[0]
     cache = _quant_cache(prefix, batch=P)
     L = int(L)

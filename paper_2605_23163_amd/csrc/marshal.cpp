@@ -217,7 +217,9 @@ void fill_attn_quant(AttnQuantCall* c, PyObject* const* a)
     p->q = pointer(q);
     p->block_k = pointer(bk); p->block_v = pointer(bv);
     p->scaffold_mask = (decltype(p->scaffold_mask))on.or_null(a[5]);
-    p->out = pointer(on(a[6]));
+    const at::Tensor& out = on(a[6]);
+    need(out.sizes() == q.sizes() && out.scalar_type() == type);
+    p->out = pointer(out);
     if (a[7] != Py_None) {
         const at::Tensor &ek = on(a[7]), &ev = on(a[8]);
         need(ek.dim() == 4 && ek.size(0) == N && ek.size(2) == Hkv && ek.size(3) == D && ev.sizes() == ek.sizes());
