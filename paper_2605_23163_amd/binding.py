@@ -448,6 +448,12 @@ def _on_current_device(*tensors):
             raise ValueError(f"tensors must live on the current device cuda:{torch.cuda.current_device()}, not on {t.device}")
 
 
+def _check_workspace(workspace, dev):
+    """A caller's workspace is written to like any other tensor of a call."""
+    if workspace is not None and not (workspace.get_device() == dev and workspace.is_contiguous()):
+        raise ValueError(f"workspace must be contiguous GPU memory on the current device cuda:{dev}")
+
+
 def _quant_cache(prefix, batch=None):
     """The cache as the library takes it.  Problems of a batch may lie apart, the arrays of one are dense."""
     k, v, ks, vs = prefix
@@ -594,6 +600,7 @@ def fdd_block_attn_quant(q, prefix, L, block_k, block_v, scaffold_mask=None, out
             _set_q_positions(c.p, q_positions)
             if c.p.n_q_positions == 0:      # (0 stands for all positions in the library)
                 return out
+    _check_workspace(workspace, dev)
     p = c.p
     ws = _set_workspace(p, workspace, lib.fdd_block_attn_quant_workspace, q.device, stream)  # noqa: F841
     p.stream = handle
@@ -628,8 +635,10 @@ def fdd_block_attn_quant_batched(q, prefix, L, block_k, block_v, out=None, scale
     if out is None:
         out = (torch.empty_like if stream is None else _maker(stream, q.device, torch.empty_like))(q)
     p, cache = _batched_quant_params(q, prefix, L, block_k, block_v, out, scale, splits, causal_block, ext_k, ext_v, E)
+    dev, handle = _device_and_stream(stream)
+    _check_workspace(workspace, dev)
     ws = _set_workspace(p, workspace, lib.fdd_block_attn_quant_workspace, q.device, stream)  # noqa: F841
-    p.stream = _stream_ptr(stream)
+    p.stream = handle
     _check(lib.fdd_block_attn_quant(C.byref(p), C.byref(cache)))
     return out
 
@@ -694,6 +703,7 @@ def fdd_token_logprobs(logits, tokens, mask=None, top=0, temperature=1.0, logpro
             C.addressof(p), logits, tokens, mask, top, temperature, logprobs, entropy, top_ids, top_logprobs, dev):
         p, logprobs, entropy, top_ids, top_logprobs = _logprob_arguments(logits, tokens, mask, top, temperature, logprobs, entropy, top_ids,
                                                                         top_logprobs, stream)
+    _check_workspace(workspace, dev)
     ws = _set_workspace(p, workspace, lib.fdd_token_logprobs_workspace, logits.device, stream)  # noqa: F841
     p.stream = handle
     _check(lib.fdd_token_logprobs(C.addressof(p)))
