@@ -393,7 +393,7 @@ typedef struct fdd_logprob_params {
     int64_t V;
     int32_t dtype;                 /* fdd_dtype of logits */
     int32_t top;                   /* 0 .. min(V, FDD_LOGPROBS_MAX_TOP) */
-    float temperature;             /* positive and finite, and so is 1.5 / temperature */
+    float temperature;             /* positive, at most 2^120, and 1.5 / temperature finite (4.41e-39 and more) */
     int32_t reserved;              /* must be 0 */
     const void *logits;            /* [N,B,V] */
     const int32_t *tokens;         /* [N,B]; may be NULL iff logprobs is */

@@ -659,9 +659,10 @@ fdd_status fdd_token_logprobs(const fdd_logprob_params* p)
     const char* const fn = "fdd_token_logprobs";
     fdd_status st = check_shape(p, fn);
     if (st != FDD_OK) return st;
-    // (0 log2(e) / temperature has to be 0)
-    if (!(p->temperature > 0.f) || std::isinf(p->temperature) || std::isinf(LOG2E * (1.f / p->temperature)))
-        return fail(FDD_ERR_UNSUPPORTED, "%s: temperature must be positive and finite, and so must 1.5 / temperature", fn);
+    // (0 log2(e) / temperature has to be 0; and a difference of logits that fp32 cannot hold, 2^128 and more, has to be one whose exponential
+    // is 0: its y is 2^128 log2(e) / 2^120 = 369 below the largest at least, beyond FAR)
+    if (!(p->temperature > 0.f) || p->temperature > 0x1p120f || std::isinf(1.5f / p->temperature))
+        return fail(FDD_ERR_UNSUPPORTED, "%s: temperature must be positive and at most 2^120, and 1.5 / temperature finite", fn);
     if (!p->logits) return fail(FDD_ERR_NULL, "%s: logits must not be NULL", fn);
     if (p->logprobs && !p->tokens) return fail(FDD_ERR_NULL, "%s: logprobs need tokens", fn);
     if (p->top > 0 && !p->top_ids != !p->top_logprobs) return fail(FDD_ERR_NULL, "%s: top_ids and top_logprobs come together", fn);
