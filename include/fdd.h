@@ -217,7 +217,8 @@ typedef struct fdd_quant_rows {
  * Values: an infinity or a magnitude above 448 * 2^119 is stored as the largest code, a NaN as a NaN;
  * infinities and NaN have no part in the scale.  The source must not overlap the cache.
  *
- * fdd_prefix_dequantize: rows [row0, row0 + rows) of the cache are read back, exactly. */
+ * fdd_prefix_dequantize: rows [row0, row0 + rows) of the cache are read back, exactly.  Rows of k and v must not overlap; they may
+ * interleave. */
 fdd_status fdd_prefix_quantize(const fdd_quant_cache *cache, int32_t row0, const fdd_quant_rows *src, void *stream);
 fdd_status fdd_prefix_dequantize(const fdd_quant_cache *cache, int32_t row0, const fdd_quant_rows *dst, void *stream);
 

@@ -16,6 +16,7 @@
 //               maximum and the rounding, so a row is read once.
 //   dequantize  threads in the order of the destination.
 #include <cmath>
+#include <cstdlib>
 #include <type_traits>
 
 #include "fdd_internal.h"
@@ -341,6 +342,23 @@ fdd_status check_rows(const fdd_quant_cache* c, int row0, const fdd_quant_rows* 
     return FDD_OK;
 }
 
+// Whether a row of k and a row of v share bytes: they must not where both are written.  (Rows may interleave, as parts of wider ones.)
+bool rows_meet(const fdd_quant_cache& c, const fdd_quant_rows& r)
+{
+    const long long es = r.dtype == FDD_BF16 ? 2 : 4, row = (long long)c.Hkv * c.D * es, n = r.rows;
+    const long long sk = row_stride(c, r.k_row_stride) * es, sv = row_stride(c, r.v_row_stride) * es;
+    if (!overlap(r.k, (unsigned long long)((n - 1) * sk + row), r.v, (unsigned long long)((n - 1) * sv + row))) return false;
+    const long long apart = (long long)(reinterpret_cast<uintptr_t>(r.v) - reinterpret_cast<uintptr_t>(r.k));
+    // rows i of k whose neighbours in v have to be looked at: with equal strides only i - j counts
+    const bool equal = sk == sv;
+    for (long long i = 0; i < (equal ? 1 : n); ++i) {
+        const long long to = i * sk - apart, j0 = to >= 0 ? to / sv : -((-to + sv - 1) / sv);      // the last row of v that starts at row i of k or in front of it
+        for (long long j = j0; j <= j0 + 1; ++j)
+            if (j >= (equal ? 1 - n : 0) && j < n && std::llabs(j * sv - to) < row) return true;
+    }
+    return false;
+}
+
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Bytes of one of K and V of a call's prefix in the call's type, over all problems of its batch
@@ -395,6 +413,7 @@ fdd_status fdd_prefix_dequantize(const fdd_quant_cache* cache, int32_t row0, con
 {
     fdd_status st = check_rows(cache, row0, dst, "fdd_prefix_dequantize");
     if (st != FDD_OK || dst->rows == 0) return st;
+    if (rows_meet(*cache, *dst)) return fail(FDD_ERR_UNSUPPORTED, "fdd_prefix_dequantize: rows of k and v overlap");
     hipError_t e = launch_dequantize(*cache, row0, *dst, 1, 0, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(FDD_ERR_LAUNCH, "fdd_prefix_dequantize: launch failed: %s", hipGetErrorString(e));
     return FDD_OK;
