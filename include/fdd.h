@@ -215,7 +215,7 @@ typedef struct fdd_quant_rows {
  * are.  It does not shrink.  (All rows of that block in front of row0 and its scale have to be there: a scale is a power of two from
  * 2^-117 to 2^119, also in a cache that was filled by other means.)  Codes behind row0 + rows and scales of later blocks are left as they were.
  * Values: an infinity or a magnitude above 448 * 2^119 is stored as the largest code, a NaN as a NaN;
- * infinities and NaN have no part in the scale.  The source must not overlap the cache.
+ * infinities and NaN have no part in the scale.  The source must not overlap the cache, nor the cache's arrays one another.
  *
  * fdd_prefix_dequantize: rows [row0, row0 + rows) of the cache are read back, exactly.  Rows of k and v must not overlap; they may
  * interleave. */

@@ -404,6 +404,12 @@ fdd_status fdd_prefix_quantize(const fdd_quant_cache* cache, int32_t row0, const
 {
     fdd_status st = check_rows(cache, row0, src, "fdd_prefix_quantize");
     if (st != FDD_OK || src->rows == 0) return st;
+    const unsigned long long codes = (unsigned long long)cache->Hkv * cache->capacity * cache->D, scales = (unsigned long long)cache->Hkv * (cache->capacity / QB) * 4;
+    const struct { const void* p; unsigned long long bytes; } arrays[] = {{cache->k, codes}, {cache->v, codes}, {cache->k_scale, scales}, {cache->v_scale, scales}};
+    for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < i; ++j)
+            if (overlap(arrays[i].p, arrays[i].bytes, arrays[j].p, arrays[j].bytes))
+                return fail(FDD_ERR_UNSUPPORTED, "fdd_prefix_quantize: arrays of the cache overlap");
     hipError_t e = launch_quantize(*cache, row0, *src, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(FDD_ERR_LAUNCH, "fdd_prefix_quantize: launch failed: %s", hipGetErrorString(e));
     return FDD_OK;

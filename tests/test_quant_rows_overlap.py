@@ -45,3 +45,11 @@ def test_rows_may_interleave(dtype):
         assert int((buf != 7.0).sum()) <= 2 * m * w
     with pytest.raises(F.FddError, match="overlap"):
         F.fdd_prefix_dequantize(p, n, k=x, v=x)
+
+
+def test_a_cache_whose_arrays_overlap_is_not_written(lib):  # noqa: F811
+    codes, scales = 4 * 256 * 128, 4 * 4 * 4
+    for kw in (dict(v=1 << 20), dict(v=(1 << 20) + codes - 16), dict(v=(1 << 20) - codes + 16), dict(v_scale=1 << 22), dict(v_scale=(1 << 22) + scales - 4),
+               dict(k_scale=1 << 20), dict(k_scale=(1 << 21) + codes - 4), dict(v_scale=(1 << 20) - scales + 4), dict(v_scale=1 << 21)):
+        assert lib.fdd_prefix_quantize(C.byref(cache(**kw)), 0, C.byref(rows()), None) == 4, kw
+        assert "overlap" in lib.fdd_last_error().decode()
