@@ -226,10 +226,13 @@ fdd_status fdd_prefix_dequantize(const fdd_quant_cache *cache, int32_t row0, con
  * except that prefix_k, prefix_v and prefix_v_packed are NULL (prefix_batch_stride and packed_batch_stride
  * are ignored): the L keys and values of the prefix are rows [0, L) of `cache`, L <= cache->capacity,
  * converted without an error.  Queries, blocks, extensions and outputs are of type p->dtype.  The result is
- * that of fdd_block_attn on the rows as fdd_prefix_dequantize returns them, up to the order of sums.
- * `cache` may be NULL iff L == 0.  The workspace is fdd_block_attn_quant_workspace(p): a bf16 call converts the
+ * that of fdd_block_attn on the rows as fdd_prefix_dequantize returns them, up to the order of sums and, in bf16,
+ * to the 16 bits of averages: where a row's keys are cut into pieces (by `splits` or by the library), each piece's
+ * average is off by 2^-11 of itself, by 2^-39 of the row's largest element of it or by 2^-126, whichever is most.
+ * `cache` may be NULL iff L == 0.  The workspace is fdd_block_attn_quant_workspace(p), no less: a bf16 call converts the
  * prefix tile by tile on its way to the matrix pipe and needs no room for it; an fp32 call converts it first and
- * needs room for its K and V in fp32.  Values and q_positions as with fdd_block_attn; a NaN in the cache is a NaN. */
+ * needs room for its K and V in fp32.  Values and q_positions as with fdd_block_attn, a NaN in the cache being one
+ * among the values: fp32 passes it on, bf16 leaves the rows that see it undefined. */
 size_t fdd_block_attn_quant_workspace(const fdd_attn_params *p);
 fdd_status fdd_block_attn_quant(const fdd_attn_params *p, const fdd_quant_cache *cache);
 
