@@ -85,9 +85,10 @@
 //     matrix instructions of the step before.  Half the bytes come from memory;
 //     a step has 8 conversions, 2 reads and 4 writes of 16 bytes of LDS a lane
 //     more (8 wavefronts).
-//   * us per call, 8-bit and bf16 prefix, Hq = 28, Hkv = 4, D = 128: N=16, B=64,
-//     L=16384 217 and 213 (1110 TFLOP/s); N=8, B=32, L=4096 26.9 and 24.5; N=1,
-//     B=32, L=16384 19.6 and 20.1, L=2048 11.3 and 10.7; 8 heads, B=1, L=8000
+//   * us per call, 8-bit and bf16 prefix, prefixes from memory (in rotation, from a
+//     graph), Hq = 28, Hkv = 4, D = 128: N=16, B=64,
+//     L=16384 220 and 216 (1095 TFLOP/s); N=8, B=32, L=4096 27.5 and 25.0; N=1,
+//     B=32, L=16384 19.9 and 20.8, L=2048 11.3 and 10.6; 8 heads, B=1, L=8000
 //     14.4 and 15.8.  Bound by the same as there; 2 % of the large calls and 1 to
 //     2 us of the short ones are the conversion.
 #include <atomic>

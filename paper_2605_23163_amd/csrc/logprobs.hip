@@ -7,7 +7,7 @@
 // Both terms of the entropy are >= 0, and S without the largest term keeps its digits where the row is nearly certain.
 //
 // Bound by the bytes of the logits, which are read once, and close behind by the vector ALUs (13 instructions an entry, an exponential
-// among them).  N=16, B=64, V=152064 bf16, top 5 77 us (4.0 TB/s); N=8, B=32 25, half of the rows selected 18.7, top 0 14.9; N=1, B=32 11.7; one
+// among them).  N=16, B=64, V=152064 bf16, top 5 71 to 77 us (4.4 to 4.0 TB/s); N=8, B=32 25.7, half of the rows selected 18.6, top 0 14.9; N=1, B=32 11.6; one
 // piece (V=512) 4.8.  A row is cut into pieces, a workgroup each; a thread requests its part together and takes its sums as the vectors come, against a number near its largest
 // entry, before it meets the others.  Entry a is left out in the end: the one thread that has it has its sums taken again, an
 // entry a lane.

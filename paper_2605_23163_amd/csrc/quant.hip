@@ -8,8 +8,10 @@
 // value has four significant bits, so it is a bf16 number (2^-9 * 2^-117 is the smallest bf16 normal one), codes can
 // move to a larger scale, and attention multiplies the values that are read back here.
 //
-// Both kernels are bound by the bytes that they move, short calls by their launch (32 rows 2.7 and 2.0 us).  K and V of 32768 rows of
-// 8 x 128 bf16 are written in 42 us (4.8 TB/s read and written) and read in 42 us, 16384 of 4 x 128 in 14.4 and 12.4 (3.5 and 4.1 TB/s).
+// Both kernels are bound by the bytes that they move, short calls by their launch (32 rows 2.5 and 1.9 us).  Written and read back, arrays in
+// rotation so that all of it comes from memory, a launch included: 32768 rows of 8 x 128 bf16 40 and 42 us (5.0 and 4.8 TB/s read and
+// written), 16384 of 4 x 128 14.3 and 12.4 (3.5 and 4.1), fp32 18.8 and 17.6 (4.5 and 4.8).  The 84 MB of the second fit the last-level cache: the
+// same arrays again and again take 12.9 and 11.5.
 // A thread takes as many elements at a time as 16 bytes of the rows hold (8
 // bf16, 4 fp32), so that neighbouring lanes load or store neighbouring pieces.
 //   quantize    one workgroup per (block of 64 rows, KV head, K or V): it holds the block in registers between the
