@@ -415,6 +415,228 @@ size_t fdd_token_logprobs_workspace(const fdd_logprob_params *p);
 fdd_status fdd_token_logprobs(const fdd_logprob_params *p);
 
 /* ------------------------------------------------------------------------
+ * Rotary positions.
+ *
+ * Channel pair i of a head, i < rot_dim / 2, is the point (x, y) = channels (i, i + rot_dim / 2), or (2i, 2i + 1) with
+ * `interleaved`; at position p it becomes
+ *     magnitude * (x cos a - y sin a, y cos a + x sin a),      a = p w_i;
+ * channels from rot_dim on stay as they are.  With w = base^(-2i / rot_dim), by `scaling`:
+ *     FDD_ROPE_NONE     w_i = w
+ *     FDD_ROPE_LINEAR   w_i = w / stretch
+ *     FDD_ROPE_BASE     w_i = (base * stretch^(rot_dim / (rot_dim - 2)))^(-2i / rot_dim): the last pair as with LINEAR, the first
+ *                       as without
+ *     FDD_ROPE_PARTS    w_i = g w + (1 - g) w / stretch, g = clamp((original w / 2 pi - 1) / 31, 0, 1): pairs that turn 32 times
+ *                       and more over the `original` length stay, those that turn once or less are stretched; magnitude is
+ *                       0.1 ln(stretch) + 1  ("YaRN: Efficient Context Window Extension of Large Language Models", arXiv
+ *                       2309.00071: its interpolation by parts and its temperature)
+ * and magnitude 1 where none is named.
+ *
+ * A frequency is held as the part of a turn that one position makes, turns[i] = round(w_i / 2 pi * 2^64) mod 2^64.  A position
+ * times it, modulo 2^64, is the angle without the whole turns: to 2^-31 of a turn at every int32 position, also negative
+ * ones.  Sine and cosine are within 2^-23 of theirs, all arithmetic is fp32, the result is rounded once.
+ *
+ * fdd_rope_turns: turns (a HOST array of rot_dim / 2) and magnitude of the table; host-only arithmetic.  A caller
+ * copies them to the device once, or fills a table of its own.
+ */
+enum { FDD_ROPE_NONE = 0, FDD_ROPE_LINEAR = 1, FDD_ROPE_BASE = 2, FDD_ROPE_PARTS = 3 };
+typedef struct fdd_rope_scaling {
+    int32_t rot_dim;               /* even, 2 .. 1024; FDD_ROPE_BASE: 4 and more */
+    int32_t scaling;               /* FDD_ROPE_* */
+    double base;                   /* above 1, finite */
+    double stretch;                /* at least 1, finite; ignored with FDD_ROPE_NONE */
+    double original;               /* positive, finite; FDD_ROPE_PARTS only */
+} fdd_rope_scaling;
+fdd_status fdd_rope_turns(const fdd_rope_scaling *p, uint64_t *turns, float *magnitude);
+
+typedef struct fdd_rope_table {
+    const uint64_t *turns;         /* [rot_dim / 2], 8-byte aligned */
+    int32_t rot_dim;               /* even, at least 2, at most the head size */
+    int32_t interleaved;           /* 0: pairs (i, i + rot_dim / 2); 1: pairs (2i, 2i + 1) */
+    float magnitude;               /* finite */
+    int32_t reserved;              /* must be 0 */
+} fdd_rope_table;
+
+/* fdd_rope: rows of queries and, if k is given, of keys are rotated, each row at its position.  Consecutive rows of an array
+ * lie `stride` elements apart (0 = dense); heads and channels of a row are dense.  q_out may be q itself with the same stride (in
+ * place), and k_out k; otherwise no output overlaps anything.  Any alignment of the type; 16-byte aligned rows and a rot_dim
+ * whose half is a multiple of 16 bytes are faster.  rows = 0 is a call that does nothing.
+ * FDD_ROPE_INVERSE turns the other way, by the same magnitude: the gradient of the rows with respect to what was rotated. */
+#define FDD_ROPE_INVERSE 1
+typedef struct fdd_rope_params {
+    int32_t rows, Hq, Hk, D;       /* Hk: heads of k, ignored where k is NULL; D at most 1024 */
+    int32_t dtype;                 /* fdd_dtype */
+    int32_t flags;                 /* FDD_ROPE_INVERSE */
+    fdd_rope_table table;
+    const int32_t *positions;      /* [rows] */
+    const void *q;                 /* [rows,Hq,D] */
+    void *q_out;
+    const void *k;                 /* [rows,Hk,D]; may be NULL */
+    void *k_out;
+    int64_t q_stride, q_out_stride, k_stride, k_out_stride;
+    void *stream;
+} fdd_rope_params;
+fdd_status fdd_rope(const fdd_rope_params *p);
+
+/* ------------------------------------------------------------------------
+ * A paged cache.
+ *
+ * K and V of N requests in pages of page_size rows that any request may take: a head's rows of a page lie together.  Row r of
+ * request n is row r mod page_size of page page_table[n][r / page_size].  lens[n] rows are held.  Both lists are DEVICE memory,
+ * read when the call runs: a captured call follows them.  What lies behind a request's last row, in pages nobody lists and in
+ * entries of the table behind the last page is never used.
+ * The library cannot read the lists on the host.  A length is clamped into [0, max_pages * page_size]; rows of a page outside
+ * [0, pages) are not written, and read as those of the nearest page there is (nothing is accessed out of bounds).
+ */
+typedef struct fdd_paged_cache {
+    void *k;                       /* [pages,Hkv,page_size,D] */
+    void *v;
+    const int32_t *page_table;     /* [N,max_pages] */
+    const int32_t *lens;           /* [N] */
+    int32_t N;
+    int32_t pages;
+    int32_t page_size;             /* a power of two, 16 .. 1024 */
+    int32_t max_pages;             /* max_pages * page_size below 2^30 */
+    int32_t Hkv, D;                /* D 64 or 128 */
+    int32_t dtype;                 /* fdd_dtype */
+    int32_t reserved;              /* must be 0 */
+} fdd_paged_cache;
+
+/* fdd_paged_append: rows join the cache behind those that each request holds.  For j in [0, n_rows[n]) source row
+ * i = rows[n][j] (rows NULL: i = j) of request n becomes row lens[n] + j, k rotated by `rope` (NULL: as it is) at position
+ * positions[n][i], or lens[n] + j where positions is NULL.  lens is not changed: the calls of all layers of a step read the same
+ * ones, and the caller adds n_rows once they have been made.  Rows that would lie behind the table's last page and rows
+ * whose i is outside [0, B) are not written.  n_rows is clamped into [0, B].  No page may be listed at two places that a call
+ * writes.  The source must not overlap the cache, nor K's pages V's. */
+typedef struct fdd_paged_append_params {
+    int32_t B;                     /* source rows per request */
+    int32_t reserved;              /* must be 0 */
+    const void *k;                 /* [N,B,Hkv,D]: token (n,b) at (n*B + b) * k_stride */
+    const void *v;
+    int64_t k_stride, v_stride;    /* elements, rows 16-byte aligned; 0 = Hkv*D */
+    const fdd_rope_table *rope;    /* a host struct; may be NULL */
+    const int32_t *positions;      /* [N,B]; may be NULL */
+    const int32_t *rows;           /* [N,B]; may be NULL */
+    const int32_t *n_rows;         /* [N]; may be NULL (= B) */
+    void *stream;
+} fdd_paged_append_params;
+fdd_status fdd_paged_append(const fdd_paged_cache *cache, const fdd_paged_append_params *p);
+
+/* ------------------------------------------------------------------------
+ * Trees of drafted tokens.
+ *
+ * The B tokens of a request are a tree: token 0 is its root, the last token that is certain, and token i > 0 follows token
+ * parents[n][i], which is in [0, i).  (A token whose entry is not has no parent: it sees itself only and is never accepted.  The
+ * entry of token 0 is not used.)  n_tokens[n] of the B tokens are there, clamped into [0, B].
+ *
+ * fdd_tree_mask: bit j mod 64 of mask[n][i][j / 64] is set where token j is i itself or one that it follows, through any number of
+ * steps; positions[n][i] = lens[n] + the number of those steps.  Tokens that are not there have no bits and position 0.
+ */
+#define FDD_TREE_MAX 1024
+typedef struct fdd_tree_mask_params {
+    int32_t N, B;                  /* B at most FDD_TREE_MAX */
+    const int32_t *parents;        /* [N,B], or [B] for all requests */
+    int64_t parents_stride;        /* entries between requests: at least B, or 0 = one tree for all */
+    const int32_t *lens;           /* [N]; may be NULL (= 0) */
+    const int32_t *n_tokens;       /* [N]; may be NULL (= B) */
+    uint64_t *mask;                /* [N,B,ceil(B/64)] out; may be NULL if positions is not */
+    int32_t *positions;            /* [N,B] out; may be NULL if mask is not */
+    void *stream;
+} fdd_tree_mask_params;
+fdd_status fdd_tree_mask(const fdd_tree_mask_params *p);
+
+/* ------------------------------------------------------------------------
+ * fdd_paged_attn: attention of every request's new tokens over its paged cache and over one another.
+ *
+ * For request n, token b < n_tokens[n], query head h (KV head kh = h / (Hq/Hkv)):
+ *   keys   = rows [0, lens[n]) of the cache ++ block_k[n, j] for the tokens j < n_tokens[n] that b sees
+ *   out[n,b,h,:] = softmax(scale * q[n,b,h,:] . keys^T) values
+ * All rows of the cache are seen.  Token b sees token j where bit j mod 64 of mask[n][b][j / 64] is set (fdd_tree_mask, or any
+ * other pattern); without a mask all tokens, as in fdd_block_attn, or with FDD_ATTN_CAUSAL_BLOCK those up to b itself.  One token
+ * per request (B = 1) is the ordinary decoding step.  Tokens n_tokens[n] .. B are not there: their K and V are not
+ * used and their rows of `out` stay as they were.  A row that sees nothing (no cache, no bit) is 0.  Queries and keys arrive rotated.
+ *
+ * FDD_BF16: products on the matrix cores with fp32 accumulation, softmax in fp32, probabilities rounded to bf16.  FDD_F32: fp32
+ * products and sums.  The order of sums depends on lens, n_tokens and max_len of all requests, and on nothing else.
+ *
+ * Values: q, k and v finite, scores within fp32's range, for what is seen; keys that a row does not see may hold anything.  A NaN
+ * or an infinity in V of a token that is there, or in a cached row, reaches all rows of its request and KV head.
+ */
+typedef struct fdd_paged_attn_params {
+    int32_t B, Hq;
+    int32_t flags;                 /* FDD_ATTN_CAUSAL_BLOCK; not together with mask */
+    int32_t max_len;               /* no request holds more rows (longer ones are cut there); 0 = max_pages * page_size.  Sizes the workspace. */
+    float scale;                   /* softmax scale; <= 0 selects 1/sqrt(D) */
+    int32_t reserved;              /* must be 0 */
+    const void *q;                 /* [N,B,Hq,D]: token (n,b) at (n*B + b) * q_stride; likewise block_k, block_v */
+    const void *block_k;           /* [N,B,Hkv,D] */
+    const void *block_v;
+    int64_t q_stride, k_stride, v_stride;   /* elements, tokens 16-byte aligned; 0 = dense */
+    const uint64_t *mask;          /* [N,B,ceil(B/64)], or [B,ceil(B/64)] for all requests; may be NULL */
+    int64_t mask_stride;           /* words between requests: at least B*ceil(B/64), or 0 = one mask for all */
+    const int32_t *n_tokens;       /* [N]; may be NULL (= B) */
+    void *out;                     /* [N,B,Hq,D] */
+    void *workspace;               /* >= fdd_paged_attn_workspace() bytes */
+    size_t workspace_bytes;
+    void *stream;
+} fdd_paged_attn_params;
+/* Bytes of scratch (host-only arithmetic; 0 for invalid params and for calls that need none). */
+size_t fdd_paged_attn_workspace(const fdd_paged_cache *cache, const fdd_paged_attn_params *p);
+fdd_status fdd_paged_attn(const fdd_paged_cache *cache, const fdd_paged_attn_params *p);
+
+/* ------------------------------------------------------------------------
+ * fdd_tree_verify: which drafted tokens stand, from given random numbers, so that what is emitted is distributed as if the target
+ * model had drawn token after token.
+ *
+ * logits[n,i,:] is the target's distribution of the token behind token i: p_i = softmax(logits[n,i,:] / temperature).  A walk
+ * starts at token 0.  At token i its children (tokens j with parents[n][j] == i, lowest j first) are tried:
+ *   temperature 0      child j stands where tokens[n][j] is the lowest id attaining the largest logit; if none does, that id is
+ *                      emitted and the walk ends.
+ *   temperature > 0    w = p_i, W = 1.  Child j with token x stands where  uniforms[n][j][0] * q(x) * W < w(x),  with q(x) = 1, or
+ *                      with draft_logits q_i = softmax(draft_logits[n,i,:] / draft_temperature), from which x was drawn.
+ *                      Otherwise what the draft accounts for is taken out: w(x) = 0, or with draft_logits
+ *                      w = max(p_i - q_i, 0); W = sum w.  If none stands, the token drawn from w by uniforms[n][i][1] = u
+ *                      is emitted, the lowest id v with w(0) + .. + w(v) > u * W, and the walk ends; where W < 2^-40 it is drawn
+ *                      from p_i instead.
+ * A child that stands is emitted and the walk goes on there.  So a walk of k tokens emits k: path[n] = (0, the tokens that
+ * stand), n_path[n] = k, emitted[n] = (what stands, the token drawn at the end); entries of path and emitted behind k are -1.  A
+ * request without tokens gets n_path 0.  The accepted rows of K and V are path's: `rows` and `n_rows` of fdd_paged_append.
+ * chances[n][j] is the probability with which token j stands when it is tried first: min(1, p(x) / q(x)); 1 for token 0, 0
+ * for tokens that are not there or have no parent; with temperature 0 it is 1 or 0.
+ *
+ * draft_logits go with chains only (parents NULL: token j follows j - 1); tokens of a tree count as chosen, not drawn.  Only rows of
+ * tokens that are there are read, of draft_logits only those that another token follows.  Tokens outside [0, V) never stand
+ * (with q(x) = 1 they take nothing out).  Uniforms are in [0, 1).
+ *
+ * Tests and chances are taken in fp32 (relative 2^-18 for logits within +-2^7 temperatures of the largest); what the last token is
+ * drawn from is summed in fp64.  Logits: finite values and -inf for entries that can never be chosen, a row that is read needs one finite
+ * entry.  NaN and +inf are not supported: such a request's outputs are undefined (ids stay in range).
+ */
+typedef struct fdd_tree_verify_params {
+    int32_t N, B;                  /* B at most FDD_TREE_MAX */
+    int64_t V;                     /* below 2^31 */
+    int32_t dtype;                 /* fdd_dtype of logits and draft_logits */
+    float temperature;             /* 0, or 2^-20 .. 2^20 */
+    float draft_temperature;       /* 2^-20 .. 2^20; draft_logits only */
+    int32_t reserved;              /* must be 0 */
+    const void *logits;            /* [N,B,V] */
+    const void *draft_logits;      /* [N,B,V]; may be NULL; ignored with temperature 0 */
+    const int32_t *tokens;         /* [N,B] */
+    const int32_t *parents;        /* [N,B], or [B] for all requests; may be NULL (= a chain) */
+    int64_t parents_stride;        /* entries between requests: at least B, or 0 = one tree for all */
+    const float *uniforms;         /* [N,B,2]; may be NULL with temperature 0 */
+    const int32_t *n_tokens;       /* [N]; may be NULL (= B) */
+    int32_t *path;                 /* [N,B] out */
+    int32_t *n_path;               /* [N] out */
+    int32_t *emitted;              /* [N,B] out */
+    float *chances;                /* [N,B] out; may be NULL */
+    void *workspace;               /* >= fdd_tree_verify_workspace() bytes */
+    size_t workspace_bytes;
+    void *stream;
+} fdd_tree_verify_params;
+size_t fdd_tree_verify_workspace(const fdd_tree_verify_params *p);
+fdd_status fdd_tree_verify(const fdd_tree_verify_params *p);
+
+/* ------------------------------------------------------------------------
  * Rollout-fork bookkeeping ("fork the KV cache N times").
  *
  * fdd_fork_block: dst[n] = src for n in [0,N), `bytes` bytes each: the

@@ -37,3 +37,16 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
 )
+from .paged import (  # noqa: F401
+    PagedCache,
+    RopeTable,
+    fdd_paged_append,
+    fdd_paged_attn,
+    fdd_paged_attn_workspace,
+    fdd_paged_cache,
+    fdd_rope,
+    fdd_rope_table,
+    fdd_tree_mask,
+    fdd_tree_verify,
+    fdd_tree_verify_workspace,
+)

@@ -24,6 +24,8 @@ FDD_LOGPROBS_MAX_TOP = 32
 EXPORTS = ("fdd_block_attn_workspace", "fdd_block_attn", "fdd_prefix_pack_bytes", "fdd_prefix_pack",
            "fdd_prefix_quantize", "fdd_prefix_dequantize", "fdd_block_attn_quant_workspace", "fdd_block_attn_quant",
            "fdd_token_logprobs_workspace", "fdd_token_logprobs",
+           "fdd_rope_turns", "fdd_rope", "fdd_paged_append", "fdd_tree_mask", "fdd_paged_attn_workspace", "fdd_paged_attn",
+           "fdd_tree_verify_workspace", "fdd_tree_verify",
            "fdd_unmask_workspace", "fdd_unmask_step", "fdd_unmask_step_static", "fdd_verify_workspace", "fdd_verify_step",
            "fdd_fork_block", "fdd_block_kv_update", "fdd_block_commit", "fdd_traj_mean", "fdd_profile_attn_events", "fdd_last_error", "fdd_version")
 
@@ -164,6 +166,11 @@ def load_library():
         lib.fdd_token_logprobs_workspace.argtypes = [C.c_void_p]
         lib.fdd_token_logprobs.restype = C.c_int
         lib.fdd_token_logprobs.argtypes = [C.c_void_p]
+        for name, args in (("fdd_rope_turns", 3), ("fdd_rope", 1), ("fdd_paged_append", 2), ("fdd_tree_mask", 1), ("fdd_paged_attn", 2),
+                           ("fdd_tree_verify", 1), ("fdd_paged_attn_workspace", 2), ("fdd_tree_verify_workspace", 1)):
+            fn = getattr(lib, name)
+            fn.restype = C.c_size_t if name.endswith("_workspace") else C.c_int
+            fn.argtypes = [C.c_void_p] * args
         lib.fdd_unmask_workspace.restype = C.c_size_t
         lib.fdd_unmask_workspace.argtypes = [C.POINTER(UnmaskParams)]
         lib.fdd_unmask_step.restype = C.c_int

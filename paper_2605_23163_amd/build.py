@@ -30,6 +30,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + os.path.j
 # without entries as bits.  The fp32 attention kernel passes the caller's NaN and infinities on.
 EXTRA = {"attn_bf16.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
          "logprobs.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
+         "paged_attn.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
          "unmask.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"]}
 
 

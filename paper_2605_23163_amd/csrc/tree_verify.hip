@@ -1,0 +1,593 @@
+// Which drafted tokens of a tree or a chain stand, from given random numbers (fdd_tree_verify).
+//
+// With p the target's distribution behind a token and q the one a child was drawn from (or 1, where it was chosen), a child x
+// stands with probability min(1, p(x) / q(x)), and what is drawn where none does comes from what q leaves of p, max(p - q, 0) (or
+// from p without the children): token after token is then distributed as p.
+//
+// Four launches (two where the target is greedy):
+//   stats   one read of the logits: maximum and sum of exponentials of pieces of every row that is there
+//   walk    one workgroup per request: joins the pieces, tests the children, leaves the path and the token it ends at
+//   weigh   the row of that token alone, once more and in fp64: sums of pieces of what the last token is drawn from
+//           (a chain with draft_logits: both rows' sums, and in a launch behind it those of max(p - q, 0))
+//   pick    the piece that the uniform falls into, entry by entry
+// A test compares two numbers: fp32 exponentials decide it unless they are within 2^-18 of each other.  The draw compares with
+// V borders that lie as close as the smallest probabilities: an fp32 exponential's error, summed over the row, would move one draw in a
+// few hundred (V = 152064, logits of deviation 2) to a neighbouring entry, so these sums are fp64, and only one row a request needs them.
+#include <cfloat>
+
+#include "paged.h"
+
+namespace fdd {
+namespace tree_verify {
+
+constexpr int MAX_PIECES = 64;          // a wavefront joins a row's
+constexpr int STAT_THREADS = 256, WALK_THREADS = 1024;
+constexpr double LOG2E = 1.4426950408889634074;
+constexpr double NOTHING_LEFT = 0x1p-40;
+
+struct Stat {        // of a piece of a row
+    float max;
+    int arg;         // greedy: lowest id of the largest
+    double sum;      // of exp((x - max) / temperature)
+};
+
+// per request, from `walk` to the launches behind it
+struct Stop {
+    int token;              // where the walk ended, or -1: nothing to draw
+    int n_path;
+    float max, draft_max;   // of the two rows
+};
+
+struct Args {
+    const void* logits;
+    const void* draft;
+    const int32_t* tokens;
+    const int32_t* parents;
+    long long parents_stride;
+    const float* uniforms;
+    const int32_t* n_tokens;
+    int32_t* path;
+    int32_t* n_path;
+    int32_t* emitted;
+    float* chances;
+    Stat* stats;            // [2][N*B][pieces]
+    Stop* stops;            // [N]
+    double* sums;           // [3][N][pieces]: of p, of what is drawn from, of q
+    int N, B, V, pieces, per_piece;       // per_piece: entries, a multiple of 8
+    float c, draft_c;                     // log2(e) / temperature
+    double c64, draft_c64;
+};
+
+__device__ __forceinline__ int count_of(const Args& a, int n) { return a.n_tokens ? min(max(a.n_tokens[n], 0), a.B) : a.B; }
+__device__ __forceinline__ int parent_at(const Args& a, int n, int j)
+{
+    if (j == 0) return -1;
+    return a.parents ? parent_of(j, a.parents[n * a.parents_stride + j]) : j - 1;
+}
+
+template <typename T>
+__device__ __forceinline__ float entry(const T* p)
+{
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(float, (uint32_t)*p << 16);
+    else return *p;
+}
+// 16 bytes of a row, which may start anywhere
+template <typename T>
+__device__ __forceinline__ void entries(const T* p, float (&x)[16 / sizeof(T)])
+{
+    uint32_t w[4];
+    __builtin_memcpy(w, p, 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 2) {
+            x[2 * i] = __builtin_bit_cast(float, w[i] << 16);
+            x[2 * i + 1] = __builtin_bit_cast(float, w[i] & 0xffff0000u);
+        } else {
+            x[i] = __builtin_bit_cast(float, w[i]);
+        }
+    }
+}
+
+__device__ __forceinline__ double wave_sum(double x)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    return x;
+}
+
+// ---- stats -------------------------------------------------------------------------------------------------------------
+template <typename T, bool GREEDY>
+__global__ __launch_bounds__(STAT_THREADS) void stats_kernel(Args a)
+{
+    constexpr int VE = 16 / sizeof(T);
+    __shared__ float s_max[STAT_THREADS / 64], s_sum[STAT_THREADS / 64];
+    __shared__ int s_arg[STAT_THREADS / 64];
+    const int piece = blockIdx.x % a.pieces, row = blockIdx.x / a.pieces, which = blockIdx.y;
+    const int n = row / a.B, i = row - n * a.B;
+    const int count = count_of(a, n);
+    if (i >= count || (which && i + 1 >= count)) return;       // (a draft's last row has no token behind it)
+    const T* const x = static_cast<const T*>(which ? a.draft : a.logits) + (long long)row * a.V;
+    const float c = which ? a.draft_c : a.c;
+    const int v0 = piece * a.per_piece, v1 = min(v0 + a.per_piece, a.V);
+    float m = -FLT_MAX, s = 0.f;          // (never above the entries, but for -inf, which weighs nothing)
+    int arg = v0;
+    bool any = false;
+    auto take = [&](const float* y, int count_y, int v) {
+        float best = y[0];
+        int at = 0;
+        for (int j = 1; j < count_y; ++j)
+            if (y[j] > best) {
+                best = y[j];
+                at = j;
+            }
+        if constexpr (GREEDY) {
+            if (!any || best > m) {
+                m = best;
+                arg = v + at;
+                any = true;
+            }
+        } else {
+            if (best > m) {
+                s *= __builtin_amdgcn_exp2f((m - best) * c);
+                m = best;
+            }
+            for (int j = 0; j < count_y; ++j) s += __builtin_amdgcn_exp2f((y[j] - m) * c);
+        }
+    };
+    const int whole = v0 + (v1 - v0) / VE * VE;
+    for (int v = v0 + threadIdx.x * VE; v < whole; v += STAT_THREADS * VE) {
+        float y[VE];
+        entries(x + v, y);
+        take(y, VE, v);
+    }
+    if (whole + (int)threadIdx.x < v1) {
+        const float y = entry(x + whole + threadIdx.x);
+        take(&y, 1, whole + threadIdx.x);
+    }
+    if (GREEDY && !any) m = -INFINITY, arg = a.V;          // (a thread without entries)
+    // join the threads
+    for (int d = 1; d < 64; d *= 2) {
+        const float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d);
+        const int arg2 = __shfl_xor(arg, d);
+        if constexpr (GREEDY) {
+            if (m2 > m || (m2 == m && arg2 < arg)) m = m2, arg = arg2;
+        } else {
+            const float top = fmaxf(m, m2);
+            s = s * __builtin_amdgcn_exp2f((m - top) * c) + s2 * __builtin_amdgcn_exp2f((m2 - top) * c);
+            m = top;
+        }
+    }
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) s_max[wave] = m, s_sum[wave] = s, s_arg[wave] = arg;
+    __syncthreads();
+    if (threadIdx.x) return;
+    double sum = 0.0;
+    for (int w = 0; w < STAT_THREADS / 64; ++w)
+        if (GREEDY ? s_max[w] > m || (s_max[w] == m && s_arg[w] < arg) : s_max[w] > m) m = s_max[w], arg = s_arg[w];
+    for (int w = 0; w < STAT_THREADS / 64; ++w) sum += (double)(s_sum[w] * __builtin_amdgcn_exp2f((s_max[w] - m) * c));
+    Stat r;
+    r.max = m;
+    r.arg = min(arg, a.V - 1);
+    r.sum = GREEDY ? 0.0 : sum;
+    a.stats[((long long)which * a.N * a.B + row) * a.pieces + piece] = r;
+}
+
+// ---- walk --------------------------------------------------------------------------------------------------------------
+template <typename T, bool GREEDY>
+__global__ __launch_bounds__(WALK_THREADS) void walk_kernel(Args a)
+{
+    __shared__ float s_max[2][FDD_TREE_MAX];
+    __shared__ double s_sum[2][FDD_TREE_MAX];
+    __shared__ int s_arg[FDD_TREE_MAX];             // greedy: of the row; else tokens
+    __shared__ int s_parent[FDD_TREE_MAX];
+    __shared__ float s_p[FDD_TREE_MAX], s_q[FDD_TREE_MAX];      // of a token under its parent's rows
+    const int n = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int count = count_of(a, n);
+    const bool draft = !GREEDY && a.draft;
+    const long long row0 = (long long)n * a.B;
+    for (int j = tid; j < a.B; j += WALK_THREADS) {
+        if (a.chances && (j == 0 || j >= count)) a.chances[row0 + j] = j < count ? 1.f : 0.f;
+        s_parent[j] = parent_at(a, n, j);
+    }
+    // rows: a wavefront joins the pieces of one after the other
+    for (int r = wave; r < (draft ? 2 : 1) * count; r += WALK_THREADS / 64) {
+        const int which = r >= count, i = which ? r - count : r;
+        if (which && i + 1 >= count) continue;
+        const float c = which ? a.draft_c : a.c;
+        Stat st = {-INFINITY, a.V - 1, 0.0};
+        if (lane < a.pieces) st = a.stats[((long long)which * a.N * a.B + row0 + i) * a.pieces + lane];
+        float m = st.max;
+        int arg = st.arg;
+        for (int d = 1; d < 64; d *= 2) {
+            const float m2 = __shfl_xor(m, d);
+            const int arg2 = __shfl_xor(arg, d);
+            if (m2 > m || (m2 == m && arg2 < arg)) m = m2, arg = arg2;
+        }
+        const double sum = GREEDY ? 0.0 : wave_sum(lane < a.pieces ? st.sum * (double)__builtin_amdgcn_exp2f((st.max - m) * c) : 0.0);
+        if (lane == 0) {
+            s_max[which][i] = m;
+            s_sum[which][i] = sum;
+            if (GREEDY) s_arg[i] = arg;
+        }
+    }
+    __syncthreads();
+    // tokens under their parents' rows
+    for (int j = tid + 1; j < count; j += WALK_THREADS) {
+        const int parent = s_parent[j], x = a.tokens[row0 + j];
+        float p = 0.f, q = 1.f;
+        if (parent >= 0 && x >= 0 && x < a.V) {
+            if constexpr (GREEDY) {
+                p = x == s_arg[parent] ? 1.f : 0.f;
+            } else {
+                p = (float)((double)__builtin_amdgcn_exp2f((entry(static_cast<const T*>(a.logits) + (row0 + parent) * a.V + x) - s_max[0][parent]) * a.c) / s_sum[0][parent]);
+                if (draft)
+                    q = (float)((double)__builtin_amdgcn_exp2f((entry(static_cast<const T*>(a.draft) + (row0 + parent) * a.V + x) - s_max[1][parent]) * a.draft_c) / s_sum[1][parent]);
+            }
+        }
+        if (a.chances) a.chances[row0 + j] = draft && q > 0.f ? fminf(1.f, p / q) : draft && p > 0.f ? 1.f : fminf(1.f, p);
+        // a token that an earlier child of the same parent has is no longer there when it is tried
+        bool again = false;
+        if (!draft && !GREEDY && parent >= 0)
+            for (int i = parent + 1; i < j; ++i) again = again || (s_parent[i] == parent && a.tokens[row0 + i] == x);
+        s_p[j] = again ? 0.f : p;
+        s_q[j] = q;
+    }
+    __syncthreads();
+    if (wave) return;
+    // children have higher numbers than their parent and are tried in order, so one pass over the tokens meets all of them
+    int now = 0, steps = 0;
+    float left = 1.f;       // of p, behind the children that fell
+    if (count > 0)
+        for (int j0 = 0; j0 < count; j0 += 64) {
+            const int j = j0 + lane;
+            const bool there = j > 0 && j < count;
+            const int parent = there ? s_parent[j] : -1, x = there ? a.tokens[row0 + j] : -1;
+            const float p = there ? s_p[j] : 0.f, q = there ? s_q[j] : 1.f;
+            const float u = there && !GREEDY ? a.uniforms[(row0 + j) * 2] : 0.f;
+            int from = j0;
+            for (;;) {
+                const uint64_t tried = __builtin_amdgcn_ballot_w64(there && parent == now && j >= from);
+                if (tried == 0) break;
+                const int l = __builtin_ctzll(tried);
+                const float p_j = __shfl(p, l), q_j = __shfl(q, l), u_j = __shfl(u, l);
+                from = j0 + l + 1;
+                const bool stands = GREEDY ? p_j > 0.f : u_j * q_j * left < p_j;
+                if (stands) {
+                    now = j0 + l;
+                    if (lane == l) {
+                        a.emitted[row0 + steps] = x;
+                        a.path[row0 + steps + 1] = j;
+                    }
+                    ++steps;
+                    left = 1.f;
+                } else {
+                    left -= p_j;
+                }
+            }
+        }
+    // (each entry has one writer: this wavefront, and for the token drawn last the last launch)
+    for (int j = lane; j < a.B; j += 64) {
+        if (count == 0 || j > steps) a.path[row0 + j] = a.emitted[row0 + j] = -1;
+        else if (j == 0) a.path[row0] = 0;
+    }
+    if (lane == 0) {
+        a.n_path[n] = count > 0 ? steps + 1 : 0;
+        if constexpr (GREEDY) {
+            if (count > 0) a.emitted[row0 + steps] = s_arg[now];
+        } else {
+            Stop st;
+            st.token = count > 0 ? now : -1;
+            st.n_path = steps + 1;
+            st.max = count > 0 ? s_max[0][now] : 0.f;
+            st.draft_max = draft && now + 1 < count ? s_max[1][now] : 0.f;
+            a.stops[n] = st;
+        }
+    }
+}
+
+// ---- weigh -------------------------------------------------------------------------------------------------------------
+// What the last token is drawn from.  CHOSEN: p without the children of the token where the walk ended; else max(p - q, 0) (its
+// only child fell), or p where it had none.
+template <typename T>
+struct Weights {
+    const T* p;
+    const T* q;                 // or nullptr
+    double p_max, q_max, p_c, q_c, p_scale, q_scale;
+    int token, count, n;
+
+    __device__ __forceinline__ double of_p(int v) const { return exp2(((double)entry(p + v) - p_max) * p_c); }
+    __device__ __forceinline__ double of_q(int v) const { return exp2(((double)entry(q + v) - q_max) * q_c); }
+    __device__ __forceinline__ double left(int v) const { return fmax(of_p(v) * p_scale - of_q(v) * q_scale, 0.0); }
+};
+template <typename T>
+__device__ __forceinline__ Weights<T> weights(const Args& a, int n, const Stop& st)
+{
+    Weights<T> w;
+    const int count = count_of(a, n);
+    const long long row = ((long long)n * a.B + st.token) * a.V;
+    w.p = static_cast<const T*>(a.logits) + row;
+    w.q = a.draft && st.token + 1 < count ? static_cast<const T*>(a.draft) + row : nullptr;
+    w.p_max = st.max;
+    w.q_max = st.draft_max;
+    w.p_c = a.c64;
+    w.q_c = a.draft_c64;
+    w.p_scale = w.q_scale = 1.0;
+    w.token = st.token;
+    w.count = count;
+    w.n = n;
+    return w;
+}
+// ids of the children of the token where the walk ended; all threads of the workgroup call it
+__device__ __forceinline__ int list_children(const Args& a, int n, int token, int count, int* list, int* size)
+{
+    if (threadIdx.x == 0) *size = 0;
+    __syncthreads();
+    if (!a.draft)
+        for (int j = token + 1 + threadIdx.x; j < count; j += blockDim.x)
+            if (parent_at(a, n, j) == token) list[atomicAdd(size, 1)] = a.tokens[(long long)n * a.B + j];      // (a set: its order means nothing)
+    __syncthreads();
+    return *size;
+}
+__device__ __forceinline__ bool is_listed(const int* list, int size, int v)
+{
+    bool hit = false;
+    for (int i = 0; i < size; ++i) hit = hit || list[i] == v;
+    return hit;
+}
+__device__ __forceinline__ double wg_sum(double x, double* scratch)
+{
+    x = wave_sum(x);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = x;
+    __syncthreads();
+    double s = 0.0;
+    for (int w = 0; w < (int)blockDim.x / 64; ++w) s += scratch[w];
+    return s;
+}
+__device__ __forceinline__ double row_sum(const double* pieces, int n) { return wave_sum((int)(threadIdx.x & 63) < n ? pieces[threadIdx.x & 63] : 0.0); }
+
+template <typename T, bool RESIDUE>
+__global__ __launch_bounds__(STAT_THREADS) void weigh_kernel(Args a)
+{
+    __shared__ int list[FDD_TREE_MAX];
+    __shared__ int size;
+    __shared__ double scratch[STAT_THREADS / 64];
+    const int piece = blockIdx.x % a.pieces, n = blockIdx.x / a.pieces;
+    const Stop st = a.stops[n];
+    if (st.token < 0) return;
+    Weights<T> w = weights<T>(a, n, st);
+    const int children = RESIDUE ? 0 : list_children(a, n, st.token, w.count, list, &size);
+    const int v0 = piece * a.per_piece, v1 = min(v0 + a.per_piece, a.V);
+    const long long np = (long long)a.N * a.pieces, at = (long long)n * a.pieces + piece;
+    double all = 0.0, left = 0.0, other = 0.0;
+    if constexpr (RESIDUE) {
+        if (!w.q) return;
+        w.p_scale = 1.0 / row_sum(a.sums + n * a.pieces, a.pieces);
+        w.q_scale = 1.0 / row_sum(a.sums + 2 * np + n * a.pieces, a.pieces);
+        for (int v = v0 + threadIdx.x; v < v1; v += STAT_THREADS) left += w.left(v);
+    } else {
+        for (int v = v0 + threadIdx.x; v < v1; v += STAT_THREADS) {
+            const double e = w.of_p(v);
+            all += e;
+            left += is_listed(list, children, v) ? 0.0 : e;
+            if (w.q) other += w.of_q(v);
+        }
+    }
+    left = wg_sum(left, scratch);
+    if constexpr (!RESIDUE) {
+        all = wg_sum(all, scratch);
+        other = wg_sum(other, scratch);
+    }
+    if (threadIdx.x == 0) {
+        a.sums[np + at] = left;
+        if constexpr (!RESIDUE) {
+            a.sums[at] = all;
+            if (w.q) a.sums[2 * np + at] = other;
+        }
+    }
+}
+
+// ---- pick --------------------------------------------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(STAT_THREADS) void pick_kernel(Args a)
+{
+    __shared__ int list[FDD_TREE_MAX];
+    __shared__ int size, s_thread, s_last;
+    __shared__ double s_part[STAT_THREADS], s_target;
+    const int n = blockIdx.x, tid = threadIdx.x;
+    const Stop st = a.stops[n];
+    if (st.token < 0) return;
+    Weights<T> w = weights<T>(a, n, st);
+    int children = list_children(a, n, st.token, w.count, list, &size);
+    const long long np = (long long)a.N * a.pieces;
+    const double* const p_sums = a.sums + (long long)n * a.pieces;
+    const double* sums = p_sums + np;
+    const double all = row_sum(p_sums, a.pieces);
+    bool residue = w.q != nullptr;
+    if (residue) {
+        w.p_scale = 1.0 / all;
+        w.q_scale = 1.0 / row_sum(p_sums + 2 * np, a.pieces);
+    }
+    double total = row_sum(sums, a.pieces);
+    if (total < NOTHING_LEFT * (residue ? 1.0 : all)) {       // the drafts account for all of p
+        residue = false;
+        children = 0;
+        w.p_scale = 1.0;
+        sums = p_sums;
+        total = all;
+    }
+    // the piece: the first whose end lies above the target, or the last one with any weight
+    double target = (double)a.uniforms[((long long)n * a.B + st.token) * 2 + 1] * total;
+    int piece = 0;
+    double before = 0.0, at = 0.0;
+    bool found = false;
+    for (int i = 0; i < a.pieces && !found; ++i) {
+        const double s = sums[i];
+        if (s > 0.0) {
+            piece = i;
+            before = at;
+            found = at + s > target;
+        }
+        at += s;
+    }
+    target -= before;
+    const int v0 = piece * a.per_piece, v1 = min(v0 + a.per_piece, a.V);
+    const int each = (v1 - v0 + STAT_THREADS - 1) / STAT_THREADS;
+    const int b0 = min(v0 + tid * each, v1), b1 = min(b0 + each, v1);
+    auto weight = [&](int v) { return residue ? w.left(v) : is_listed(list, children, v) ? 0.0 : w.of_p(v) * w.p_scale; };
+    double mine = 0.0;
+    for (int v = b0; v < b1; ++v) mine += weight(v);
+    s_part[tid] = mine;
+    if (tid == 0) s_thread = -1, s_last = v0;
+    __syncthreads();
+    if (tid == 0) {
+        double sum = 0.0;
+        int last = 0;
+        for (int t = 0; t < STAT_THREADS; ++t) {
+            if (s_part[t] > 0.0) {
+                last = t;
+                s_target = target - sum;
+                if (sum + s_part[t] > target) break;
+            }
+            sum += s_part[t];
+        }
+        s_thread = last;
+    }
+    __syncthreads();
+    if (tid != s_thread) return;
+    double sum = 0.0;
+    int token = b0 < v1 ? b0 : v0;
+    for (int v = b0; v < b1; ++v) {
+        const double x = weight(v);
+        if (x > 0.0) token = v;
+        sum += x;
+        if (x > 0.0 && sum > s_target) break;
+    }
+    a.emitted[(long long)n * a.B + st.n_path - 1] = token;
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------------
+
+struct Plan {
+    int pieces, per_piece;
+    size_t stats, stops, sums;      // bytes
+};
+
+Plan make_plan(const fdd_tree_verify_params& p)
+{
+    const long long rows = (long long)p.N * p.B * (p.draft_logits ? 2 : 1);
+    long long pieces = (8ll * kNumCU + rows - 1) / rows;
+    const long long most = (p.V + 2047) / 2048;
+    if (pieces > most) pieces = most;
+    if (pieces > MAX_PIECES) pieces = MAX_PIECES;
+    if (pieces < 1) pieces = 1;
+    Plan pl;
+    pl.per_piece = (int)(((p.V + pieces - 1) / pieces + 7) / 8 * 8);
+    pl.pieces = (int)((p.V + pl.per_piece - 1) / pl.per_piece);
+    auto round = [](size_t x) { return (x + 255) & ~(size_t)255; };
+    pl.stats = round((size_t)rows * pl.pieces * sizeof(Stat));
+    pl.stops = round((size_t)p.N * sizeof(Stop));
+    pl.sums = round((size_t)3 * p.N * pl.pieces * sizeof(double));
+    return pl;
+}
+
+template <typename T>
+hipError_t launch(const Args& a, bool greedy, hipStream_t s)
+{
+    const dim3 stats((unsigned)((long long)a.N * a.B * a.pieces), a.draft ? 2u : 1u);
+    if (greedy) {
+        stats_kernel<T, true><<<stats, STAT_THREADS, 0, s>>>(a);
+        walk_kernel<T, true><<<dim3((unsigned)a.N), WALK_THREADS, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    const dim3 rows((unsigned)((long long)a.N * a.pieces));
+    stats_kernel<T, false><<<stats, STAT_THREADS, 0, s>>>(a);
+    walk_kernel<T, false><<<dim3((unsigned)a.N), WALK_THREADS, 0, s>>>(a);
+    weigh_kernel<T, false><<<rows, STAT_THREADS, 0, s>>>(a);
+    if (a.draft) weigh_kernel<T, true><<<rows, STAT_THREADS, 0, s>>>(a);
+    pick_kernel<T><<<dim3((unsigned)a.N), STAT_THREADS, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace tree_verify
+}  // namespace fdd
+
+using namespace fdd;
+using namespace fdd::tree_verify;
+
+#define fail set_error
+
+namespace {
+
+const char* const kFn = "fdd_tree_verify";
+
+bool in_range(float t) { return t >= 0x1p-20f && t <= 0x1p20f; }
+
+fdd_status check_shape(const fdd_tree_verify_params* p)
+{
+    if (!p) return fail(FDD_ERR_NULL, "%s: params is NULL", kFn);
+    if (p->N <= 0 || p->B <= 0 || p->V <= 0) return fail(FDD_ERR_SHAPE, "%s: N, B, V must be positive (got N=%d B=%d V=%lld)", kFn, p->N, p->B, (long long)p->V);
+    if (p->B > FDD_TREE_MAX) return fail(FDD_ERR_UNSUPPORTED, "%s: B=%d is above %d", kFn, p->B, FDD_TREE_MAX);
+    if (p->V >= (1ll << 31) - (1ll << 20)) return fail(FDD_ERR_SHAPE, "%s: V must be below 2^31 - 2^20", kFn);
+    if ((long long)p->N * p->B > (1ll << 24)) return fail(FDD_ERR_SHAPE, "%s: N*B too large", kFn);
+    if (p->dtype != FDD_F32 && p->dtype != FDD_BF16) return fail(FDD_ERR_DTYPE, "%s: dtype %d is neither FDD_F32 nor FDD_BF16", kFn, p->dtype);
+    if (p->reserved != 0) return fail(FDD_ERR_UNSUPPORTED, "%s: reserved field must be 0", kFn);
+    if (p->temperature != 0.f && !in_range(p->temperature)) return fail(FDD_ERR_UNSUPPORTED, "%s: temperature must be 0 (greedy) or from 2^-20 to 2^20", kFn);
+    if (p->draft_logits && !in_range(p->draft_temperature)) return fail(FDD_ERR_UNSUPPORTED, "%s: draft_temperature must be from 2^-20 to 2^20", kFn);
+    return FDD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fdd_tree_verify_workspace(const fdd_tree_verify_params* p)
+{
+    if (check_shape(p) != FDD_OK) return 0;
+    const Plan pl = make_plan(*p);
+    return pl.stats + pl.stops + pl.sums;
+}
+
+fdd_status fdd_tree_verify(const fdd_tree_verify_params* p)
+{
+    const fdd_status st = check_shape(p);
+    if (st != FDD_OK) return st;
+    const bool greedy = p->temperature == 0.f;
+    if (!p->logits || !p->tokens || !p->path || !p->n_path || !p->emitted || (!greedy && !p->uniforms))
+        return fail(FDD_ERR_NULL, "%s: logits, tokens, path, n_path and emitted must not be NULL, nor uniforms where the temperature is not 0", kFn);
+    if (p->draft_logits && p->parents) return fail(FDD_ERR_UNSUPPORTED, "%s: draft_logits go with chains only (parents must be NULL)", kFn);
+    if (p->parents && p->parents_stride != 0 && (p->parents_stride < p->B || p->parents_stride > (1ll << 28)))
+        return fail(FDD_ERR_SHAPE, "%s: parents_stride=%lld must be 0, or at least B=%d and at most 2^28", kFn, (long long)p->parents_stride, p->B);
+    const uintptr_t es = (uintptr_t)dtype_bytes(p->dtype);
+    if (!aligned_to(p->logits, es) || !aligned_to(p->draft_logits, es)) return fail(FDD_ERR_UNSUPPORTED, "%s: logits must be aligned to their element type", kFn);
+    const void* lists[] = {p->tokens, p->parents, p->uniforms, p->n_tokens, p->path, p->n_path, p->emitted, p->chances};
+    for (const void* x : lists)
+        if (!aligned_to(x, 4)) return fail(FDD_ERR_UNSUPPORTED, "%s: arrays must be 4-byte aligned", kFn);
+    const Plan pl = make_plan(*p);
+    const size_t need = pl.stats + pl.stops + pl.sums;
+    if (!p->workspace) return fail(FDD_ERR_WORKSPACE, "%s: workspace is NULL, %zu bytes needed", kFn, need);
+    if (!aligned_to(p->workspace, 256)) return fail(FDD_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", kFn);
+    if (p->workspace_bytes < need) return fail(FDD_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", kFn, p->workspace_bytes, need);
+    Args a = {};
+    a.logits = p->logits; a.draft = greedy ? nullptr : p->draft_logits; a.tokens = p->tokens; a.parents = p->parents; a.parents_stride = p->parents_stride;
+    a.uniforms = p->uniforms; a.n_tokens = p->n_tokens; a.path = p->path; a.n_path = p->n_path; a.emitted = p->emitted; a.chances = p->chances;
+    char* const ws = static_cast<char*>(p->workspace);
+    a.stats = reinterpret_cast<Stat*>(ws);
+    a.stops = reinterpret_cast<Stop*>(ws + pl.stats);
+    a.sums = reinterpret_cast<double*>(ws + pl.stats + pl.stops);
+    a.N = p->N; a.B = p->B; a.V = (int)p->V; a.pieces = pl.pieces; a.per_piece = pl.per_piece;
+    if (!greedy) {
+        a.c64 = LOG2E / (double)p->temperature;
+        a.c = (float)a.c64;
+    }
+    if (a.draft) {
+        a.draft_c64 = LOG2E / (double)p->draft_temperature;
+        a.draft_c = (float)a.draft_c64;
+    }
+    const hipStream_t s = static_cast<hipStream_t>(p->stream);
+    const hipError_t e = p->dtype == FDD_BF16 ? launch<uint16_t>(a, greedy, s) : launch<float>(a, greedy, s);
+    if (e != hipSuccess) return fail(FDD_ERR_LAUNCH, "%s: launch failed: %s", kFn, hipGetErrorString(e));
+    return FDD_OK;
+}
+
+}  // extern "C"
