@@ -1,8 +1,8 @@
-// Arguments of the two calls of a denoise step, of a fork, and of the calls on a prefix cache in 8 bits and on log probabilities,
-// from tensors to the C structs of fdd.h.
+// Arguments of the two calls of a denoise step, of a fork, and of the calls on a prefix cache in 8 bits, on log probabilities, on a
+// paged cache and on trees of drafted tokens, from tensors to the C structs of fdd.h.
 //
-// Host code, a CPython module: `attn`, `unmask`, `quant`, `attn_quant` and `logprobs` check shapes, types and placement as binding.py does and fill the
-// struct at the given address.  They return True, or False (and set no exception) for anything that is not the ordinary
+// Host code, a CPython module: each function but `fork` checks shapes, types and placement as binding.py and paged.py do and fills the
+// struct at the given address.  It returns True, or False (and set no exception) for anything that is not the ordinary
 // case - a wrong shape, a tensor subclass, an active torch function mode - and binding.py's own checks then accept it or
 // raise their errors.  Nothing is kept between calls.  In Python a tensor property costs about 0.1 us, and a call reads
 // 40 to 60 of them: 2.3 us for attention, 4.5 us for unmasking, beside 2.5 us per kernel launch.
@@ -269,6 +269,207 @@ void fill_logprobs(fdd_logprob_params* p, PyObject* const* a)
     }
 }
 
+// ---- a paged cache and trees of drafted tokens -----------------------------------------------------------------------------
+
+struct AppendCall {
+    fdd_paged_cache cache;
+    fdd_paged_append_params p;
+    fdd_rope_table table;
+};
+
+struct PagedAttnCall {
+    fdd_paged_cache cache;
+    fdd_paged_attn_params p;
+};
+
+// a dense array of this type and shape, or nullptr for None
+template <typename P>
+P* shaped(const OnDevice& on, PyObject* o, at::ScalarType type, at::IntArrayRef shape)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = on(o);
+    need(t.scalar_type() == type && t.sizes() == shape);
+    return (P*)pointer(t);
+}
+
+// the same for each of N requests, or (without that dimension) one for all of them; the entries between requests
+template <typename P>
+P* per_request(const OnDevice& on, PyObject* o, at::ScalarType type, int64_t N, at::IntArrayRef tail, int64_t* stride)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = on(o);
+    const bool own = t.dim() == (int64_t)tail.size() + 1;
+    need(t.scalar_type() == type && (own ? t.size(0) == N && t.sizes().slice(1) == tail : t.sizes() == tail));
+    if (own) {
+        *stride = 1;
+        for (const int64_t x : tail) *stride *= x;
+    }
+    return (P*)pointer(t);
+}
+
+// rows [..,heads,D] that are evenly spaced over all dimensions in front: address, and the stride of rows (0: there is one)
+void* even_rows(const at::Tensor& t, int64_t* stride)
+{
+    const int64_t d = t.dim();
+    need(d >= 2 && t.is_cuda() && t.numel() > 0);
+    const int64_t H = t.size(d - 2), D = t.size(d - 1);
+    need((D == 1 || t.stride(d - 1) == 1) && (H == 1 || t.stride(d - 2) == D));
+    int64_t step = 0, rows = 1;
+    for (int64_t i = d - 3; i >= 0; --i) {
+        if (t.size(i) == 1) continue;
+        need(step == 0 || t.stride(i) == step * rows);
+        if (step == 0) step = t.stride(i);
+        rows *= t.size(i);
+    }
+    need(step == 0 || step >= H * D);
+    *stride = step;
+    return t.data_ptr();
+}
+
+void fill_table(fdd_rope_table* r, PyObject* o, const OnDevice& on)
+{
+    need(PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 3);
+    const at::Tensor& turns = on(PyTuple_GET_ITEM(o, 0));
+    need(turns.scalar_type() == at::kLong && turns.dim() == 1 && turns.numel() < (1 << 20));
+    r->turns = (decltype(r->turns))pointer(turns);
+    r->rot_dim = int32_of(2 * turns.numel());
+    const int interleaved = PyObject_IsTrue(PyTuple_GET_ITEM(o, 1));
+    need(interleaved >= 0);
+    r->interleaved = interleaved;
+    r->magnitude = float_of(PyTuple_GET_ITEM(o, 2));
+}
+
+void fill_paged(fdd_paged_cache* c, PyObject* o, const OnDevice& on)
+{
+    need(PyTuple_Check(o) && PyTuple_GET_SIZE(o) == 4);
+    const at::Tensor &k = on(PyTuple_GET_ITEM(o, 0)), &v = on(PyTuple_GET_ITEM(o, 1)), &table = on(PyTuple_GET_ITEM(o, 2)), &lens = on(PyTuple_GET_ITEM(o, 3));
+    need(k.dim() == 4 && v.sizes() == k.sizes() && v.scalar_type() == k.scalar_type());
+    need(table.dim() == 2 && table.scalar_type() == at::kInt && lens.dim() == 1 && lens.scalar_type() == at::kInt && lens.size(0) == table.size(0));
+    c->k = pointer(k); c->v = pointer(v);
+    c->page_table = (const int32_t*)pointer(table); c->lens = (const int32_t*)pointer(lens);
+    c->N = int32_of(table.size(0)); c->max_pages = int32_of(table.size(1));
+    c->pages = int32_of(k.size(0)); c->Hkv = int32_of(k.size(1)); c->page_size = int32_of(k.size(2)); c->D = int32_of(k.size(3));
+    c->dtype = (decltype(c->dtype))dtype_code(k);
+}
+
+// q, positions, table, k, out, k_out, inverse, device
+void fill_rope(fdd_rope_params* p, PyObject* const* a)
+{
+    const OnDevice on{int32_of(a[7])};
+    const at::Tensor &q = on(a[0]), &pos = on(a[1]), &out = on(a[4]);
+    need(q.dim() >= 2);
+    const int64_t lead = q.dim() - 2;
+    need(pos.scalar_type() == at::kInt && pos.sizes() == q.sizes().slice(0, lead));
+    p->rows = int32_of(pos.numel());
+    p->Hq = int32_of(q.size(lead)); p->D = int32_of(q.size(lead + 1));
+    p->dtype = (decltype(p->dtype))dtype_code(q);
+    const int inverse = PyObject_IsTrue(a[6]);
+    need(inverse >= 0);
+    p->flags = inverse ? FDD_ROPE_INVERSE : 0;
+    fill_table(&p->table, a[2], on);
+    p->positions = (const int32_t*)pointer(pos);
+    need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type());
+    p->q = even_rows(q, &p->q_stride);
+    p->q_out = even_rows(out, &p->q_out_stride);
+    if (a[3] == Py_None) {
+        need(a[5] == Py_None);
+        return;
+    }
+    const at::Tensor &k = on(a[3]), &k_out = on(a[5]);
+    need(k.dim() == q.dim() && k.sizes().slice(0, lead) == q.sizes().slice(0, lead) && k.size(lead + 1) == p->D && k.scalar_type() == q.scalar_type());
+    need(k_out.sizes() == k.sizes() && k_out.scalar_type() == k.scalar_type());
+    p->Hk = int32_of(k.size(lead));
+    p->k = even_rows(k, &p->k_stride);
+    p->k_out = even_rows(k_out, &p->k_out_stride);
+}
+
+// k, v, cache, table, positions, rows, n_rows, device
+void fill_append(AppendCall* c, PyObject* const* a)
+{
+    const OnDevice on{int32_of(a[7])};
+    const at::Tensor &k = on(a[0]), &v = on(a[1]);
+    fill_paged(&c->cache, a[2], on);
+    need(k.dim() == 4 && v.sizes() == k.sizes() && k.size(0) == c->cache.N && k.size(2) == c->cache.Hkv && k.size(3) == c->cache.D);
+    need(dtype_code(k) == c->cache.dtype && v.scalar_type() == k.scalar_type());
+    const int64_t N = k.size(0), B = k.size(1);
+    c->p.B = int32_of(B);
+    c->p.k = even_rows(k, &c->p.k_stride);
+    c->p.v = even_rows(v, &c->p.v_stride);
+    if (a[3] != Py_None) {
+        fill_table(&c->table, a[3], on);
+        c->p.rope = &c->table;
+    }
+    c->p.positions = shaped<const int32_t>(on, a[4], at::kInt, {N, B});
+    c->p.rows = shaped<const int32_t>(on, a[5], at::kInt, {N, B});
+    c->p.n_rows = shaped<const int32_t>(on, a[6], at::kInt, {N});
+}
+
+// parents, lens, n_tokens, mask, positions, device; the request's number is mask's
+void fill_tree_mask(fdd_tree_mask_params* p, PyObject* const* a)
+{
+    const OnDevice on{int32_of(a[5])};
+    const at::Tensor& mask = on(a[3]);
+    need(mask.dim() == 3);
+    const int64_t N = mask.size(0), B = mask.size(1);
+    p->N = int32_of(N); p->B = int32_of(B);
+    need(a[0] != Py_None && a[4] != Py_None);
+    p->parents = per_request<const int32_t>(on, a[0], at::kInt, N, {B}, &p->parents_stride);
+    p->lens = shaped<const int32_t>(on, a[1], at::kInt, {N});
+    p->n_tokens = shaped<const int32_t>(on, a[2], at::kInt, {N});
+    p->mask = shaped<uint64_t>(on, a[3], at::kLong, {N, B, (B + 63) / 64});
+    p->positions = shaped<int32_t>(on, a[4], at::kInt, {N, B});
+}
+
+// q, cache, block_k, block_v, mask, n_tokens, causal_block, max_len, scale, out, device
+void fill_paged_attn(PagedAttnCall* c, PyObject* const* a)
+{
+    const OnDevice on{int32_of(a[10])};
+    const at::Tensor &q = on(a[0]), &k = on(a[2]), &v = on(a[3]), &out = on(a[9]);
+    fill_paged(&c->cache, a[1], on);
+    fdd_paged_attn_params* const p = &c->p;
+    need(q.dim() == 4 && k.dim() == 4 && v.sizes() == k.sizes() && q.size(0) == c->cache.N && q.size(3) == c->cache.D);
+    const int64_t N = q.size(0), B = q.size(1);
+    need(k.size(0) == N && k.size(1) == B && k.size(2) == c->cache.Hkv && k.size(3) == c->cache.D);
+    need(dtype_code(q) == c->cache.dtype && k.scalar_type() == q.scalar_type() && v.scalar_type() == q.scalar_type());
+    need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type());
+    p->B = int32_of(B); p->Hq = int32_of(q.size(2));
+    const int causal = PyObject_IsTrue(a[6]);
+    need(causal >= 0);
+    p->flags = causal ? FDD_ATTN_CAUSAL_BLOCK : 0;
+    p->max_len = int32_of(a[7]);
+    p->scale = a[8] == Py_None ? 0.f : float_of(a[8]);
+    p->q = even_rows(q, &p->q_stride);
+    p->block_k = even_rows(k, &p->k_stride);
+    p->block_v = even_rows(v, &p->v_stride);
+    p->mask = per_request<const uint64_t>(on, a[4], at::kLong, N, {B, (B + 63) / 64}, &p->mask_stride);
+    p->n_tokens = shaped<const int32_t>(on, a[5], at::kInt, {N});
+    p->out = pointer(out);
+}
+
+// logits, tokens, uniforms, parents, draft_logits, n_tokens, temperature, draft_temperature, path, n_path, emitted, chances, device
+void fill_tree_verify(fdd_tree_verify_params* p, PyObject* const* a)
+{
+    const OnDevice on{int32_of(a[12])};
+    const at::Tensor& x = on(a[0]);
+    need(x.dim() == 3);
+    const int64_t N = x.size(0), B = x.size(1);
+    p->N = int32_of(N); p->B = int32_of(B); p->V = x.size(2);
+    p->dtype = (decltype(p->dtype))dtype_code(x);
+    p->temperature = float_of(a[6]);
+    p->draft_temperature = float_of(a[7]);
+    p->logits = pointer(x);
+    p->draft_logits = shaped<const void>(on, a[4], x.scalar_type(), x.sizes());
+    need(a[1] != Py_None && a[8] != Py_None && a[9] != Py_None && a[10] != Py_None && a[11] != Py_None);
+    p->tokens = shaped<const int32_t>(on, a[1], at::kInt, {N, B});
+    p->uniforms = shaped<const float>(on, a[2], at::kFloat, {N, B, 2});
+    p->parents = per_request<const int32_t>(on, a[3], at::kInt, N, {B}, &p->parents_stride);
+    p->n_tokens = shaped<const int32_t>(on, a[5], at::kInt, {N});
+    p->path = shaped<int32_t>(on, a[8], at::kInt, {N, B});
+    p->n_path = shaped<int32_t>(on, a[9], at::kInt, {N});
+    p->emitted = shaped<int32_t>(on, a[10], at::kInt, {N, B});
+    p->chances = shaped<float>(on, a[11], at::kFloat, {N, B});
+}
+
 // address of a zeroed struct, then the arguments
 template <typename P, int ARGS, void (*FILL)(P*, PyObject* const*)>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n)
@@ -323,6 +524,11 @@ PyMethodDef methods[] = {
     {"quant", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<QuantCall, 5, fill_quant>)), METH_FASTCALL, "fill an fdd_quant_cache and the fdd_quant_rows behind it"},
     {"attn_quant", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<AttnQuantCall, 15, fill_attn_quant>)), METH_FASTCALL, "fill an fdd_attn_params and the fdd_quant_cache behind it"},
     {"logprobs", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<fdd_logprob_params, 10, fill_logprobs>)), METH_FASTCALL, "fill an fdd_logprob_params"},
+    {"rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<fdd_rope_params, 8, fill_rope>)), METH_FASTCALL, "fill an fdd_rope_params"},
+    {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<AppendCall, 8, fill_append>)), METH_FASTCALL, "fill an fdd_paged_cache, the fdd_paged_append_params behind it and their table"},
+    {"tree_mask", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<fdd_tree_mask_params, 6, fill_tree_mask>)), METH_FASTCALL, "fill an fdd_tree_mask_params"},
+    {"paged_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<PagedAttnCall, 11, fill_paged_attn>)), METH_FASTCALL, "fill an fdd_paged_cache and the fdd_paged_attn_params behind it"},
+    {"tree_verify", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&call<fdd_tree_verify_params, 13, fill_tree_verify>)), METH_FASTCALL, "fill an fdd_tree_verify_params"},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
@@ -337,7 +543,12 @@ PyMODINIT_FUNC PyInit__marshal()
               PyModule_AddIntConstant(m, "unmask_bytes", sizeof(fdd_unmask_params)) < 0 ||
               PyModule_AddIntConstant(m, "quant_bytes", sizeof(QuantCall)) < 0 ||
               PyModule_AddIntConstant(m, "attn_quant_bytes", sizeof(AttnQuantCall)) < 0 ||
-              PyModule_AddIntConstant(m, "logprobs_bytes", sizeof(fdd_logprob_params)) < 0)) {
+              PyModule_AddIntConstant(m, "logprobs_bytes", sizeof(fdd_logprob_params)) < 0 ||
+              PyModule_AddIntConstant(m, "rope_bytes", sizeof(fdd_rope_params)) < 0 ||
+              PyModule_AddIntConstant(m, "append_bytes", sizeof(AppendCall)) < 0 ||
+              PyModule_AddIntConstant(m, "tree_mask_bytes", sizeof(fdd_tree_mask_params)) < 0 ||
+              PyModule_AddIntConstant(m, "paged_attn_bytes", sizeof(PagedAttnCall)) < 0 ||
+              PyModule_AddIntConstant(m, "tree_verify_bytes", sizeof(fdd_tree_verify_params)) < 0)) {
         Py_DECREF(m);
         return nullptr;
     }

@@ -5,8 +5,8 @@
 //     wavefront.  All of them use every tile of keys that the workgroup brings into LDS.
 //   * Keys come in tiles: those of the cache, then those of the request's own tokens.  How many a request has is known on the
 //     device only (lens, n_tokens): each workgroup works out for itself, from these two lists, how many tiles there are in
-//     all, how many of them a piece gets so that all pieces together are about as many as the chip takes at once, and which
-//     piece is its own (`find`).  A long request is cut into more pieces than a short one; the host only knows a bound.
+//     all, how many of them a piece gets so that all pieces together are as many as the chip takes at once, and which
+//     piece is its own (`Cutting`).  A long request is cut into more pieces than a short one; the host only knows a bound.
 //   * Scores are produced transposed, S^T = K Q^T, with 32x32 matrix instructions: each lane then owns one query row
 //     (lane % 32) and half of the keys, so that maximum and sum of the streaming softmax are in-lane reductions plus
 //     one exchange between the halves, and the same registers are the B operand of O^T += V^T P^T.
@@ -21,6 +21,7 @@
 #include <type_traits>
 
 #include "paged.h"
+#include "wave.h"
 
 namespace fdd {
 namespace paged_attn {
@@ -99,12 +100,7 @@ __device__ __forceinline__ Request request(const Cut& c, int n)
     return r;
 }
 
-__device__ __forceinline__ int wave_sum(int x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    return x;
-}
+__device__ __forceinline__ int wave_sum(int x) { return (int)wave_reduce((uint32_t)x, [](uint32_t p, uint32_t q) { return p + q; }); }
 __device__ __forceinline__ int wave_scan(int x, int lane)      // inclusive
 {
 #pragma unroll
@@ -115,58 +111,69 @@ __device__ __forceinline__ int wave_scan(int x, int lane)      // inclusive
     return x;
 }
 
-// Tiles per piece: all tiles of all M-tiles over the pieces aimed at
-template <typename C>
-__device__ __forceinline__ int tiles_per_piece(const Cut& c, int lane)
-{
-    int mine = 0;
-    for (int n = lane; n < c.N; n += 64) {
-        const Request r = request<C>(c, n);
-        mine += r.mtiles * r.tiles;
-    }
-    const int all = wave_sum(mine) * c.Hkv;
-    return max(MIN_TILES, (all + c.W - 1) / c.W);
-}
-
 struct Piece {
     int n, kh, mt, piece, pieces;      // n < 0: none
     int item;                          // its place among all
     Request r;
 };
-// The item-th piece of all; items of a request are ordered by (KV head, piece, M-tile), so that neighbours read the same keys.
-// `total`: of all requests (where item is none of them).
+
+// How all requests are cut.  Lane n holds request n of the first 64; others are read again where they are needed.
 template <typename C>
-__device__ __forceinline__ Piece find(const Cut& c, int lane, int per_piece, int item, int* total)
-{
-    int base = 0;
-    Piece p;
-    p.n = -1;
-    p.item = item;
-    for (int n0 = 0; n0 < c.N; n0 += 64) {
-        Request r = {0, 0, 0, 0};
-        if (n0 + lane < c.N) r = request<C>(c, n0 + lane);
-        const int pieces = (r.tiles + per_piece - 1) / per_piece;
-        const int items = c.Hkv * r.mtiles * pieces;
-        const int end = base + wave_scan(items, lane);
-        const uint64_t here = __builtin_amdgcn_ballot_w64(item >= end - items && item < end);
-        if (here) {
-            const int l = __builtin_ctzll(here);
-            auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
-            p.n = n0 + l;
-            p.r = {of(r.len), of(r.count), of(r.mtiles), of(r.tiles)};
-            p.pieces = of(pieces);
-            const int at = item - of(end - items);
-            const int rest = at / p.r.mtiles;
-            p.mt = at - rest * p.r.mtiles;
-            p.kh = rest / p.pieces;
-            p.piece = rest - p.kh * p.pieces;
-            return p;
+struct Cutting {
+    Request r;
+    int per_piece;      // tiles of a piece, at most
+
+    __device__ __forceinline__ int pieces_of(const Request& x) const { return (x.tiles + per_piece - 1) / per_piece; }
+    __device__ __forceinline__ int items_of(const Cut& c, const Request& x) const { return c.Hkv * x.mtiles * pieces_of(x); }
+    // Tiles of a piece: all tiles over the pieces aimed at.
+    __device__ __forceinline__ void set(const Cut& c, int lane)
+    {
+        r = {0, 0, 0, 0};
+        if (lane < c.N) r = request<C>(c, lane);
+        int tiles = r.mtiles * r.tiles;
+        for (int n = 64 + lane; n < c.N; n += 64) {
+            const Request x = request<C>(c, n);
+            tiles += x.mtiles * x.tiles;
         }
-        base = __builtin_amdgcn_readlane(end, 63);
+        const int all = wave_sum(tiles) * c.Hkv;
+        per_piece = max(MIN_TILES, __builtin_amdgcn_readfirstlane((all + c.W - 1) / c.W));
     }
-    *total = base;
-    return p;
-}
+    // The item-th piece.  Items of a request are ordered by (KV head, piece, M-tile).  Workgroups take them as they come, neighbours
+    // on different XCDs: with neighbours on one XCD, whose M-tiles then share keys in its L2, 16 requests of one token and up to
+    // 8192 rows took 54 us instead of 45, and 16 of 64 tokens and 16384 rows 310 instead of 301.
+    __device__ __forceinline__ Piece find(const Cut& c, int lane, int item) const
+    {
+        const int items0 = items_of(c, r), end0 = wave_scan(items0, lane);
+        Piece p;
+        p.n = -1;
+        p.item = item;
+        Request x = r;
+        int items = items0, end = end0;
+        for (int n0 = 0;;) {
+            const uint64_t here = __builtin_amdgcn_ballot_w64(item >= end - items && item < end);
+            if (here) {
+                const int l = __builtin_ctzll(here);
+                auto of = [&](int y) { return __builtin_amdgcn_readlane(y, l); };
+                p.n = n0 + l;
+                p.r = {of(x.len), of(x.count), of(x.mtiles), of(x.tiles)};
+                p.pieces = of(pieces_of(x));
+                const int in = item - of(end - items);
+                const int rest = in / p.r.mtiles;
+                p.mt = in - rest * p.r.mtiles;
+                p.kh = rest / p.pieces;
+                p.piece = rest - p.kh * p.pieces;
+                return p;
+            }
+            n0 += 64;
+            if (n0 >= c.N) return p;
+            const int base = __builtin_amdgcn_readlane(end, 63);
+            x = {0, 0, 0, 0};
+            if (n0 + lane < c.N) x = request<C>(c, n0 + lane);
+            items = items_of(c, x);
+            end = base + wave_scan(items, lane);
+        }
+    }
+};
 
 template <typename T, int D, int WAVES>
 struct Cfg {
@@ -196,9 +203,9 @@ __global__ __launch_bounds__(WAVES * 64) void attn_kernel(Args a)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
     // ---- this workgroup's piece --------------------------------------------------------------------------------------
-    const int per_piece = __builtin_amdgcn_readfirstlane(tiles_per_piece<C>(a.cut, lane));
-    int total = 0;
-    Piece p = find<C>(a.cut, lane, per_piece, (int)wg_id_x(), &total);
+    Cutting<C> cutting;
+    cutting.set(a.cut, lane);
+    const Piece p = cutting.find(a.cut, lane, (int)wg_id_x());
     if (p.n < 0) return;
     const int n = p.n, kh = p.kh, len = p.r.len, count = p.r.count;
     const int cache_tiles = (len + KT - 1) / KT;
@@ -430,7 +437,7 @@ __global__ __launch_bounds__(WAVES * 64) void attn_kernel(Args a)
                     *reinterpret_cast<f32x4*>(op + db * 32 + v4 * 8) = f32x4{x[0], x[1], x[2], x[3]};
                 }
             }
-    } else {
+    } else if (row_ok) {
         f32x4* const wo = reinterpret_cast<f32x4*>(a.ws_o) + ((long long)p.item * WAVES + wave) * (DB * 4 * 64) + lane;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -453,71 +460,96 @@ struct MergeArgs {
     int Hq, max_mt;
 };
 
-// One wavefront per (request, KV head, M-tile, its 32-row wavefront, two of its 16-byte columns): lane = as in the accumulators.
+// One wavefront per (request, KV head, M-tile, its 32-row wavefront, MERGE_COLS of its 16-byte columns): lane = as in the accumulators.
+// Bound by latency where pieces are many: UNROLL of them are on their way at a time.
+constexpr int MERGE_COLS = 2, UNROLL = 8;
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = Cfg<T, D, WAVES>;
-    constexpr int COLS = D / 8;      // 16-byte columns of a lane
+    constexpr int COLS = D / 8, GROUPS = COLS / MERGE_COLS;
     const int tid = thread_id_x(), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
-    const int job = __builtin_amdgcn_readfirstlane((int)wg_id_x() * 4 + (tid >> 6));
+    int job = __builtin_amdgcn_readfirstlane((int)wg_id_x() * 4 + (tid >> 6));
+    const int col0 = job % GROUPS * MERGE_COLS;
+    job /= GROUPS;
     const int wave = job % WAVES, mtile = job / WAVES;
     const int mt = mtile % a.max_mt, head = mtile / a.max_mt;
     const int n = head / a.cut.Hkv, kh = head - n * a.cut.Hkv;
     if (n >= a.cut.N) return;
-    const int per_piece = __builtin_amdgcn_readfirstlane(tiles_per_piece<C>(a.cut, lane));
-    int base = 0;
-    Request mine = {0, 0, 0, 0};
-    for (int n0 = 0; n0 <= n; n0 += 64) {
-        Request r = {0, 0, 0, 0};
-        if (n0 + lane < a.cut.N && n0 + lane <= n) r = request<C>(a.cut, n0 + lane);
-        const int items = n0 + lane < n ? a.cut.Hkv * r.mtiles * ((r.tiles + per_piece - 1) / per_piece) : 0;
-        base += wave_sum(items);
-        if (n < n0 + 64) {
-            const int l = n - n0;
-            mine = {__builtin_amdgcn_readlane(r.len, l), __builtin_amdgcn_readlane(r.count, l), __builtin_amdgcn_readlane(r.mtiles, l), __builtin_amdgcn_readlane(r.tiles, l)};
-        }
+    Cutting<C> cutting;
+    cutting.set(a.cut, lane);
+    int before = lane < n ? cutting.items_of(a.cut, cutting.r) : 0;
+    Request x = cutting.r;
+    for (int n0 = 64; n0 <= n; n0 += 64) {
+        x = {0, 0, 0, 0};
+        if (n0 + lane <= n) x = request<C>(a.cut, n0 + lane);
+        if (n0 + lane < n) before += cutting.items_of(a.cut, x);
     }
-    const int pieces = (mine.tiles + per_piece - 1) / per_piece;
+    const int base = wave_sum(before), l = n & 63;
+    const Request mine = {__builtin_amdgcn_readlane(x.len, l), __builtin_amdgcn_readlane(x.count, l), __builtin_amdgcn_readlane(x.mtiles, l),
+                          __builtin_amdgcn_readlane(x.tiles, l)};
+    const int pieces = cutting.pieces_of(mine);
     if (pieces <= 1 || mt >= mine.mtiles) return;
     const int row = (mt * WAVES + wave) * 32 + l32;
     const bool row_ok = row < mine.count * a.cut.G;
-    if (__builtin_amdgcn_ballot_w64(row_ok) == 0) return;
+    if (!row_ok) return;
     const int first = base + (kh * pieces) * mine.mtiles + mt;
-    float m = -INFINITY;
-    for (int i = 0; i < pieces; ++i) m = fmaxf(m, a.ws_ml[((long long)(first + i * mine.mtiles) * WAVES * 32 + wave * 32 + l32) * 2]);
-    float l = 0.f;
-    f32x4 x[COLS];
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2* const ml0 = reinterpret_cast<const f32x2*>(a.ws_ml) + ((long long)first * WAVES + wave) * 32 + l32;
+    const f32x4* const wo0 = reinterpret_cast<const f32x4*>(a.ws_o) + (((long long)first * WAVES + wave) * COLS + col0) * 64 + lane;
+    const long long ml_step = (long long)mine.mtiles * WAVES * 32, wo_step = (long long)mine.mtiles * WAVES * COLS * 64;
+    float m = -INFINITY, l_sum = 0.f;
+    f32x4 y[MERGE_COLS];
 #pragma unroll
-    for (int j = 0; j < COLS; ++j) x[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < pieces; ++i) {
-        const long long item = first + (long long)i * mine.mtiles;
-        const float* const ml = a.ws_ml + (item * WAVES * 32 + wave * 32 + l32) * 2;
-        const float w = ml[0] == -INFINITY ? 0.f : exp2_fast(ml[0] - m);
-        l = fmaf(w, ml[1], l);
-        const f32x4* const wo = reinterpret_cast<const f32x4*>(a.ws_o) + (item * WAVES + wave) * (COLS * 64) + lane;
+    for (int j = 0; j < MERGE_COLS; ++j) y[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < pieces; i += UNROLL) {
+        f32x2 ml[UNROLL];
+        f32x4 w[UNROLL][MERGE_COLS];
 #pragma unroll
-        for (int j = 0; j < COLS; ++j) {
-            const f32x4 y = wo[j * 64];
-            x[j] = f32x4{fmaf(w, y[0], x[j][0]), fmaf(w, y[1], x[j][1]), fmaf(w, y[2], x[j][2]), fmaf(w, y[3], x[j][3])};
+        for (int u = 0; u < UNROLL; ++u) {
+            const int at = min(i + u, pieces - 1);
+            ml[u] = ml0[at * ml_step];
+#pragma unroll
+            for (int j = 0; j < MERGE_COLS; ++j) w[u][j] = wo0[at * wo_step + j * 64];
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            if (i + u >= pieces) ml[u][0] = -INFINITY;
+            top = fmaxf(top, ml[u][0]);
+        }
+        const float ref = top == -INFINITY ? 0.f : top;
+        const float old = exp2_fast(m - ref);
+        m = top;
+        l_sum *= old;
+#pragma unroll
+        for (int j = 0; j < MERGE_COLS; ++j) y[j] = f32x4{y[j][0] * old, y[j][1] * old, y[j][2] * old, y[j][3] * old};
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const float f = exp2_fast(ml[u][0] - ref);
+            l_sum = fmaf(f, ml[u][1], l_sum);
+#pragma unroll
+            for (int j = 0; j < MERGE_COLS; ++j) {
+                const f32x4 z = w[u][j];
+                y[j] = f32x4{fmaf(f, z[0], y[j][0]), fmaf(f, z[1], y[j][1]), fmaf(f, z[2], y[j][2]), fmaf(f, z[3], y[j][3])};
+            }
         }
     }
-    if (!row_ok) return;
     const int token = row / a.cut.G, g = row - token * a.cut.G;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    T* const op = static_cast<T*>(a.out) + (((long long)n * a.cut.B + token) * a.Hq + kh * a.cut.G + g) * D + 4 * half;
+    const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;
+    T* const op = static_cast<T*>(a.out) + (((long long)n * a.cut.B + token) * a.Hq + kh * a.cut.G + g) * D + 4 * half + col0 * 8;
 #pragma unroll
-    for (int j = 0; j < COLS; ++j) {
-        float y[4];
+    for (int j = 0; j < MERGE_COLS; ++j) {
+        float z[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = l > 0.f ? x[j][e] * inv : 0.f;
+        for (int e = 0; e < 4; ++e) z[e] = l_sum > 0.f ? y[j][e] * inv : 0.f;
         if constexpr (std::is_same<T, float>::value) {
-            *reinterpret_cast<f32x4*>(op + j * 8) = f32x4{y[0], y[1], y[2], y[3]};
+            *reinterpret_cast<f32x4*>(op + j * 8) = f32x4{z[0], z[1], z[2], z[3]};
         } else {
             u32x2 w;
-            w[0] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[0]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[1]) << 16;
-            w[1] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[2]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)y[3]) << 16;
+            w[0] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)z[0]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)z[1]) << 16;
+            w[1] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)z[2]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)z[3]) << 16;
             *reinterpret_cast<u32x2*>(op + j * 8) = w;
         }
     }
@@ -570,7 +602,7 @@ hipError_t launch(const fdd_paged_cache& c, const fdd_paged_attn_params& p, cons
     e = hipGetLastError();
     if (e != hipSuccess || !pl.partials) return e;
     MergeArgs m = {a.cut, a.ws_o, a.ws_ml, p.out, p.Hq, pl.max_mt};
-    const long long jobs = (long long)c.N * c.Hkv * pl.max_mt * WAVES;
+    const long long jobs = (long long)c.N * c.Hkv * pl.max_mt * WAVES * (D / 8 / MERGE_COLS);
     merge_kernel<T, D, WAVES><<<dim3((unsigned)((jobs + 3) / 4)), 256, 0, s>>>(m);
     return hipGetLastError();
 }

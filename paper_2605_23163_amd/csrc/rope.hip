@@ -252,8 +252,9 @@ __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a)
     }
 }
 
-// One workgroup per request and 256 of its tokens.  A token's ancestors have ever lower numbers, so its words are finished one
-// after the other, from the last to the first.
+// One workgroup per request.  A token's ancestors: its own, and those of the one that a pointer names; the pointers' distances
+// double from round to round, so that ceil(log2 B) rounds reach every root (walking from parent to parent takes as many LDS
+// latencies as the tree is deep: 10.8 us for 64 trees of 256 tokens, 170 deep).  WORDS: of a token's bits.
 struct TreeArgs {
     const int32_t* parents;
     long long parents_stride;
@@ -261,32 +262,49 @@ struct TreeArgs {
     const int32_t* n_tokens;
     uint64_t* mask;
     int32_t* positions;
-    int B, words;
+    int B;
 };
 
-__global__ __launch_bounds__(THREADS) void tree_mask_kernel(TreeArgs a)
+template <int WORDS, int MAX_B>
+__global__ __launch_bounds__(MAX_B) void tree_mask_kernel(TreeArgs a)
 {
-    __shared__ int32_t parent[FDD_TREE_MAX];
-    const int n = blockIdx.x, i = blockIdx.y * THREADS + threadIdx.x;
+    __shared__ uint64_t bits[MAX_B][WORDS];
+    __shared__ int32_t jump[MAX_B];
+    const int n = blockIdx.x, i = threadIdx.x, words = (a.B + 63) >> 6;
     const int there = a.n_tokens ? min(a.n_tokens[n], a.B) : a.B;
-    for (int j = threadIdx.x; j < min(a.B, (int)(blockIdx.y + 1) * THREADS); j += THREADS) parent[j] = parent_of(j, a.parents[n * a.parents_stride + j]);
-    __syncthreads();
-    if (i >= a.B) return;
-    int at = i < there ? i : -1, steps = -1, w = a.words - 1;
-    uint64_t bits = 0;
-    uint64_t* const out = a.mask ? a.mask + ((long long)n * a.B + i) * a.words : nullptr;
-    while (w >= 0) {
-        if (at >= 0 && (at >> 6) == w) {
-            bits |= 1ull << (at & 63);
-            ++steps;
-            at = parent[at];
-        } else {
-            if (out) out[w] = bits;
-            bits = 0;
-            --w;
-        }
+    const bool mine = i < there;
+    int at = mine && i > 0 ? parent_of(i, a.parents[n * a.parents_stride + i]) : -1;
+    const int len = a.lens ? a.lens[n] : 0;
+    uint64_t b[WORDS];
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+        b[w] = mine && (i >> 6) == w ? 1ull << (i & 63) : 0ull;
+        bits[i][w] = b[w];
     }
-    if (a.positions) a.positions[(long long)n * a.B + i] = i < there ? (a.lens ? a.lens[n] : 0) + steps : 0;
+    jump[i] = at;
+    __syncthreads();
+    for (int far = 1; far < there; far *= 2) {
+        int next = -1;
+        if (at >= 0) {
+#pragma unroll
+            for (int w = 0; w < WORDS; ++w) b[w] |= bits[at][w];
+            next = jump[at];
+        }
+        at = next;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) bits[i][w] = b[w];
+        jump[i] = at;
+        __syncthreads();
+    }
+    if (i >= a.B) return;
+    int steps = -1;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+        steps += __builtin_popcountll(b[w]);
+        if (a.mask && w < words) a.mask[((long long)n * a.B + i) * words + w] = b[w];
+    }
+    if (a.positions) a.positions[(long long)n * a.B + i] = mine ? len + steps : 0;
 }
 
 }  // namespace
@@ -519,8 +537,14 @@ fdd_status fdd_tree_mask(const fdd_tree_mask_params* p)
     if (!aligned_to(p->parents, 4) || !aligned_to(p->lens, 4) || !aligned_to(p->n_tokens, 4) || !aligned_to(p->mask, 8) || !aligned_to(p->positions, 4))
         return fail(FDD_ERR_UNSUPPORTED, "%s: mask must be 8-byte aligned, the other arrays 4-byte aligned", fn);
     if ((long long)p->N * p->B >= (1ll << 31)) return fail(FDD_ERR_SHAPE, "%s: N*B too large", fn);
-    TreeArgs a = {p->parents, p->parents_stride, p->lens, p->n_tokens, p->mask, p->positions, p->B, (p->B + 63) / 64};
-    tree_mask_kernel<<<dim3((unsigned)p->N, (unsigned)((p->B + THREADS - 1) / THREADS)), THREADS, 0, static_cast<hipStream_t>(p->stream)>>>(a);
+    TreeArgs a = {p->parents, p->parents_stride, p->lens, p->n_tokens, p->mask, p->positions, p->B};
+    const dim3 grid((unsigned)p->N);
+    const hipStream_t s = static_cast<hipStream_t>(p->stream);
+    if (p->B <= 64) tree_mask_kernel<1, 64><<<grid, 64, 0, s>>>(a);
+    else if (p->B <= 128) tree_mask_kernel<2, 128><<<grid, 128, 0, s>>>(a);
+    else if (p->B <= 256) tree_mask_kernel<4, 256><<<grid, 256, 0, s>>>(a);
+    else if (p->B <= 512) tree_mask_kernel<8, 512><<<grid, 512, 0, s>>>(a);
+    else tree_mask_kernel<16, 1024><<<grid, 1024, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(FDD_ERR_LAUNCH, "%s: launch failed: %s", fn, hipGetErrorString(e));
     return FDD_OK;

@@ -16,12 +16,14 @@
 #include <cfloat>
 
 #include "paged.h"
+#include "wave.h"
 
 namespace fdd {
 namespace tree_verify {
 
 constexpr int MAX_PIECES = 64;          // a wavefront joins a row's
 constexpr int STAT_THREADS = 256, WALK_THREADS = 1024;
+constexpr int WP = 1024, PICK = 8;      // pieces of the row that is drawn from, at most; its entries that a thread looks at together
 constexpr double LOG2E = 1.4426950408889634074;
 constexpr double NOTHING_LEFT = 0x1p-40;
 
@@ -52,8 +54,9 @@ struct Args {
     float* chances;
     Stat* stats;            // [2][N*B][pieces]
     Stop* stops;            // [N]
-    double* sums;           // [3][N][pieces]: of p, of what is drawn from, of q
+    double* sums;           // [3][N][w_pieces]: of p, of what is drawn from, of q
     int N, B, V, pieces, per_piece;       // per_piece: entries, a multiple of 8
+    int w_pieces, w_per;                  // of the row that is drawn from
     float c, draft_c;                     // log2(e) / temperature
     double c64, draft_c64;
 };
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(WALK_THREADS) void walk_kernel(Args a)
     __syncthreads();
     if (wave) return;
     // children have higher numbers than their parent and are tried in order, so one pass over the tokens meets all of them
-    int now = 0, steps = 0;
+    int now = 0, steps = 0;        // (uniform)
     float left = 1.f;       // of p, behind the children that fell
     if (count > 0)
         for (int j0 = 0; j0 < count; j0 += 64) {
@@ -249,7 +252,8 @@ __global__ __launch_bounds__(WALK_THREADS) void walk_kernel(Args a)
                 const uint64_t tried = __builtin_amdgcn_ballot_w64(there && parent == now && j >= from);
                 if (tried == 0) break;
                 const int l = __builtin_ctzll(tried);
-                const float p_j = __shfl(p, l), q_j = __shfl(q, l), u_j = __shfl(u, l);
+                auto of = [&](float y) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, y), l)); };
+                const float p_j = of(p), q_j = of(q), u_j = of(u);
                 from = j0 + l + 1;
                 const bool stands = GREEDY ? p_j > 0.f : u_j * q_j * left < p_j;
                 if (stands) {
@@ -341,10 +345,54 @@ __device__ __forceinline__ double wg_sum(double x, double* scratch)
     if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = x;
     __syncthreads();
     double s = 0.0;
-    for (int w = 0; w < (int)blockDim.x / 64; ++w) s += scratch[w];
+    for (int w = 0; w < STAT_THREADS / 64; ++w) s += scratch[w];
     return s;
 }
-__device__ __forceinline__ double row_sum(const double* pieces, int n) { return wave_sum((int)(threadIdx.x & 63) < n ? pieces[threadIdx.x & 63] : 0.0); }
+// sum of the threads before this one
+__device__ __forceinline__ double wg_before(double x, double* scratch)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double end = x;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const double y = __shfl_up(end, d);
+        if (lane >= d) end += y;
+    }
+    __syncthreads();
+    if (lane == 63) scratch[wave] = end;
+    __syncthreads();
+    double before = __shfl_up(end, 1);
+    if (lane == 0) before = 0.0;
+    for (int w = 0; w < STAT_THREADS / 64; ++w) before += w < wave ? scratch[w] : 0.0;
+    return before;
+}
+// lowest of the threads' first and highest of their second numbers.  (Of LDS atomics to one place the compiler makes a loop over the lanes:
+// two of them for each entry were 35 us of a call.)
+__device__ __forceinline__ void wg_first_last(int* first, int* last, int* scratch)
+{
+    const int f = (int)wave_reduce((uint32_t)*first, [](uint32_t x, uint32_t y) { return (uint32_t)min((int)x, (int)y); });
+    const int l = (int)wave_reduce((uint32_t)*last, [](uint32_t x, uint32_t y) { return (uint32_t)max((int)x, (int)y); });
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+        scratch[threadIdx.x >> 6] = f;
+        scratch[STAT_THREADS / 64 + (threadIdx.x >> 6)] = l;
+    }
+    __syncthreads();
+    *first = scratch[0];
+    *last = scratch[STAT_THREADS / 64];
+    for (int w = 1; w < STAT_THREADS / 64; ++w) {
+        *first = min(*first, scratch[w]);
+        *last = max(*last, scratch[STAT_THREADS / 64 + w]);
+    }
+}
+// of a row's pieces; a thread has up to WP / STAT_THREADS that follow one another
+__device__ __forceinline__ double row_sum(const double* sums, int n, double* scratch)
+{
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < WP / STAT_THREADS; ++i) s += (int)threadIdx.x * (WP / STAT_THREADS) + i < n ? sums[threadIdx.x * (WP / STAT_THREADS) + i] : 0.0;
+    return wg_sum(s, scratch);
+}
 
 template <typename T, bool RESIDUE>
 __global__ __launch_bounds__(STAT_THREADS) void weigh_kernel(Args a)
@@ -352,18 +400,18 @@ __global__ __launch_bounds__(STAT_THREADS) void weigh_kernel(Args a)
     __shared__ int list[FDD_TREE_MAX];
     __shared__ int size;
     __shared__ double scratch[STAT_THREADS / 64];
-    const int piece = blockIdx.x % a.pieces, n = blockIdx.x / a.pieces;
+    const int piece = blockIdx.x % a.w_pieces, n = blockIdx.x / a.w_pieces;
     const Stop st = a.stops[n];
     if (st.token < 0) return;
     Weights<T> w = weights<T>(a, n, st);
+    if (RESIDUE && !w.q) return;
     const int children = RESIDUE ? 0 : list_children(a, n, st.token, w.count, list, &size);
-    const int v0 = piece * a.per_piece, v1 = min(v0 + a.per_piece, a.V);
-    const long long np = (long long)a.N * a.pieces, at = (long long)n * a.pieces + piece;
+    const int v0 = piece * a.w_per, v1 = min(v0 + a.w_per, a.V);
+    const long long np = (long long)a.N * a.w_pieces, at = (long long)n * a.w_pieces + piece;
     double all = 0.0, left = 0.0, other = 0.0;
     if constexpr (RESIDUE) {
-        if (!w.q) return;
-        w.p_scale = 1.0 / row_sum(a.sums + n * a.pieces, a.pieces);
-        w.q_scale = 1.0 / row_sum(a.sums + 2 * np + n * a.pieces, a.pieces);
+        w.p_scale = 1.0 / row_sum(a.sums + (long long)n * a.w_pieces, a.w_pieces, scratch);
+        w.q_scale = 1.0 / row_sum(a.sums + 2 * np + (long long)n * a.w_pieces, a.w_pieces, scratch);
         for (int v = v0 + threadIdx.x; v < v1; v += STAT_THREADS) left += w.left(v);
     } else {
         for (int v = v0 + threadIdx.x; v < v1; v += STAT_THREADS) {
@@ -391,24 +439,26 @@ __global__ __launch_bounds__(STAT_THREADS) void weigh_kernel(Args a)
 template <typename T>
 __global__ __launch_bounds__(STAT_THREADS) void pick_kernel(Args a)
 {
+    constexpr int EACH = WP / STAT_THREADS;
     __shared__ int list[FDD_TREE_MAX];
-    __shared__ int size, s_thread, s_last;
-    __shared__ double s_part[STAT_THREADS], s_target;
+    __shared__ int size, ends[2 * STAT_THREADS / 64];
+    __shared__ double scratch[STAT_THREADS / 64], s_target;
     const int n = blockIdx.x, tid = threadIdx.x;
     const Stop st = a.stops[n];
     if (st.token < 0) return;
     Weights<T> w = weights<T>(a, n, st);
-    int children = list_children(a, n, st.token, w.count, list, &size);
-    const long long np = (long long)a.N * a.pieces;
-    const double* const p_sums = a.sums + (long long)n * a.pieces;
+    const long long np = (long long)a.N * a.w_pieces;
+    const double* const p_sums = a.sums + (long long)n * a.w_pieces;
     const double* sums = p_sums + np;
-    const double all = row_sum(p_sums, a.pieces);
+    const float u = a.uniforms[((long long)n * a.B + st.token) * 2 + 1];
+    int children = list_children(a, n, st.token, w.count, list, &size);
+    const double all = row_sum(p_sums, a.w_pieces, scratch);
+    double total = row_sum(sums, a.w_pieces, scratch);
     bool residue = w.q != nullptr;
     if (residue) {
         w.p_scale = 1.0 / all;
-        w.q_scale = 1.0 / row_sum(p_sums + 2 * np, a.pieces);
+        w.q_scale = 1.0 / row_sum(p_sums + 2 * np, a.w_pieces, scratch);
     }
-    double total = row_sum(sums, a.pieces);
     if (total < NOTHING_LEFT * (residue ? 1.0 : all)) {       // the drafts account for all of p
         residue = false;
         children = 0;
@@ -416,60 +466,68 @@ __global__ __launch_bounds__(STAT_THREADS) void pick_kernel(Args a)
         sums = p_sums;
         total = all;
     }
-    // the piece: the first whose end lies above the target, or the last one with any weight
-    double target = (double)a.uniforms[((long long)n * a.B + st.token) * 2 + 1] * total;
-    int piece = 0;
-    double before = 0.0, at = 0.0;
-    bool found = false;
-    for (int i = 0; i < a.pieces && !found; ++i) {
-        const double s = sums[i];
-        if (s > 0.0) {
-            piece = i;
-            before = at;
-            found = at + s > target;
-        }
-        at += s;
+    // the piece: the first whose end lies above the target, or (by rounding) the last one with any weight
+    const double target = (double)u * total;
+    double part[EACH], mine = 0.0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        part[i] = tid * EACH + i < a.w_pieces ? sums[tid * EACH + i] : 0.0;
+        mine += part[i];
     }
-    target -= before;
-    const int v0 = piece * a.per_piece, v1 = min(v0 + a.per_piece, a.V);
-    const int each = (v1 - v0 + STAT_THREADS - 1) / STAT_THREADS;
-    const int b0 = min(v0 + tid * each, v1), b1 = min(b0 + each, v1);
-    auto weight = [&](int v) { return residue ? w.left(v) : is_listed(list, children, v) ? 0.0 : w.of_p(v) * w.p_scale; };
-    double mine = 0.0;
-    for (int v = b0; v < b1; ++v) mine += weight(v);
-    s_part[tid] = mine;
-    if (tid == 0) s_thread = -1, s_last = v0;
-    __syncthreads();
-    if (tid == 0) {
-        double sum = 0.0;
-        int last = 0;
-        for (int t = 0; t < STAT_THREADS; ++t) {
-            if (s_part[t] > 0.0) {
-                last = t;
-                s_target = target - sum;
-                if (sum + s_part[t] > target) break;
-            }
-            sum += s_part[t];
+    const double at = wg_before(mine, scratch);
+    int first = INT32_MAX, last = -1;
+    {
+        double end = at;
+        for (int i = 0; i < EACH; ++i) {
+            end += part[i];
+            if (!(part[i] > 0.0)) continue;
+            last = tid * EACH + i;
+            if (end > target) first = min(first, last);
         }
-        s_thread = last;
+    }
+    wg_first_last(&first, &last, ends);
+    const int piece = first != INT32_MAX ? first : max(last, 0);
+    if (tid == piece / EACH) {
+        double begin = at;
+        for (int i = 0; i < piece % EACH; ++i) begin += part[i];
+        s_target = target - begin;
     }
     __syncthreads();
-    if (tid != s_thread) return;
-    double sum = 0.0;
-    int token = b0 < v1 ? b0 : v0;
-    for (int v = b0; v < b1; ++v) {
-        const double x = weight(v);
-        if (x > 0.0) token = v;
-        sum += x;
-        if (x > 0.0 && sum > s_target) break;
+    double left = s_target;
+    last = -1;
+    // its entries, STAT_THREADS * PICK at a time
+    const int v0 = piece * a.w_per, v1 = min(v0 + a.w_per, a.V);
+    first = INT32_MAX;
+    for (int b = v0; b < v1; b += STAT_THREADS * PICK) {
+        double x[PICK], sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < PICK; ++i) {
+            const int v = b + tid * PICK + i;
+            x[i] = v >= v1 ? 0.0 : residue ? w.left(v) : is_listed(list, children, v) ? 0.0 : w.of_p(v);
+            sum += x[i];
+        }
+        double end = wg_before(sum, scratch);
+        int from = INT32_MAX, to = last;
+#pragma unroll
+        for (int i = 0; i < PICK; ++i) {
+            end += x[i];
+            if (!(x[i] > 0.0)) continue;
+            to = b + tid * PICK + i;
+            if (end > left) from = min(from, to);
+        }
+        wg_first_last(&from, &to, ends);
+        first = from;
+        last = to;
+        if (first != INT32_MAX) break;
+        left -= wg_sum(sum, scratch);
     }
-    a.emitted[(long long)n * a.B + st.n_path - 1] = token;
+    if (tid == 0) a.emitted[(long long)n * a.B + st.n_path - 1] = first != INT32_MAX ? first : last >= 0 ? last : v0;
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------------
 
 struct Plan {
-    int pieces, per_piece;
+    int pieces, per_piece, w_pieces, w_per;
     size_t stats, stops, sums;      // bytes
 };
 
@@ -487,7 +545,10 @@ Plan make_plan(const fdd_tree_verify_params& p)
     auto round = [](size_t x) { return (x + 255) & ~(size_t)255; };
     pl.stats = round((size_t)rows * pl.pieces * sizeof(Stat));
     pl.stops = round((size_t)p.N * sizeof(Stop));
-    pl.sums = round((size_t)3 * p.N * pl.pieces * sizeof(double));
+    constexpr int unit = STAT_THREADS * PICK;
+    pl.w_per = (int)(((p.V + WP - 1) / WP + unit - 1) / unit * unit);
+    pl.w_pieces = (int)((p.V + pl.w_per - 1) / pl.w_per);
+    pl.sums = round((size_t)3 * p.N * pl.w_pieces * sizeof(double));
     return pl;
 }
 
@@ -500,7 +561,7 @@ hipError_t launch(const Args& a, bool greedy, hipStream_t s)
         walk_kernel<T, true><<<dim3((unsigned)a.N), WALK_THREADS, 0, s>>>(a);
         return hipGetLastError();
     }
-    const dim3 rows((unsigned)((long long)a.N * a.pieces));
+    const dim3 rows((unsigned)((long long)a.N * a.w_pieces));
     stats_kernel<T, false><<<stats, STAT_THREADS, 0, s>>>(a);
     walk_kernel<T, false><<<dim3((unsigned)a.N), WALK_THREADS, 0, s>>>(a);
     weigh_kernel<T, false><<<rows, STAT_THREADS, 0, s>>>(a);
@@ -576,6 +637,7 @@ fdd_status fdd_tree_verify(const fdd_tree_verify_params* p)
     a.stops = reinterpret_cast<Stop*>(ws + pl.stats);
     a.sums = reinterpret_cast<double*>(ws + pl.stats + pl.stops);
     a.N = p->N; a.B = p->B; a.V = (int)p->V; a.pieces = pl.pieces; a.per_piece = pl.per_piece;
+    a.w_pieces = pl.w_pieces; a.w_per = pl.w_per;
     if (!greedy) {
         a.c64 = LOG2E / (double)p->temperature;
         a.c = (float)a.c64;

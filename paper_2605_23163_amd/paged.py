@@ -60,6 +60,29 @@ class TreeVerifyParams(C.Structure):
                 ("workspace_bytes", C.c_size_t), ("stream", C.c_void_p)]
 
 
+class AppendCall(C.Structure):
+    _fields_ = [("cache", PagedCacheStruct), ("p", AppendParams), ("table", RopeTableStruct)]
+
+
+class PagedAttnCall(C.Structure):
+    _fields_ = [("cache", PagedCacheStruct), ("p", PagedAttnParams)]
+
+
+_BYTES = dict(rope_bytes=RopeParams, append_bytes=AppendCall, tree_mask_bytes=TreeMaskParams, paged_attn_bytes=PagedAttnCall, tree_verify_bytes=TreeVerifyParams)
+_APPEND_AT, _ATTN_AT = AppendCall.p.offset, PagedAttnCall.p.offset
+_fits = {}      # whether a module's structs are these
+
+
+def _marshal():
+    """The native argument marshalling, or None where it was not built, or from another header."""
+    m = _b._marshal
+    if m is None:
+        return None
+    if m not in _fits:
+        _fits[m] = all(getattr(m, name, None) == C.sizeof(t) for name, t in _BYTES.items())
+    return m if _fits[m] else None
+
+
 class PagedCache(NamedTuple):
     """K and V of N requests in pages: ``k``, ``v`` [pages,Hkv,page_size,D], ``page_table`` int32 [N,max_pages] and ``lens`` int32 [N],
     the rows that each request holds.  Both lists are read when a call runs."""
@@ -172,24 +195,33 @@ def fdd_rope(q, positions, table, k=None, out=None, k_out=None, inverse=False, s
     Returns the rotated q, or (q, k)."""
     lib = load_library()
     dev, handle = _device_and_stream(stream)
+    if k is None and k_out is not None:
+        raise ValueError("k_out needs k")
+    if out is None or (k is not None and k_out is None):
+        empty = lambda x: (_b.torch.empty if stream is None else _maker(stream, x.device, _b.torch.empty))(tuple(x.shape), dtype=x.dtype, device=x.device)
+        out = empty(q) if out is None else out
+        k_out = empty(k) if k is not None and k_out is None else k_out
+    p = RopeParams()
+    m = _marshal()
+    if m is None or not m.rope(C.addressof(p), q, positions, table, k, out, k_out, inverse, dev):
+        p = _rope_params(q, positions, table, k, out, k_out, inverse)
+    p.stream = handle
+    if p.rows:
+        _check(lib.fdd_rope(C.addressof(p)))
+    return out if k is None else (out, k_out)
+
+
+def _rope_params(q, positions, table, k, out, k_out, inverse):
     torch = _b.torch
     lead = tuple(q.shape[:-2])
     if positions.dtype != torch.int32 or tuple(positions.shape) != lead:
         raise TypeError(f"positions must be torch.int32 {list(lead)}")
-    if (k is None) and k_out is not None:
-        raise ValueError("k_out needs k")
-    pairs = [(q, out, "q")] + ([(k, k_out, "k")] if k is not None else [])
-    outs = []
-    for x, o, name in pairs:
-        if o is None:
-            new = torch.empty if stream is None else _maker(stream, x.device, torch.empty)
-            o = new(tuple(x.shape), dtype=x.dtype, device=x.device)
-        elif o.shape != x.shape or o.dtype != x.dtype:
+    for x, o, name in ((q, out, "q"), (k, k_out, "k")):
+        if x is not None and (o.shape != x.shape or o.dtype != x.dtype):
             raise ValueError(f"the output of {name} must have its shape and type")
-        outs.append(o)
     if k is not None and (k.dtype != q.dtype or k.shape[-1] != q.shape[-1]):
         raise TypeError("q and k must share element type and head size")
-    _on_current_device(q, k, positions, *outs)
+    _on_current_device(q, k, positions, out, k_out)
     p = RopeParams()
     rows = 1
     for n in lead:
@@ -198,15 +230,12 @@ def fdd_rope(q, positions, table, k=None, out=None, k_out=None, inverse=False, s
     p.table = _table_struct(table, p.D)
     p.positions = _dev(positions, "positions")
     p.q, p.q_stride = _rope_array(q, "q", lead)
-    p.q_out, p.q_out_stride = _rope_array(outs[0], "out", lead)
+    p.q_out, p.q_out_stride = _rope_array(out, "out", lead)
     if k is not None:
         p.Hk = k.shape[-2]
         p.k, p.k_stride = _rope_array(k, "k", lead)
-        p.k_out, p.k_out_stride = _rope_array(outs[1], "k_out", lead)
-    p.stream = handle
-    if rows:
-        _check(lib.fdd_rope(C.addressof(p)))
-    return outs[0] if k is None else (outs[0], outs[1])
+        p.k_out, p.k_out_stride = _rope_array(k_out, "k_out", lead)
+    return p
 
 
 def fdd_paged_cache(N, pages, page_size, max_pages, Hkv, D, dtype=None, device="cuda") -> PagedCache:
@@ -242,26 +271,34 @@ def fdd_paged_append(k, v, cache, table=None, positions=None, rows=None, n_rows=
     ``n_rows`` to it once every layer's call has been made."""
     lib = load_library()
     dev, handle = _device_and_stream(stream)
+    call = AppendCall()
+    m = _marshal()
+    if m is None or not m.append(C.addressof(call), k, v, cache, table, positions, rows, n_rows, dev):
+        call = AppendCall()
+        _append_params(call, k, v, cache, table, positions, rows, n_rows)
+    call.p.stream = handle
+    _check(lib.fdd_paged_append(C.addressof(call), C.addressof(call) + _APPEND_AT))
+
+
+def _append_params(call, k, v, cache, table, positions, rows, n_rows):
     torch = _b.torch
-    c = _cache_struct(cache)
+    c = call.cache = _cache_struct(cache)
     if k.dim() != 4:
         raise ValueError("k and v must be [N,B,Hkv,D]")
     B = k.shape[1]
     if k.dtype != v.dtype or _dtype_code(k) != c.dtype:
         raise TypeError("k and v must have the cache's element type")
     _on_current_device(k, v, positions, rows, n_rows)
-    p = AppendParams()
+    p = call.p
     p.B = B
     p.k, p.k_stride = _tokens(k, "k", (c.N, B, c.Hkv, c.D))
     p.v, p.v_stride = _tokens(v, "v", (c.N, B, c.Hkv, c.D))
     if table is not None:
-        t = _table_struct(table, c.D)
-        p.rope = C.addressof(t)
+        call.table = _table_struct(table, c.D)
+        p.rope = C.addressof(call.table)
     p.positions = _typed(positions, torch.int32, (c.N, B), "positions")
     p.rows = _typed(rows, torch.int32, (c.N, B), "rows")
     p.n_rows = _typed(n_rows, torch.int32, (c.N,), "n_rows")
-    p.stream = handle
-    _check(lib.fdd_paged_append(C.addressof(c), C.addressof(p)))
 
 
 def fdd_tree_mask(parents, lens=None, n_tokens=None, mask=None, positions=None, N=None, stream=None):
@@ -269,6 +306,12 @@ def fdd_tree_mask(parents, lens=None, n_tokens=None, mask=None, positions=None, 
     ``n_tokens`` or ``N`` to say how many).  Returns (mask int64 [N,B,ceil(B/64)], the bits of fdd_paged_attn's ``mask``, positions int32 [N,B])."""
     lib = load_library()
     dev, handle = _device_and_stream(stream)
+    p = TreeMaskParams()
+    m = _marshal()
+    if mask is not None and positions is not None and N is None and m is not None and m.tree_mask(C.addressof(p), parents, lens, n_tokens, mask, positions, dev):
+        p.stream = handle
+        _check(lib.fdd_tree_mask(C.addressof(p)))
+        return mask, positions
     torch = _b.torch
     if parents.dim() not in (1, 2):
         raise TypeError("parents must be torch.int32 [N,B] or [B]")
@@ -336,11 +379,16 @@ def fdd_paged_attn(q, cache, block_k, block_v, mask=None, n_tokens=None, causal_
     if out is None:
         make = torch.empty if n_tokens is None else torch.zeros
         out = (make if stream is None else _maker(stream, q.device, make))(tuple(q.shape), dtype=q.dtype, device=q.device)
-    p, c = _paged_attn_params(q, cache, block_k, block_v, mask, n_tokens, out, scale, causal_block, max_len)
+    call = PagedAttnCall()
+    m = _marshal()
+    if m is None or not m.paged_attn(C.addressof(call), q, cache, block_k, block_v, mask, n_tokens, causal_block, max_len, scale, out, dev):
+        call.p, call.cache = _paged_attn_params(q, cache, block_k, block_v, mask, n_tokens, out, scale, causal_block, max_len)
     _check_workspace(workspace, dev)
-    ws = _set_workspace(p, workspace, lambda _: lib.fdd_paged_attn_workspace(C.addressof(c), C.addressof(p)), q.device, stream)  # noqa: F841
+    at = C.addressof(call)
+    p = call.p
+    ws = _set_workspace(p, workspace, lambda _: lib.fdd_paged_attn_workspace(at, at + _ATTN_AT), q.device, stream)  # noqa: F841
     p.stream = handle
-    _check(lib.fdd_paged_attn(C.addressof(c), C.addressof(p)))
+    _check(lib.fdd_paged_attn(at, at + _ATTN_AT))
     return out
 
 
@@ -373,6 +421,20 @@ def fdd_tree_verify(logits, tokens, uniforms=None, parents=None, draft_logits=No
     Returns (path int32 [N,B], n_path int32 [N], emitted int32 [N,B], chances float32 [N,B])."""
     lib = load_library()
     dev, handle = _device_and_stream(stream)
+    m = _marshal()
+    p = TreeVerifyParams()
+    if path is None or n_path is None or emitted is None or chances is None or m is None or not m.tree_verify(
+            C.addressof(p), logits, tokens, uniforms, parents, draft_logits, n_tokens, temperature, draft_temperature, path, n_path, emitted, chances, dev):
+        p, path, n_path, emitted, chances = _verify_arguments(logits, tokens, uniforms, parents, draft_logits, n_tokens, temperature, draft_temperature, path,
+                                                              n_path, emitted, chances, stream)
+    _check_workspace(workspace, dev)
+    ws = _set_workspace(p, workspace, lambda _: lib.fdd_tree_verify_workspace(C.addressof(p)), logits.device, stream)  # noqa: F841
+    p.stream = handle
+    _check(lib.fdd_tree_verify(C.addressof(p)))
+    return path, n_path, emitted, chances
+
+
+def _verify_arguments(logits, tokens, uniforms, parents, draft_logits, n_tokens, temperature, draft_temperature, path, n_path, emitted, chances, stream):
     torch = _b.torch
     p = _verify_params(logits, draft_logits, temperature, draft_temperature)
     N, B = p.N, p.B
@@ -388,8 +450,4 @@ def fdd_tree_verify(logits, tokens, uniforms=None, parents=None, draft_logits=No
     p.n_tokens = _typed(n_tokens, torch.int32, (N,), "n_tokens")
     p.path, p.n_path = _typed(outs[0], torch.int32, (N, B), "path"), _typed(outs[1], torch.int32, (N,), "n_path")
     p.emitted, p.chances = _typed(outs[2], torch.int32, (N, B), "emitted"), _typed(outs[3], torch.float32, (N, B), "chances")
-    _check_workspace(workspace, dev)
-    ws = _set_workspace(p, workspace, lambda _: lib.fdd_tree_verify_workspace(C.addressof(p)), logits.device, stream)  # noqa: F841
-    p.stream = handle
-    _check(lib.fdd_tree_verify(C.addressof(p)))
-    return tuple(outs)
+    return (p, *outs)
