@@ -19,6 +19,7 @@
 //   * A request whose tiles are one piece is normalised and written at once; otherwise pieces leave fp32 sums and (m, l), which
 //     merge_kernel joins in the order of the pieces.
 #include <type_traits>
+#include <utility>
 
 #include "paged.h"
 #include "wave.h"
@@ -43,6 +44,7 @@ struct Cut {
     const int32_t* lens;
     const int32_t* n_tokens;
     int N, B, G, Hkv;
+    FastDiv dG;
     int max_len;        // longer requests are cut here
     int W;              // pieces aimed at
 };
@@ -79,10 +81,24 @@ __device__ __forceinline__ void wait_loads()      // until at most N of this wav
     static_assert(N >= 0 && N < 64, "counter range");
     __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
+// The order of the source across this point is the order of the instructions.
+#define SCHED_FENCE() __builtin_amdgcn_sched_barrier(0)
 __device__ __forceinline__ void wg_barrier() { asm volatile("s_barrier" ::: "memory"); }
 __device__ __forceinline__ i16x4 read_tr(const lds_i16x4* __restrict__ p)
 {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16(const_cast<lds_i16x4*>(p));
+}
+
+// f(J0), f(J0 + 1), .. f(J1 - 1) with compile-time arguments
+template <int J0, typename F, int... J>
+__device__ __forceinline__ void each_of(const F& f, std::integer_sequence<int, J...>)
+{
+    (f(std::integral_constant<int, J0 + J>()), ...);
+}
+template <int J0, int J1, typename F>
+__device__ __forceinline__ void each(const F& f)
+{
+    each_of<J0>(f, std::make_integer_sequence<int, J1 - J0>());
 }
 
 struct Request {
@@ -185,15 +201,17 @@ struct Cfg {
     static constexpr int CH = ROW / 16;                  // 16-byte pieces per row
     static constexpr int RPB = 1024 / ROW;               // rows per 1 KB piece
     static constexpr int RPL = ROW < 256 ? 256 / ROW : 1;      // rows per 256-byte bank line
+    static constexpr int SW = CH < 16 ? CH - 1 : 15;     // K's swizzle repeats after 16 rows or 16 bank lines
     static constexpr int NI = T_BYTES / 1024 / WAVES;    // pieces per wavefront, tile and operand
-    static constexpr int SLOTS = WAVES == 8 ? 3 : 2;
+    static constexpr int RUN = NI * RPB < 16 ? NI * RPB : 16;      // rows that are moved together: they lie in one page
+    static constexpr int SLOTS = WAVES == 8 ? (BF16 ? 4 : 3) : 2;      // of K and of V
     static constexpr int V_RING = SLOTS * T_BYTES;
     static constexpr int LDS = 2 * SLOTS * T_BYTES;
     static_assert(NI >= 1, "a tile has a piece for every wavefront");
 };
 
 template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void attn_kernel(Args a)
+__global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Args a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = Cfg<T, D, WAVES>;
@@ -209,9 +227,18 @@ __global__ __launch_bounds__(WAVES * 64) void attn_kernel(Args a)
     if (p.n < 0) return;
     const int n = p.n, kh = p.kh, len = p.r.len, count = p.r.count;
     const int cache_tiles = (len + KT - 1) / KT;
-    int t_begin = (int)((long long)p.r.tiles * p.piece / p.pieces), t_end = (int)((long long)p.r.tiles * (p.piece + 1) / p.pieces);
-    t_begin = __builtin_amdgcn_readfirstlane(t_begin);
-    t_end = __builtin_amdgcn_readfirstlane(t_end);
+    // page numbers, one a lane: of an even window of 64 pages and of an odd one
+    const int32_t* const table = a.table + (long long)n * a.max_pages;
+    auto window_at = [&](int w) { return table[min((w << 6) + lane, a.max_pages - 1)]; };
+    int t_begin, t_end;
+    {
+        const int each = p.r.tiles / p.pieces, more = p.r.tiles - each * p.pieces;
+        t_begin = __builtin_amdgcn_readfirstlane(each * p.piece + min(p.piece, more));
+        t_end = __builtin_amdgcn_readfirstlane(t_begin + each + (p.piece < more ? 1 : 0));
+    }
+    int window0 = (t_begin * KT >> a.page_shift) >> 6, window1 = window0;
+    int entries0 = window_at(window0), entries1 = entries0;
+    if (window0 & 1) window0 = -1; else window1 = -1;
 
     // ---- rows ----------------------------------------------------------------------------------------------------------
     const int G = a.cut.G, rows = count * G;
@@ -219,62 +246,12 @@ __global__ __launch_bounds__(WAVES * 64) void attn_kernel(Args a)
     const int row = row0 + wave * 32 + l32;
     const bool row_ok = row < rows;
     const int row_c = min(row, rows - 1);
-    const int token = row_c / G, g = row_c - token * G;
+    const int token = fast_div(row_c, a.cut.dG), g = row_c - token * G;
     if (a.causal) {      // keys behind the M-tile's last token are not seen
-        const int last = (min(row0 + WAVES * 32, rows) - 1) / G;
+        const int last = fast_div(min(row0 + WAVES * 32, rows) - 1, a.cut.dG);
         t_end = min(t_end, cache_tiles + last / KT + 1);
     }
-    const int W64 = (a.cut.B + 63) >> 6;
-    const uint64_t* const bits = a.mask ? a.mask + n * a.mask_stride + (long long)token * W64 : nullptr;
-
-    // ---- tiles: global memory -> LDS --------------------------------------------------------------------------------------
-    // page numbers of the next 64 pages, one a lane
-    const int32_t* const table = a.table + (long long)n * a.max_pages;
-    int window = -1, entries = 0;
-    auto page_at = [&](int index) -> int {
-        if ((index >> 6) != window) {
-            window = index >> 6;
-            entries = table[min((window << 6) + lane, a.max_pages - 1)];
-            entries = min(max(entries, 0), a.pages - 1);
-        }
-        return __builtin_amdgcn_readlane(entries, index & 63);
-    };
-    const uint32_t page_bytes = (uint32_t)C::ROW << a.page_shift;
-    const int page_mask = (1 << a.page_shift) - 1;
-    // chunk of row r that lands at 16-byte piece `at` of its place in LDS
-    auto k_chunk = [&](int at, int r) { return at ^ ((r / C::RPL) & (C::CH - 1)); };
-    auto v_chunk = [&](int at, int r) { return C::BF16 ? at ^ ((((r / C::RPL) & 3) << 2) & (C::CH - 1)) : at; };
-    const int lane_row = lane / C::CH, lane_at = lane % C::CH;
-    auto fetch = [&](int t, int slot) {
-        unsigned char* const dst = lds + slot * C::T_BYTES + wave * (C::NI * 1024);
-        if (t < cache_tiles) {
-#pragma unroll
-            for (int i = 0; i < C::NI; ++i) {
-                const int r0 = (wave * C::NI + i) * C::RPB, r = r0 + lane_row;
-                const int first = min(t * KT + r0, len - 1);      // (a piece behind the last row repeats it)
-                const int page = page_at(first >> a.page_shift);
-                const long long at = ((long long)page * a.cut.Hkv + kh) * page_bytes;
-                const uint32_t in_page = (uint32_t)(min(t * KT + r, len - 1) & page_mask) * C::ROW;
-                const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(a.k_pages)) + at, 0, page_bytes, RSRC_FLAGS);
-                const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(a.v_pages)) + at, 0, page_bytes, RSRC_FLAGS);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(dst + i * 1024), 16, in_page + k_chunk(lane_at, r) * 16, 0, 0, 0);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(dst + C::V_RING + i * 1024), 16, in_page + v_chunk(lane_at, r) * 16, 0, 0, 0);
-            }
-        } else {
-            const int key0 = (t - cache_tiles) * KT, last = count - 1 - key0;
-            const char* const kb = static_cast<const char*>(a.bk) + (((long long)n * a.cut.B + key0) * a.k_stride + kh * D) * (long long)sizeof(T);
-            const char* const vb = static_cast<const char*>(a.bv) + (((long long)n * a.cut.B + key0) * a.v_stride + kh * D) * (long long)sizeof(T);
-            const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(kb), 0, 0xffffffffu, RSRC_FLAGS);
-            const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vb), 0, 0xffffffffu, RSRC_FLAGS);
-#pragma unroll
-            for (int i = 0; i < C::NI; ++i) {
-                const int r = (wave * C::NI + i) * C::RPB + lane_row;
-                const uint32_t rr = (uint32_t)min(r, last);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void*)(dst + i * 1024), 16, rr * (uint32_t)a.k_stride * (uint32_t)sizeof(T) + k_chunk(lane_at, r) * 16, 0, 0, 0);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void*)(dst + C::V_RING + i * 1024), 16, rr * (uint32_t)a.v_stride * (uint32_t)sizeof(T) + v_chunk(lane_at, r) * 16, 0, 0, 0);
-            }
-        }
-    };
+    const uint64_t* const bits = a.mask ? a.mask + n * a.mask_stride + (long long)token * ((a.cut.B + 63) >> 6) : nullptr;
 
     // ---- queries: B operand of S^T = K Q^T --------------------------------------------------------------------------------
     constexpr int QF = D * (int)sizeof(T) / 32;       // 16-byte fragments of a lane: half of a row
@@ -284,6 +261,103 @@ __global__ __launch_bounds__(WAVES * 64) void attn_kernel(Args a)
 #pragma unroll
         for (int i = 0; i < QF; ++i) qf[i] = *reinterpret_cast<const u32x4*>(qp + i * 32);
     }
+    uint64_t bits0 = ~0ull;
+    if (bits) bits0 = bits[0];
+    // (they are here from now on: a first use behind the requests below would wait for the tiles on their way too)
+#pragma unroll
+    for (int i = 0; i < QF; ++i) asm volatile("" : "+v"(qf[i]));
+    asm volatile("" : "+v"(bits0));
+    auto in_pool = [&](int page) { return min(max(page, 0), a.pages - 1); };
+    entries0 = in_pool(entries0);
+    entries1 = in_pool(entries1);
+
+    // ---- tiles: global memory -> LDS --------------------------------------------------------------------------------------
+    auto page_at = [&](int index) __attribute__((always_inline)) -> int {
+        const int w = index >> 6;
+        if (w & 1) {
+            if (w != window1) {
+                window1 = w;
+                entries1 = in_pool(window_at(w));      // (used here: a wait behind the branch would be one for all tiles on their way, every time)
+            }
+            return __builtin_amdgcn_readlane(entries1, index & 63);
+        } else {
+            if (w != window0) {
+                window0 = w;
+                entries0 = in_pool(window_at(w));
+            }
+            return __builtin_amdgcn_readlane(entries0, index & 63);
+        }
+    };
+    constexpr int ROW_SHIFT = C::ROW == 512 ? 9 : C::ROW == 256 ? 8 : 7;
+    const uint32_t page_bytes = (uint32_t)C::ROW << a.page_shift;
+    auto page_base = [&](int page) { return (unsigned long long)((uint32_t)page * (uint32_t)a.cut.Hkv + (uint32_t)kh) << (a.page_shift + ROW_SHIFT); };
+    const int page_mask = (1 << a.page_shift) - 1;
+    const int row_w = wave * C::NI * C::RPB;          // first row of a tile that this wavefront moves
+    const int lane_row = row_w + lane / C::CH, lane_at = lane % C::CH;
+    // the 16-byte piece of row r that comes to lie at `lane_at`
+    auto k_from = [&](int r) { return lane_at ^ ((r / C::RPL) & C::SW); };
+    auto v_from = [&](int r) { return C::BF16 ? lane_at ^ ((((r / C::RPL) & 3) << 2) & (C::CH - 1)) : lane_at; };
+    // Offsets of this lane in a run of RUN rows, which lies in one page, less what the instruction's offset adds (1 KB a piece, to
+    // both sides).  They are the same for every run: the swizzles repeat after 16 rows, V's after a piece.
+    uint32_t k_voff[C::RUN / C::RPB];
+#pragma unroll
+    for (int i = 0; i < C::RUN / C::RPB; ++i) k_voff[i] = (uint32_t)((lane / C::CH) * C::ROW + k_from(lane_row + i * C::RPB) * 16);
+    const uint32_t v_voff = (uint32_t)((lane / C::CH) * C::ROW + v_from(lane_row) * 16);
+    // K or V of tile t, all of whose rows are there; `pages`: where its runs' pages lie in the pools
+    constexpr int RUNS = C::NI * C::RPB / C::RUN;
+    auto find_pages = [&](int t, unsigned long long (&pages)[RUNS]) __attribute__((always_inline)) {
+        each<0, RUNS>([&](auto run) __attribute__((always_inline)) {
+            constexpr int R0 = decltype(run)::value * C::RUN;
+            pages[decltype(run)::value] = page_base(page_at((t * KT + row_w + R0) >> a.page_shift));
+        });
+    };
+    auto fetch_full = [&](auto is_v, int t, int slot, const unsigned long long (&pages)[RUNS]) __attribute__((always_inline)) {
+        constexpr bool V = decltype(is_v)::value;
+        unsigned char* const dst = lds + (V ? C::V_RING : 0) + slot * C::T_BYTES + wave * (C::NI * 1024);
+        each<0, RUNS>([&](auto run) __attribute__((always_inline)) {
+            constexpr int R0 = decltype(run)::value * C::RUN;
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(V ? a.v_pages : a.k_pages)) + pages[decltype(run)::value], 0, page_bytes, RSRC_FLAGS);
+            const uint32_t in_page = (uint32_t)((t * KT + row_w + R0) & page_mask) * C::ROW;
+            each<0, C::RUN / C::RPB>([&](auto piece) __attribute__((always_inline)) {
+                constexpr int i = decltype(piece)::value;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(dst + R0 * C::ROW + i / 4 * 4096), 16, V ? v_voff : k_voff[i], in_page + i / 4 * 4096, i % 4 * 1024, 0);
+            });
+        });
+    };
+    // any tile
+    auto fetch = [&](auto is_v, int t, int slot) __attribute__((always_inline)) {
+        constexpr bool V = decltype(is_v)::value;
+        unsigned char* const dst = lds + (V ? C::V_RING : 0) + slot * C::T_BYTES + wave * (C::NI * 1024);
+        if ((t + 1) * KT <= len) {
+            unsigned long long pages[RUNS];
+            find_pages(t, pages);
+            fetch_full(is_v, t, slot, pages);
+            return;
+        }
+        // the last tile of the cache (what lies behind its last row is this row again), and the request's own tokens
+        const bool cache = t < cache_tiles;
+        const int key0 = cache ? t * KT : (t - cache_tiles) * KT, last = (cache ? len : count) - 1 - key0;
+        const long long stride = cache ? D : V ? a.v_stride : a.k_stride;
+#pragma unroll 1
+        for (int i = 0; i < C::NI; ++i) {
+            const char* base;
+            int from_row = 0;
+            if (cache) {      // (a piece lies in one page; one behind the last row is that row's)
+                const int first = min(row_w + i * C::RPB, last);
+                base = static_cast<const char*>(V ? a.v_pages : a.k_pages) + page_base(page_at((key0 + first) >> a.page_shift));
+                from_row = (key0 + first) & ~page_mask;
+            } else {
+                base = static_cast<const char*>(V ? a.bv : a.bk) + (((long long)n * a.cut.B + key0) * stride + kh * D) * (long long)sizeof(T);
+                from_row = key0;
+            }
+            const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, 0xffffffffu, RSRC_FLAGS);
+            const int r = lane_row + i * C::RPB;
+            const uint32_t at = (uint32_t)(key0 + min(r, last) - from_row) * (uint32_t)stride * (uint32_t)sizeof(T);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(dst + i * 1024), 16, at + (V ? v_from(r) : k_from(r)) * 16, 0, 0, 0);
+        }
+    };
+    const std::false_type is_k;
+    const std::true_type is_v;
 
     // ---- streaming softmax: one query row per lane ---------------------------------------------------------------------------
     f32x16 o[DB];
@@ -307,86 +381,212 @@ __global__ __launch_bounds__(WAVES * 64) void attn_kernel(Args a)
             limit = m == -INFINITY ? m : m + a.slack;
         }
     };
-
-    const int k_off = l32 * C::ROW, k_swz = (l32 / C::RPL) & (C::CH - 1);
-    int v_off[DB];
-    {
-        const int row_l = half * 4 + ((lane & 15) >> 2), x = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-        const int sw = (((row_l / C::RPL) & 3) << 2) & (C::CH - 1);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) v_off[db] = (row_l * C::ROW + ((x ^ sw) << 4) + (lane & 1) * 8) ^ (db << 6);
-    }
-
     constexpr int KB = KT / 32;
-    auto step = [&](int t, int slot) {
-        const unsigned char* const kt = lds + slot * C::T_BYTES;
-        const unsigned char* const vt = kt + C::V_RING;
-        f32x16 s[KB];
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
-#pragma unroll
-            for (int i = 0; i < QF; ++i) {
-                const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + kb * 32 * C::ROW + k_off + (((2 * i + half) ^ k_swz) << 4));
-                if constexpr (C::BF16) {
-                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]), s[kb], 0, 0, 0);
-                } else {
-                    const f32x4 kx = __builtin_bit_cast(f32x4, kf), qx = __builtin_bit_cast(f32x4, qf[i]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) s[kb] = __builtin_amdgcn_mfma_f32_32x32x2f32(kx[j], qx[j], s[kb], 0, 0, 0);
-                }
-            }
-        }
-        // keys that the row does not see
+    // keys of tile t that the row does not see: whether there are any, and their scores out of the way
+    auto is_masked = [&](int t) { return t >= cache_tiles || (t + 1) * KT > len; };
+    auto mask_scores = [&](int t, f32x16 (&s)[KB]) __attribute__((always_inline)) {
         const bool cache = t < cache_tiles;
         const int key0 = cache ? t * KT : (t - cache_tiles) * KT;
         const int valid = cache ? len - key0 : count - key0;
-        if (!cache || valid < KT) {
-            uint64_t see = valid >= 64 ? ~0ull : (1ull << valid) - 1;
-            if (!cache) {
-                if (bits) see &= bits[key0 >> 6] >> (key0 & 63);
-                else if (a.causal) see &= token - key0 >= 63 ? ~0ull : token < key0 ? 0ull : (2ull << (token - key0)) - 1;
-            }
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                const uint32_t w = (uint32_t)(see >> (32 * kb + 4 * half));
-#pragma unroll
-                for (int v = 0; v < 16; ++v) s[kb][v] = (w >> (8 * (v / 4) + v % 4)) & 1 ? s[kb][v] : -INFINITY;
-            }
+        uint64_t see = valid >= 64 ? ~0ull : (1ull << valid) - 1;
+        if (!cache) {
+            if (bits) see &= (key0 < 64 ? bits0 : bits[key0 >> 6]) >> (key0 & 63);
+            else if (a.causal) see &= token - key0 >= 63 ? ~0ull : token < key0 ? 0ull : (2ull << (token - key0)) - 1;
         }
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+            const uint32_t w = (uint32_t)(see >> (32 * kb + 4 * half));
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[kb][v] = (w >> (8 * (v / 4) + v % 4)) & 1 ? s[kb][v] : -INFINITY;
+        }
+    };
+    auto largest = [&](const f32x16 (&s)[KB]) __attribute__((always_inline)) {
         float mx = s[0][0];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
-        update_reference(mx);
-        const float mc = m_ref * a.c;
-        float sum = 0.f;
+        return mx;
+    };
+
+    // fragments: K's 16-byte piece 2 i + half of row l32 of a 32-key block; V's as the transposing reads take them
+    const int k_off = l32 * C::ROW, k_swz = (l32 / C::RPL) & C::SW;
+    constexpr int S = C::SLOTS;
+    if constexpr (C::BF16) {
+        // K runs a tile ahead of V: step t takes the exponentials of tile t while the matrix pipe works on the scores of t + 1,
+        // then on P V of t while the vector ALUs look for the maximum of t + 1.  Requested in step t: K of t + S, V of t + S - 1.
+        // (fragment i lies at the place of fragment 0 with i XORed in, as channels db of V do)
+        const int k_frag = k_off + ((half ^ k_swz) << 4);
+        int v_frag;
+        {
+            const int row_l = half * 4 + ((lane & 15) >> 2), x = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+            const int sw = (((row_l / C::RPL) & 3) << 2) & (C::CH - 1);
+            v_frag = C::V_RING + row_l * C::ROW + ((x ^ sw) << 4) + (lane & 1) * 8;
+        }
+        auto read_k = [&](int base, auto jc) __attribute__((always_inline)) {
+            constexpr int j = decltype(jc)::value;
+            return *reinterpret_cast<const bf16x8*>(lds + ((base + k_frag) ^ (j % QF << 5)) + j / QF * 32 * C::ROW);
+        };
+        auto read_v = [&](int base, auto jc) __attribute__((always_inline)) {      // 16-key step j / DB, channels j % DB
+            constexpr int j = decltype(jc)::value;
+            const unsigned char* const p0 = lds + ((base + v_frag) ^ (j % DB << 6)) + j / DB * 16 * C::ROW;
+            const i16x4 lo = read_tr((const lds_i16x4*)p0), hi = read_tr((const lds_i16x4*)(p0 + 8 * C::ROW));
+            typedef short i16x8 __attribute__((ext_vector_type(8)));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        constexpr int NQ = 2 * QF, NP = 4 * DB;      // matrix instructions of a tile's scores and of its P V
+        constexpr int AHEAD = 3;                     // fragments are read so far ahead
+        const int tiles = t_end - t_begin;
+        // Half tiles are requested in the order K0 V0 K1 V1 ..: `n` of them may still be on their way
+        auto wait_halves = [&](int n) {
+            constexpr int H = C::NI;
+            if (n >= 4 && 4 * H < 64) wait_loads<4 * H < 64 ? 4 * H : 0>();
+            else if (n >= 3 && 3 * H < 64) wait_loads<3 * H < 64 ? 3 * H : 0>();
+            else if (n >= 2) wait_loads<2 * H>();
+            else if (n == 1) wait_loads<H>();
+            else wait_loads<0>();
+        };
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+        for (int i = 0; i < S; ++i) {
+            if (i < tiles) fetch(is_k, t_begin + i, i);
+            if (i + 1 < S && i < tiles) fetch(is_v, t_begin + i, i);
+        }
+        // pages of the tile whose V is requested next in the steps that request whole tiles only
+        unsigned long long pages[RUNS];
+        // Step i: the probabilities of tile i (scores in s) and P V; scores of tile i + 1 into `to`.
+        auto step = [&](auto next, auto whole, int i, f32x16 (&s)[2], f32x16 (&to)[2]) __attribute__((always_inline)) {
+            constexpr bool NEXT = decltype(next)::value;
+            if constexpr (decltype(whole)::value) {      // everything that it touches and requests are whole tiles of the cache
+                wait_loads<(2 * S - 4) * C::NI>();
+                wg_barrier();
+                fetch_full(is_v, t_begin + i + S - 1, (i + S - 1) % S, pages);
+                find_pages(t_begin + i + S, pages);
+                fetch_full(is_k, t_begin + i + S, i % S, pages);
+            } else {
+                wait_halves(min(2 * (i + S) - 1, 2 * tiles) - min(2 * i + 3, 2 * tiles));       // V of tile i, K of tile i + 1 are there
+                wg_barrier();       // for everyone, and everyone is done with the slots that are requested now
+                if (i + S - 1 < tiles) fetch(is_v, t_begin + i + S - 1, (i + S - 1) % S);
+                if (i + S < tiles) fetch(is_k, t_begin + i + S, i % S);
+            }
+            const int k_base = (i + 1) % S * C::T_BYTES, v_base = i % S * C::T_BYTES;
+            const float mc = m_ref * a.c;
+            float sum = 0.f;
+            bf16x8 pf[4], f[AHEAD + 1];
+            auto read = [&](auto jc) __attribute__((always_inline)) {
+                constexpr int j = decltype(jc)::value;
+                if constexpr (j < NQ) return read_k(k_base, jc);
+                else return read_v(v_base, std::integral_constant<int, j - NQ>());
+            };
+            auto probability = [&](auto entry) __attribute__((always_inline)) {
+                constexpr int e = decltype(entry)::value;
+                const float x = exp2_fast(fmaf(s[e / 16][e % 16], a.c, -mc));
+                sum += x;
+                s[e / 16][e % 16] = x;
+                if constexpr (e & 1) {
+                    pf[e / 8][e % 8 - 1] = (__bf16)s[e / 16][e % 16 - 1];
+                    pf[e / 8][e % 8] = (__bf16)x;
+                }
+            };
+            constexpr int J0 = NEXT ? 0 : NQ;
+            if constexpr (!NEXT) each<0, 16>(probability);
+            each<J0, J0 + AHEAD>([&](auto jc) __attribute__((always_inline)) { f[decltype(jc)::value % (AHEAD + 1)] = read(jc); });
+            SCHED_FENCE();
+            float mx0 = -INFINITY, mx1 = -INFINITY;
+            each<J0, NQ + NP>([&](auto jc) __attribute__((always_inline)) {
+                constexpr int j = decltype(jc)::value;
+                if constexpr (j + AHEAD < NQ + NP) f[(j + AHEAD) % (AHEAD + 1)] = read(std::integral_constant<int, j + AHEAD>());
+                const bf16x8 x = f[j % (AHEAD + 1)];
+                if constexpr (j < NQ) {
+                    if constexpr (j % QF) to[j / QF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, qf[j % QF]), to[j / QF], 0, 0, 0);
+                    else to[j / QF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, qf[j % QF]), f32x16{}, 0, 0, 0);
+                    each<j * 16 / NQ, (j + 1) * 16 / NQ>(probability);
+                } else {
+                    constexpr int jj = j - NQ;
+                    o[jj % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pf[jj / DB], o[jj % DB], 0, 0, 0);
+                    if constexpr (jj < NP / 2) {
+                        each<16 + jj * 32 / NP, 16 + (jj + 1) * 32 / NP>(probability);
+                    } else if constexpr (NEXT) {
+                        each<(jj - NP / 2) * 32 / NP, (jj - NP / 2 + 1) * 32 / NP>([&](auto pair) __attribute__((always_inline)) {
+                            constexpr int e = 2 * decltype(pair)::value;
+                            if constexpr (e & 2) mx1 = fmaxf(mx1, fmaxf(to[e / 16][e % 16], to[e / 16][e % 16 + 1]));
+                            else mx0 = fmaxf(mx0, fmaxf(to[e / 16][e % 16], to[e / 16][e % 16 + 1]));
+                        });
+                    }
+                }
+                SCHED_FENCE();
+            });
+            l_run += sum;
+            if (NEXT) {
+                float mx = fmaxf(mx0, mx1);
+                if constexpr (!decltype(whole)::value)
+                    if (is_masked(t_begin + i + 1)) {
+                        mask_scores(t_begin + i + 1, to);
+                        mx = largest(to);
+                    }
+                update_reference(mx);
+            }
+        };
+        if (tiles > 0) {
+            f32x16 s0[2], s1[2];
+            wait_halves(min(2 * S - 1, 2 * tiles) - 1);      // K of the first tile
+            wg_barrier();
+            {
+                bf16x8 f[AHEAD + 1];
+                each<0, AHEAD>([&](auto jc) __attribute__((always_inline)) { f[decltype(jc)::value] = read_k(0, jc); });
+                each<0, NQ>([&](auto jc) __attribute__((always_inline)) {
+                    constexpr int j = decltype(jc)::value;
+                    if constexpr (j + AHEAD < NQ) f[(j + AHEAD) % (AHEAD + 1)] = read_k(0, std::integral_constant<int, j + AHEAD>());
+                    const bf16x8 x = f[j % (AHEAD + 1)], q = __builtin_bit_cast(bf16x8, qf[j % QF]);
+                    if constexpr (j % QF) s0[j / QF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q, s0[j / QF], 0, 0, 0);
+                    else s0[j / QF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q, f32x16{}, 0, 0, 0);
+                });
+            }
+            if (is_masked(t_begin)) mask_scores(t_begin, s0);
+            update_reference(largest(s0));
+            // (two steps a round: the scores change places without moves)
+            const std::true_type yes;
+            const std::false_type no;
+            int i = 0;
+            const int whole = min(t_end, len / KT) - t_begin - S;      // steps that request whole tiles
+            if (whole >= 2) find_pages(t_begin + S - 1, pages);
+            for (; i + 2 <= whole; i += 2) {
+                step(yes, yes, i, s0, s1);
+                step(yes, yes, i + 1, s1, s0);
+            }
+            for (; i + 2 < tiles; i += 2) {
+                step(yes, no, i, s0, s1);
+                step(yes, no, i + 1, s1, s0);
+            }
+            if (i + 1 < tiles) {
+                step(yes, no, i, s0, s1);
+                step(no, no, i + 1, s1, s0);
+            } else {
+                step(no, no, i, s0, s1);
+            }
+        }
+    } else {
+        auto step = [&](int t, int slot) {
+            const unsigned char* const kt = lds + slot * C::T_BYTES;
+            const unsigned char* const vt = kt + C::V_RING;
+            f32x16 s[1];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[0][v] = 0.f;
+#pragma unroll
+            for (int i = 0; i < QF; ++i) {
+                const f32x4 kx = *reinterpret_cast<const f32x4*>(kt + k_off + (((2 * i + half) ^ k_swz) << 4)), qx = __builtin_bit_cast(f32x4, qf[i]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kx[j], qx[j], s[0], 0, 0, 0);
+            }
+            if (is_masked(t)) mask_scores(t, s);
+            update_reference(largest(s));
+            const float mc = m_ref * a.c;
+            float sum = 0.f;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                s[kb][v] = exp2_fast(fmaf(s[kb][v], a.c, -mc));
-                sum += s[kb][v];
+                s[0][v] = exp2_fast(fmaf(s[0][v], a.c, -mc));
+                sum += s[0][v];
             }
-        l_run += sum;
-        if constexpr (C::BF16) {
-#pragma unroll
-            for (int t4 = 0; t4 < KT / 16; ++t4) {
-                bf16x8 pf;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) pf[e] = (__bf16)s[t4 / 2][(t4 & 1) * 8 + e];
-#pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    const unsigned char* const vp = vt + v_off[db] + t4 * 16 * C::ROW;
-                    const i16x4 lo = read_tr((const lds_i16x4*)vp), hi = read_tr((const lds_i16x4*)(vp + 8 * C::ROW));
-                    typedef short i16x8 __attribute__((ext_vector_type(8)));
-                    const i16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), pf, o[db], 0, 0, 0);
-                }
-            }
-        } else {
+            l_run += sum;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const unsigned char* const vp = vt + (8 * (v / 4) + 4 * half + v % 4) * C::ROW + l32 * 4;
@@ -394,25 +594,26 @@ __global__ __launch_bounds__(WAVES * 64) void attn_kernel(Args a)
                 for (int db = 0; db < DB; ++db)
                     o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(vp + db * 128), s[0][v], o[db], 0, 0, 0);
             }
+        };
+        constexpr int LOADS = 2 * C::NI;
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i)
+            if (t_begin + i < t_end) {
+                fetch(is_k, t_begin + i, i);
+                fetch(is_v, t_begin + i, i);
+            }
+        int slot = 0;
+        for (int t = t_begin; t < t_end; ++t) {
+            if (S == 3 && t + 1 < t_end) wait_loads<LOADS>();
+            else wait_loads<0>();
+            wg_barrier();       // the tile is there, and everyone is done with the slot that the next one goes to
+            if (t + S - 1 < t_end) {
+                fetch(is_k, t + S - 1, slot == 0 ? S - 1 : slot - 1);
+                fetch(is_v, t + S - 1, slot == 0 ? S - 1 : slot - 1);
+            }
+            step(t, slot);
+            slot = slot + 1 == S ? 0 : slot + 1;
         }
-    };
-
-    // ---- the piece's tiles -----------------------------------------------------------------------------------------------
-    constexpr int LOADS = 2 * C::NI;
-#pragma unroll
-    for (int i = 0; i < C::SLOTS - 1; ++i)
-        if (t_begin + i < t_end) fetch(t_begin + i, i);
-    // (the queries are here from now on: otherwise each step's first use of them waits for the tiles on their way too)
-#pragma unroll
-    for (int i = 0; i < QF; ++i) asm volatile("" : "+v"(qf[i]));
-    int slot = 0;
-    for (int t = t_begin; t < t_end; ++t) {
-        if (C::SLOTS == 3 && t + 1 < t_end) wait_loads<LOADS>();
-        else wait_loads<0>();
-        wg_barrier();       // the tile is there, and everyone is done with the slot that the next one goes to
-        if (t + C::SLOTS - 1 < t_end) fetch(t + C::SLOTS - 1, slot == 0 ? C::SLOTS - 1 : slot - 1);
-        step(t, slot);
-        slot = slot + 1 == C::SLOTS ? 0 : slot + 1;
     }
 
     // ---- out ---------------------------------------------------------------------------------------------------------------
@@ -588,7 +789,7 @@ Plan make_plan(const fdd_paged_cache& c, const fdd_paged_attn_params& p)
 
 Cut make_cut(const fdd_paged_cache& c, const fdd_paged_attn_params& p, const Plan& pl)
 {
-    return {c.lens, p.n_tokens, c.N, p.B, p.Hq / c.Hkv, c.Hkv, pl.max_len, pl.W};
+    return {c.lens, p.n_tokens, c.N, p.B, p.Hq / c.Hkv, c.Hkv, make_fastdiv((uint32_t)(p.Hq / c.Hkv)), pl.max_len, pl.W};
 }
 
 template <typename T, int D, int WAVES>

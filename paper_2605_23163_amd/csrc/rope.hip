@@ -325,7 +325,8 @@ fdd_status fdd::check_paged_cache(const fdd_paged_cache* c, const char* fn)
     if (c->D != 64 && c->D != 128) return fail(FDD_ERR_UNSUPPORTED, "%s: head size D=%d not supported (64 or 128)", fn, c->D);
     if (c->dtype != FDD_F32 && c->dtype != FDD_BF16) return fail(FDD_ERR_DTYPE, "%s: dtype %d is neither FDD_F32 nor FDD_BF16", fn, c->dtype);
     if ((long long)c->max_pages * c->page_size >= (1ll << 30)) return fail(FDD_ERR_SHAPE, "%s: max_pages*page_size must be below 2^30", fn);
-    if (c->Hkv > 65535 || (long long)c->N * c->Hkv >= (1ll << 28)) return fail(FDD_ERR_SHAPE, "%s: N*Hkv too large", fn);
+    if (c->Hkv > 65535 || (long long)c->N * c->Hkv >= (1ll << 28) || (long long)c->pages * c->Hkv >= (1ll << 32))
+        return fail(FDD_ERR_SHAPE, "%s: N*Hkv or pages*Hkv too large", fn);
     if ((long long)c->page_size * c->Hkv * c->D * 4 >= (1ll << 31)) return fail(FDD_ERR_SHAPE, "%s: a page must stay below 2 GiB", fn);
     if (c->reserved != 0) return fail(FDD_ERR_UNSUPPORTED, "%s: reserved field of the cache must be 0", fn);
     if (!c->k || !c->v || !c->page_table || !c->lens) return fail(FDD_ERR_NULL, "%s: k, v, page_table and lens of the cache must not be NULL", fn);
