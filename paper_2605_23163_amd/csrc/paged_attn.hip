@@ -105,6 +105,9 @@ struct Request {
     int len, count;     // rows of the cache, new tokens
     int mtiles, tiles;  // M-tiles of a KV head; tiles of keys
 };
+// Rows of each of a request's M-tiles: as many, in whole wavefronts (448 rows are two M-tiles of 224, not of 256 and 192: wavefronts
+// without rows leave the LDS and the matrix pipe to the others).
+__device__ __forceinline__ int rows_per_mtile(int rows, int mtiles) { return ((rows + 31) / 32 + mtiles - 1) / mtiles * 32; }
 template <typename C>
 __device__ __forceinline__ Request request(const Cut& c, int n)
 {
@@ -204,7 +207,7 @@ struct Cfg {
     static constexpr int SW = CH < 16 ? CH - 1 : 15;     // K's swizzle repeats after 16 rows or 16 bank lines
     static constexpr int NI = T_BYTES / 1024 / WAVES;    // pieces per wavefront, tile and operand
     static constexpr int RUN = NI * RPB < 16 ? NI * RPB : 16;      // rows that are moved together: they lie in one page
-    static constexpr int SLOTS = WAVES == 8 ? (BF16 ? 4 : 3) : 2;      // of K and of V
+    static constexpr int SLOTS = WAVES == 8 ? 4 : 2;     // of K and of V
     static constexpr int V_RING = SLOTS * T_BYTES;
     static constexpr int LDS = 2 * SLOTS * T_BYTES;
     static_assert(NI >= 1, "a tile has a piece for every wavefront");
@@ -242,13 +245,14 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
 
     // ---- rows ----------------------------------------------------------------------------------------------------------
     const int G = a.cut.G, rows = count * G;
-    const int row0 = p.mt * (WAVES * 32);
+    const int mrows = rows_per_mtile(rows, p.r.mtiles), row0 = p.mt * mrows, row_end = min(row0 + mrows, rows);
     const int row = row0 + wave * 32 + l32;
-    const bool row_ok = row < rows;
+    const bool row_ok = row < row_end;
+    const bool busy = row0 + wave * 32 < row_end;      // (others move their share of the tiles)
     const int row_c = min(row, rows - 1);
     const int token = fast_div(row_c, a.cut.dG), g = row_c - token * G;
     if (a.causal) {      // keys behind the M-tile's last token are not seen
-        const int last = fast_div(min(row0 + WAVES * 32, rows) - 1, a.cut.dG);
+        const int last = fast_div(row_end - 1, a.cut.dG);
         t_end = min(t_end, cache_tiles + last / KT + 1);
     }
     const uint64_t* const bits = a.mask ? a.mask + n * a.mask_stride + (long long)token * ((a.cut.B + 63) >> 6) : nullptr;
@@ -459,9 +463,6 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
             if constexpr (decltype(whole)::value) {      // everything that it touches and requests are whole tiles of the cache
                 wait_loads<(2 * S - 4) * C::NI>();
                 wg_barrier();
-                fetch_full(is_v, t_begin + i + S - 1, (i + S - 1) % S, pages);
-                find_pages(t_begin + i + S, pages);
-                fetch_full(is_k, t_begin + i + S, i % S, pages);
             } else {
                 wait_halves(min(2 * (i + S) - 1, 2 * tiles) - min(2 * i + 3, 2 * tiles));       // V of tile i, K of tile i + 1 are there
                 wg_barrier();       // for everyone, and everyone is done with the slots that are requested now
@@ -496,6 +497,11 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                 constexpr int j = decltype(jc)::value;
                 if constexpr (j + AHEAD < NQ + NP) f[(j + AHEAD) % (AHEAD + 1)] = read(std::integral_constant<int, j + AHEAD>());
                 const bf16x8 x = f[j % (AHEAD + 1)];
+                if constexpr (decltype(whole)::value) {      // the requests stand between the matrix instructions, whose shadow they are made in
+                    if constexpr (j == NQ) fetch_full(is_v, t_begin + i + S - 1, (i + S - 1) % S, pages);
+                    if constexpr (j == NQ + NP / 4) find_pages(t_begin + i + S, pages);
+                    if constexpr (j == NQ + NP / 2) fetch_full(is_k, t_begin + i + S, i % S, pages);
+                }
                 if constexpr (j < NQ) {
                     if constexpr (j % QF) to[j / QF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, qf[j % QF]), to[j / QF], 0, 0, 0);
                     else to[j / QF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, qf[j % QF]), f32x16{}, 0, 0, 0);
@@ -526,7 +532,19 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                 update_reference(mx);
             }
         };
-        if (tiles > 0) {
+        if (!busy) {      // the same requests, waits and barriers as below
+            if (tiles > 0) {
+                wait_halves(min(2 * S - 1, 2 * tiles) - 1);
+                wg_barrier();
+            }
+#pragma unroll 1
+            for (int i = 0; i < tiles; ++i) {
+                wait_halves(min(2 * (i + S) - 1, 2 * tiles) - min(2 * i + 3, 2 * tiles));
+                wg_barrier();
+                if (i + S - 1 < tiles) fetch(is_v, t_begin + i + S - 1, (i + S - 1) % S);
+                if (i + S < tiles) fetch(is_k, t_begin + i + S, i % S);
+            }
+        } else if (tiles > 0) {
             f32x16 s0[2], s1[2];
             wait_halves(min(2 * S - 1, 2 * tiles) - 1);      // K of the first tile
             wg_barrier();
@@ -611,7 +629,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                 fetch(is_k, t + S - 1, slot == 0 ? S - 1 : slot - 1);
                 fetch(is_v, t + S - 1, slot == 0 ? S - 1 : slot - 1);
             }
-            step(t, slot);
+            if (busy) step(t, slot);
             slot = slot + 1 == S ? 0 : slot + 1;
         }
     }
@@ -692,8 +710,9 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
                           __builtin_amdgcn_readlane(x.tiles, l)};
     const int pieces = cutting.pieces_of(mine);
     if (pieces <= 1 || mt >= mine.mtiles) return;
-    const int row = (mt * WAVES + wave) * 32 + l32;
-    const bool row_ok = row < mine.count * a.cut.G;
+    const int rows = mine.count * a.cut.G, mrows = rows_per_mtile(rows, mine.mtiles);
+    const int row = mt * mrows + wave * 32 + l32;
+    const bool row_ok = wave * 32 < mrows && row < rows;
     if (!row_ok) return;
     const int first = base + (kh * pieces) * mine.mtiles + mt;
     typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -737,7 +756,7 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
             }
         }
     }
-    const int token = row / a.cut.G, g = row - token * a.cut.G;
+    const int token = fast_div(row, a.cut.dG), g = row - token * a.cut.G;
     const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;
     T* const op = static_cast<T*>(a.out) + (((long long)n * a.cut.B + token) * a.Hq + kh * a.cut.G + g) * D + 4 * half + col0 * 8;
 #pragma unroll
@@ -771,7 +790,7 @@ Plan make_plan(const fdd_paged_cache& c, const fdd_paged_attn_params& p)
 {
     Plan pl;
     const long long rows = (long long)p.B * (p.Hq / c.Hkv);
-    pl.waves = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+    pl.waves = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || c.dtype == FDD_F32 ? 4 : 8;
     pl.kt = c.dtype == FDD_BF16 ? 64 : 32;
     const int capacity = c.max_pages * c.page_size;
     pl.max_len = p.max_len > 0 ? (p.max_len < capacity ? p.max_len : capacity) : capacity;
@@ -811,12 +830,9 @@ hipError_t launch(const fdd_paged_cache& c, const fdd_paged_attn_params& p, cons
 template <typename T, int D>
 hipError_t launch_waves(const fdd_paged_cache& c, const fdd_paged_attn_params& p, const Plan& pl, const Args& a)
 {
-    switch (pl.waves) {
-    case 1: return launch<T, D, 1>(c, p, pl, a);
-    case 2: return launch<T, D, 2>(c, p, pl, a);
-    case 4: return launch<T, D, 4>(c, p, pl, a);
-    default: return launch<T, D, 8>(c, p, pl, a);
-    }
+    if constexpr (std::is_same<T, uint16_t>::value)
+        if (pl.waves == 8) return launch<T, D, 8>(c, p, pl, a);
+    return pl.waves == 1 ? launch<T, D, 1>(c, p, pl, a) : pl.waves == 2 ? launch<T, D, 2>(c, p, pl, a) : launch<T, D, 4>(c, p, pl, a);
 }
 
 }  // namespace paged_attn
