@@ -317,11 +317,11 @@ void* even_rows(const at::Tensor& t, int64_t* stride)
     int64_t step = 0, rows = 1;
     for (int64_t i = d - 3; i >= 0; --i) {
         if (t.size(i) == 1) continue;
-        need(step == 0 || t.stride(i) == step * rows);
-        if (step == 0) step = t.stride(i);
+        need(rows == 1 || t.stride(i) == step * rows);
+        if (rows == 1) step = t.stride(i);
         rows *= t.size(i);
     }
-    need(step == 0 || step >= H * D);
+    need(rows == 1 || step >= H * D);
     *stride = step;
     return t.data_ptr();
 }

@@ -180,11 +180,11 @@ def _rope_array(t, name, lead):
     step, rows = 0, 1
     for n, st in zip(reversed(lead), reversed(s[:-2])):      # rows must be evenly spaced over all leading dimensions
         if n > 1 and t.numel():
-            if step and st != step * rows:
+            if rows > 1 and st != step * rows:
                 raise ValueError(f"rows of {name} must be evenly spaced")
-            step = step or st
+            step = step if rows > 1 else st
             rows *= n
-    if step and step < H * D:
+    if rows > 1 and step < H * D:
         raise ValueError(f"rows of {name} must not overlap")
     return t.data_ptr(), step
 
