@@ -38,6 +38,8 @@ struct Stop {
     int token;              // where the walk ended, or -1: nothing to draw
     int n_path;
     float max, draft_max;   // of the two rows
+    int children;           // entries of the request's list: ids of the children that fell
+    int residue;            // a chain with draft_logits whose next token fell
 };
 
 struct Args {
@@ -54,6 +56,7 @@ struct Args {
     float* chances;
     Stat* stats;            // [2][N*B][pieces]
     Stop* stops;            // [N]
+    int32_t* lists;         // [N,B]
     double* sums;           // [3][N][w_pieces]: of p, of what is drawn from, of q
     int N, B, V, pieces, per_piece;       // per_piece: entries, a multiple of 8
     int w_pieces, w_per;                  // of the row that is drawn from
@@ -176,62 +179,77 @@ __global__ __launch_bounds__(STAT_THREADS) void stats_kernel(Args a)
 }
 
 // ---- walk --------------------------------------------------------------------------------------------------------------
+// Bound by the latency of what depends on one another: lists, then pieces and the tokens' logits, then LDS only.
 template <typename T, bool GREEDY>
 __global__ __launch_bounds__(WALK_THREADS) void walk_kernel(Args a)
 {
     __shared__ float s_max[2][FDD_TREE_MAX];
     __shared__ double s_sum[2][FDD_TREE_MAX];
-    __shared__ int s_arg[FDD_TREE_MAX];             // greedy: of the row; else tokens
-    __shared__ int s_parent[FDD_TREE_MAX];
-    __shared__ float s_p[FDD_TREE_MAX], s_q[FDD_TREE_MAX];      // of a token under its parent's rows
+    __shared__ int s_arg[FDD_TREE_MAX], s_token[FDD_TREE_MAX], s_parent[FDD_TREE_MAX];
+    __shared__ float s_p[FDD_TREE_MAX], s_q[FDD_TREE_MAX], s_u[FDD_TREE_MAX];      // of a token, under its parent's rows
     const int n = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int count = count_of(a, n);
     const bool draft = !GREEDY && a.draft;
     const long long row0 = (long long)n * a.B;
-    for (int j = tid; j < a.B; j += WALK_THREADS) {
-        if (a.chances && (j == 0 || j >= count)) a.chances[row0 + j] = j < count ? 1.f : 0.f;
-        s_parent[j] = parent_at(a, n, j);
+    // a thread has one token (B <= WALK_THREADS)
+    const int j = tid, jc = min(j, a.B - 1);
+    const int token = a.tokens[row0 + jc];
+    const int parent = parent_at(a, n, jc);
+    const float u = GREEDY ? 0.f : a.uniforms[(row0 + jc) * 2];
+    const int count = count_of(a, n);
+    const bool there = j < count, inside = token >= 0 && token < a.V;
+    float of_p = 0.f, of_q = 0.f;
+    if (!GREEDY && there && parent >= 0 && inside) {
+        of_p = entry(static_cast<const T*>(a.logits) + (row0 + parent) * a.V + token);
+        if (draft) of_q = entry(static_cast<const T*>(a.draft) + (row0 + parent) * a.V + token);
     }
-    // rows: a wavefront joins the pieces of one after the other
-    for (int r = wave; r < (draft ? 2 : 1) * count; r += WALK_THREADS / 64) {
+    // rows: a power of two of lanes joins the pieces of one
+    int span = 1;
+    while (span < a.pieces) span *= 2;
+    for (int r0 = wave * (64 / span); r0 < (draft ? 2 : 1) * count; r0 += WALK_THREADS / span) {
+        const int r = r0 + lane / span, piece = lane & (span - 1);
         const int which = r >= count, i = which ? r - count : r;
-        if (which && i + 1 >= count) continue;
+        const bool row = r < (draft ? 2 : 1) * count && !(which && i + 1 >= count);
         const float c = which ? a.draft_c : a.c;
         Stat st = {-INFINITY, a.V - 1, 0.0};
-        if (lane < a.pieces) st = a.stats[((long long)which * a.N * a.B + row0 + i) * a.pieces + lane];
+        if (row && piece < a.pieces) st = a.stats[((long long)which * a.N * a.B + row0 + i) * a.pieces + piece];
         float m = st.max;
         int arg = st.arg;
-        for (int d = 1; d < 64; d *= 2) {
+        for (int d = 1; d < span; d *= 2) {
             const float m2 = __shfl_xor(m, d);
             const int arg2 = __shfl_xor(arg, d);
             if (m2 > m || (m2 == m && arg2 < arg)) m = m2, arg = arg2;
         }
-        const double sum = GREEDY ? 0.0 : wave_sum(lane < a.pieces ? st.sum * (double)__builtin_amdgcn_exp2f((st.max - m) * c) : 0.0);
-        if (lane == 0) {
+        double sum = GREEDY || !row || piece >= a.pieces ? 0.0 : st.sum * (double)__builtin_amdgcn_exp2f((st.max - m) * c);
+        if (!GREEDY)
+            for (int d = 1; d < span; d *= 2) sum += __shfl_xor(sum, d);
+        if (row && piece == 0) {
             s_max[which][i] = m;
             s_sum[which][i] = sum;
             if (GREEDY) s_arg[i] = arg;
         }
     }
+    if (j < a.B) {
+        s_parent[j] = there ? parent : -1;
+        s_token[j] = token;
+        s_u[j] = u;
+    }
     __syncthreads();
-    // tokens under their parents' rows
-    for (int j = tid + 1; j < count; j += WALK_THREADS) {
-        const int parent = s_parent[j], x = a.tokens[row0 + j];
-        float p = 0.f, q = 1.f;
-        if (parent >= 0 && x >= 0 && x < a.V) {
+    if (j < a.B) {
+        float p = 0.f, q = 1.f, chance = there && j == 0 ? 1.f : 0.f;
+        if (there && parent >= 0 && inside) {
             if constexpr (GREEDY) {
-                p = x == s_arg[parent] ? 1.f : 0.f;
+                p = token == s_arg[parent] ? 1.f : 0.f;
             } else {
-                p = (float)((double)__builtin_amdgcn_exp2f((entry(static_cast<const T*>(a.logits) + (row0 + parent) * a.V + x) - s_max[0][parent]) * a.c) / s_sum[0][parent]);
-                if (draft)
-                    q = (float)((double)__builtin_amdgcn_exp2f((entry(static_cast<const T*>(a.draft) + (row0 + parent) * a.V + x) - s_max[1][parent]) * a.draft_c) / s_sum[1][parent]);
+                p = (float)((double)__builtin_amdgcn_exp2f((of_p - s_max[0][parent]) * a.c) / s_sum[0][parent]);
+                if (draft) q = (float)((double)__builtin_amdgcn_exp2f((of_q - s_max[1][parent]) * a.draft_c) / s_sum[1][parent]);
             }
+            chance = draft && q > 0.f ? fminf(1.f, p / q) : draft && p > 0.f ? 1.f : fminf(1.f, p);
         }
-        if (a.chances) a.chances[row0 + j] = draft && q > 0.f ? fminf(1.f, p / q) : draft && p > 0.f ? 1.f : fminf(1.f, p);
+        if (a.chances) a.chances[row0 + j] = chance;
         // a token that an earlier child of the same parent has is no longer there when it is tried
         bool again = false;
-        if (!draft && !GREEDY && parent >= 0)
-            for (int i = parent + 1; i < j; ++i) again = again || (s_parent[i] == parent && a.tokens[row0 + i] == x);
+        if (!draft && !GREEDY && there && parent >= 0)
+            for (int i = parent + 1; i < j; ++i) again = again || (s_parent[i] == parent && s_token[i] == token);
         s_p[j] = again ? 0.f : p;
         s_q[j] = q;
     }
@@ -239,41 +257,48 @@ __global__ __launch_bounds__(WALK_THREADS) void walk_kernel(Args a)
     if (wave) return;
     // children have higher numbers than their parent and are tried in order, so one pass over the tokens meets all of them
     int now = 0, steps = 0;        // (uniform)
-    float left = 1.f;       // of p, behind the children that fell
-    if (count > 0)
-        for (int j0 = 0; j0 < count; j0 += 64) {
-            const int j = j0 + lane;
-            const bool there = j > 0 && j < count;
-            const int parent = there ? s_parent[j] : -1, x = there ? a.tokens[row0 + j] : -1;
-            const float p = there ? s_p[j] : 0.f, q = there ? s_q[j] : 1.f;
-            const float u = there && !GREEDY ? a.uniforms[(row0 + j) * 2] : 0.f;
-            int from = j0;
-            for (;;) {
-                const uint64_t tried = __builtin_amdgcn_ballot_w64(there && parent == now && j >= from);
-                if (tried == 0) break;
-                const int l = __builtin_ctzll(tried);
-                auto of = [&](float y) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, y), l)); };
-                const float p_j = of(p), q_j = of(q), u_j = of(u);
-                from = j0 + l + 1;
-                const bool stands = GREEDY ? p_j > 0.f : u_j * q_j * left < p_j;
-                if (stands) {
-                    now = j0 + l;
-                    if (lane == l) {
-                        a.emitted[row0 + steps] = x;
-                        a.path[row0 + steps + 1] = j;
-                    }
-                    ++steps;
-                    left = 1.f;
-                } else {
-                    left -= p_j;
+    float left = 1.f;              // of p, behind the children that fell
+    for (int j0 = 0; j0 < count; j0 += 64) {
+        const int k = j0 + lane;
+        const bool here = k > 0 && k < count;
+        const int up = here ? s_parent[k] : -1, x = here ? s_token[k] : -1;
+        const float p = here ? s_p[k] : 0.f, q = here ? s_q[k] : 1.f, v = here ? s_u[k] : 0.f;
+        int from = j0;
+        for (;;) {
+            const uint64_t tried = __builtin_amdgcn_ballot_w64(here && up == now && k >= from);
+            if (tried == 0) break;
+            const int l = __builtin_ctzll(tried);
+            auto of = [&](float y) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, y), l)); };
+            const float p_l = of(p), q_l = of(q), u_l = of(v);
+            from = j0 + l + 1;
+            const bool stands = GREEDY ? p_l > 0.f : u_l * q_l * left < p_l;
+            if (stands) {
+                now = j0 + l;
+                if (lane == l) {
+                    a.emitted[row0 + steps] = x;
+                    a.path[row0 + steps + 1] = k;
                 }
+                ++steps;
+                left = 1.f;
+            } else {
+                left -= p_l;
             }
         }
-    // (each entry has one writer: this wavefront, and for the token drawn last the last launch)
-    for (int j = lane; j < a.B; j += 64) {
-        if (count == 0 || j > steps) a.path[row0 + j] = a.emitted[row0 + j] = -1;
-        else if (j == 0) a.path[row0] = 0;
     }
+    // (each entry has one writer: this wavefront, and for the token drawn last the last launch)
+    for (int k = lane; k < a.B; k += 64) {
+        if (count == 0 || k > steps) a.path[row0 + k] = a.emitted[row0 + k] = -1;
+        else if (k == 0) a.path[row0] = 0;
+    }
+    int children = 0;
+    if (!GREEDY && !draft)
+        for (int j0 = now & ~63; j0 < count; j0 += 64) {
+            const int k = j0 + lane;
+            const bool child = k > now && k < count && s_parent[k] == now;
+            const uint64_t all = __builtin_amdgcn_ballot_w64(child);
+            if (child) a.lists[row0 + children + __builtin_popcountll(all & ((1ull << lane) - 1))] = s_token[k];
+            children += __builtin_popcountll(all);
+        }
     if (lane == 0) {
         a.n_path[n] = count > 0 ? steps + 1 : 0;
         if constexpr (GREEDY) {
@@ -283,60 +308,75 @@ __global__ __launch_bounds__(WALK_THREADS) void walk_kernel(Args a)
             st.token = count > 0 ? now : -1;
             st.n_path = steps + 1;
             st.max = count > 0 ? s_max[0][now] : 0.f;
-            st.draft_max = draft && now + 1 < count ? s_max[1][now] : 0.f;
+            st.residue = draft && now + 1 < count;
+            st.draft_max = st.residue ? s_max[1][now] : 0.f;
+            st.children = children;
             a.stops[n] = st;
         }
     }
 }
 
 // ---- weigh -------------------------------------------------------------------------------------------------------------
-// What the last token is drawn from.  CHOSEN: p without the children of the token where the walk ended; else max(p - q, 0) (its
-// only child fell), or p where it had none.
+// What the last token is drawn from: p without the children of the token where the walk ended; or max(p - q, 0) where a chain's next
+// token fell.  A thread has PICK entries that follow one another.
 template <typename T>
 struct Weights {
     const T* p;
-    const T* q;                 // or nullptr
+    const T* q;
+    int V, children;
+    const int* list;            // in LDS
+    bool residue;
     double p_max, q_max, p_c, q_c, p_scale, q_scale;
-    int token, count, n;
 
-    __device__ __forceinline__ double of_p(int v) const { return exp2(((double)entry(p + v) - p_max) * p_c); }
-    __device__ __forceinline__ double of_q(int v) const { return exp2(((double)entry(q + v) - q_max) * q_c); }
-    __device__ __forceinline__ double left(int v) const { return fmax(of_p(v) * p_scale - of_q(v) * q_scale, 0.0); }
+    __device__ __forceinline__ Weights(const Args& a, int n, const Stop& st, const int* children_ids)
+    {
+        const long long row = ((long long)n * a.B + st.token) * a.V;
+        p = static_cast<const T*>(a.logits) + row;
+        residue = st.residue != 0;
+        q = residue ? static_cast<const T*>(a.draft) + row : nullptr;
+        V = a.V;
+        children = st.children;
+        list = children_ids;
+        p_max = st.max;
+        q_max = st.draft_max;
+        p_c = a.c64;
+        q_c = a.draft_c64;
+        p_scale = q_scale = 1.0;
+    }
+    __device__ __forceinline__ void read(const T* row, int v, float (&x)[PICK]) const
+    {
+        constexpr int VE = 16 / sizeof(T);
+        if (v + PICK <= V) {
+            float y[PICK / VE][VE];
+#pragma unroll
+            for (int i = 0; i < PICK / VE; ++i) entries(row + v + i * VE, y[i]);
+#pragma unroll
+            for (int i = 0; i < PICK; ++i) x[i] = y[i / VE][i % VE];
+        } else {
+#pragma unroll
+            for (int i = 0; i < PICK; ++i) x[i] = v + i < V ? entry(row + v + i) : -INFINITY;
+        }
+    }
+    __device__ __forceinline__ static double exponential(float x, double top, double c) { return exp2(((double)x - top) * c); }
+    // bits of the entries at v that were children's
+    __device__ __forceinline__ uint32_t taken(int v) const
+    {
+        uint32_t bits = 0;
+        for (int i = 0; i < children; ++i) {
+            const uint32_t d = (uint32_t)(list[i] - v);
+            bits |= d < (uint32_t)PICK ? 1u << d : 0u;
+        }
+        return bits;
+    }
 };
-template <typename T>
-__device__ __forceinline__ Weights<T> weights(const Args& a, int n, const Stop& st)
+// the request's stop and its children's ids, in LDS
+__device__ __forceinline__ Stop get_stop(const Args& a, int n, int* list)
 {
-    Weights<T> w;
-    const int count = count_of(a, n);
-    const long long row = ((long long)n * a.B + st.token) * a.V;
-    w.p = static_cast<const T*>(a.logits) + row;
-    w.q = a.draft && st.token + 1 < count ? static_cast<const T*>(a.draft) + row : nullptr;
-    w.p_max = st.max;
-    w.q_max = st.draft_max;
-    w.p_c = a.c64;
-    w.q_c = a.draft_c64;
-    w.p_scale = w.q_scale = 1.0;
-    w.token = st.token;
-    w.count = count;
-    w.n = n;
-    return w;
-}
-// ids of the children of the token where the walk ended; all threads of the workgroup call it
-__device__ __forceinline__ int list_children(const Args& a, int n, int token, int count, int* list, int* size)
-{
-    if (threadIdx.x == 0) *size = 0;
-    __syncthreads();
+    const Stop st = a.stops[n];
     if (!a.draft)
-        for (int j = token + 1 + threadIdx.x; j < count; j += blockDim.x)
-            if (parent_at(a, n, j) == token) list[atomicAdd(size, 1)] = a.tokens[(long long)n * a.B + j];      // (a set: its order means nothing)
+        for (int i = threadIdx.x; i < a.B; i += STAT_THREADS) list[i] = a.lists[(long long)n * a.B + i];      // (those behind the last are not used)
     __syncthreads();
-    return *size;
-}
-__device__ __forceinline__ bool is_listed(const int* list, int size, int v)
-{
-    bool hit = false;
-    for (int i = 0; i < size; ++i) hit = hit || list[i] == v;
-    return hit;
+    return st;
 }
 __device__ __forceinline__ double wg_sum(double x, double* scratch)
 {
@@ -385,52 +425,93 @@ __device__ __forceinline__ void wg_first_last(int* first, int* last, int* scratc
         *last = max(*last, scratch[STAT_THREADS / 64 + w]);
     }
 }
-// of a row's pieces; a thread has up to WP / STAT_THREADS that follow one another
-__device__ __forceinline__ double row_sum(const double* sums, int n, double* scratch)
+// Sum of a row's pieces, in every lane.  (Every wavefront for itself: no barrier.  So is the search below.)
+__device__ __forceinline__ double row_sum(const double* sums, int n)
 {
     double s = 0.0;
+    for (int i = threadIdx.x & 63; i < n; i += 64) s += sums[i];
+    return wave_sum(s);
+}
+// The piece that `share` of the sum of all falls into, the first whose end lies above it, or (by rounding) the last one with any
+// weight, and what of the sum lies in front of it; lane l has pieces l each .. (l + 1) each - 1.
+struct Found {
+    int piece;
+    double target, before;
+};
+__device__ __forceinline__ Found find_piece(const double* sums, int n, double share)
+{
+    const int lane = threadIdx.x & 63, each = (n + 63) >> 6, first = lane * each;
+    double mine = 0.0;
+    for (int i = 0; i < each; ++i) mine += first + i < n ? sums[first + i] : 0.0;
+    double end = mine;
 #pragma unroll
-    for (int i = 0; i < WP / STAT_THREADS; ++i) s += (int)threadIdx.x * (WP / STAT_THREADS) + i < n ? sums[threadIdx.x * (WP / STAT_THREADS) + i] : 0.0;
-    return wg_sum(s, scratch);
+    for (int d = 1; d < 64; d *= 2) {
+        const double y = __shfl_up(end, d);
+        if (lane >= d) end += y;
+    }
+    Found f;
+    f.target = share * __shfl(end, 63);
+    const uint64_t over = __builtin_amdgcn_ballot_w64(mine > 0.0 && end > f.target), any = __builtin_amdgcn_ballot_w64(mine > 0.0);
+    const int l = over ? __builtin_ctzll(over) : any ? 63 - __builtin_clzll(any) : 0;
+    double at = __shfl(end - mine, l);
+    f.piece = min(l * each, n - 1);
+    f.before = at;
+    for (int i = 0; i < each && l * each + i < n; ++i) {
+        const double s = sums[l * each + i];
+        if (s > 0.0) {
+            f.piece = l * each + i;
+            f.before = at;
+            if (at + s > f.target) break;
+        }
+        at += s;
+    }
+    return f;
 }
 
 template <typename T, bool RESIDUE>
 __global__ __launch_bounds__(STAT_THREADS) void weigh_kernel(Args a)
 {
     __shared__ int list[FDD_TREE_MAX];
-    __shared__ int size;
     __shared__ double scratch[STAT_THREADS / 64];
     const int piece = blockIdx.x % a.w_pieces, n = blockIdx.x / a.w_pieces;
-    const Stop st = a.stops[n];
-    if (st.token < 0) return;
-    Weights<T> w = weights<T>(a, n, st);
-    if (RESIDUE && !w.q) return;
-    const int children = RESIDUE ? 0 : list_children(a, n, st.token, w.count, list, &size);
-    const int v0 = piece * a.w_per, v1 = min(v0 + a.w_per, a.V);
     const long long np = (long long)a.N * a.w_pieces, at = (long long)n * a.w_pieces + piece;
+    const Stop st = get_stop(a, n, list);
+    if (st.token < 0 || (RESIDUE && !st.residue)) return;
+    Weights<T> w(a, n, st, list);
+    const int v0 = piece * a.w_per, v1 = min(v0 + a.w_per, a.V);
     double all = 0.0, left = 0.0, other = 0.0;
     if constexpr (RESIDUE) {
-        w.p_scale = 1.0 / row_sum(a.sums + (long long)n * a.w_pieces, a.w_pieces, scratch);
-        w.q_scale = 1.0 / row_sum(a.sums + 2 * np + (long long)n * a.w_pieces, a.w_pieces, scratch);
-        for (int v = v0 + threadIdx.x; v < v1; v += STAT_THREADS) left += w.left(v);
-    } else {
-        for (int v = v0 + threadIdx.x; v < v1; v += STAT_THREADS) {
-            const double e = w.of_p(v);
-            all += e;
-            left += is_listed(list, children, v) ? 0.0 : e;
-            if (w.q) other += w.of_q(v);
+        w.p_scale = 1.0 / row_sum(a.sums + (long long)n * a.w_pieces, a.w_pieces);
+        w.q_scale = 1.0 / row_sum(a.sums + 2 * np + (long long)n * a.w_pieces, a.w_pieces);
+    }
+    for (int v = v0 + threadIdx.x * PICK; v < v1; v += STAT_THREADS * PICK) {
+        float x[PICK], y[PICK];
+        w.read(w.p, v, x);
+        if (w.residue) w.read(w.q, v, y);
+        if constexpr (RESIDUE) {
+#pragma unroll
+            for (int i = 0; i < PICK; ++i) left += fmax(w.exponential(x[i], w.p_max, w.p_c) * w.p_scale - w.exponential(y[i], w.q_max, w.q_c) * w.q_scale, 0.0);
+        } else {
+            const uint32_t taken = w.taken(v);
+#pragma unroll
+            for (int i = 0; i < PICK; ++i) {
+                const double e = w.exponential(x[i], w.p_max, w.p_c);
+                all += e;
+                left += taken >> i & 1 ? 0.0 : e;
+                if (w.residue) other += w.exponential(y[i], w.q_max, w.q_c);
+            }
         }
     }
     left = wg_sum(left, scratch);
     if constexpr (!RESIDUE) {
         all = wg_sum(all, scratch);
-        other = wg_sum(other, scratch);
+        if (w.residue) other = wg_sum(other, scratch);
     }
     if (threadIdx.x == 0) {
         a.sums[np + at] = left;
         if constexpr (!RESIDUE) {
             a.sums[at] = all;
-            if (w.q) a.sums[2 * np + at] = other;
+            if (w.residue) a.sums[2 * np + at] = other;
         }
     }
 }
@@ -439,73 +520,52 @@ __global__ __launch_bounds__(STAT_THREADS) void weigh_kernel(Args a)
 template <typename T>
 __global__ __launch_bounds__(STAT_THREADS) void pick_kernel(Args a)
 {
-    constexpr int EACH = WP / STAT_THREADS;
     __shared__ int list[FDD_TREE_MAX];
-    __shared__ int size, ends[2 * STAT_THREADS / 64];
-    __shared__ double scratch[STAT_THREADS / 64], s_target;
+    __shared__ int ends[2 * STAT_THREADS / 64];
+    __shared__ double scratch[STAT_THREADS / 64];
     const int n = blockIdx.x, tid = threadIdx.x;
-    const Stop st = a.stops[n];
-    if (st.token < 0) return;
-    Weights<T> w = weights<T>(a, n, st);
     const long long np = (long long)a.N * a.w_pieces;
     const double* const p_sums = a.sums + (long long)n * a.w_pieces;
-    const double* sums = p_sums + np;
+    const Stop st = get_stop(a, n, list);
+    if (st.token < 0) return;
+    Weights<T> w(a, n, st, list);
     const float u = a.uniforms[((long long)n * a.B + st.token) * 2 + 1];
-    int children = list_children(a, n, st.token, w.count, list, &size);
-    const double all = row_sum(p_sums, a.w_pieces, scratch);
-    double total = row_sum(sums, a.w_pieces, scratch);
-    bool residue = w.q != nullptr;
-    if (residue) {
+    const double* sums = p_sums + np;
+    const double all = row_sum(p_sums, a.w_pieces), total = row_sum(sums, a.w_pieces);
+    if (w.residue) {
         w.p_scale = 1.0 / all;
-        w.q_scale = 1.0 / row_sum(p_sums + 2 * np, a.w_pieces, scratch);
+        w.q_scale = 1.0 / row_sum(p_sums + 2 * np, a.w_pieces);
     }
-    if (total < NOTHING_LEFT * (residue ? 1.0 : all)) {       // the drafts account for all of p
-        residue = false;
-        children = 0;
-        w.p_scale = 1.0;
+    if (total < NOTHING_LEFT * (w.residue ? 1.0 : all)) {       // the drafts account for all of p
+        w.residue = false;
+        w.children = 0;
         sums = p_sums;
-        total = all;
     }
-    // the piece: the first whose end lies above the target, or (by rounding) the last one with any weight
-    const double target = (double)u * total;
-    double part[EACH], mine = 0.0;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        part[i] = tid * EACH + i < a.w_pieces ? sums[tid * EACH + i] : 0.0;
-        mine += part[i];
-    }
-    const double at = wg_before(mine, scratch);
-    int first = INT32_MAX, last = -1;
-    {
-        double end = at;
-        for (int i = 0; i < EACH; ++i) {
-            end += part[i];
-            if (!(part[i] > 0.0)) continue;
-            last = tid * EACH + i;
-            if (end > target) first = min(first, last);
-        }
-    }
-    wg_first_last(&first, &last, ends);
-    const int piece = first != INT32_MAX ? first : max(last, 0);
-    if (tid == piece / EACH) {
-        double begin = at;
-        for (int i = 0; i < piece % EACH; ++i) begin += part[i];
-        s_target = target - begin;
-    }
-    __syncthreads();
-    double left = s_target;
-    last = -1;
+    const Found f = find_piece(sums, a.w_pieces, (double)u);
+    double left = f.target - f.before;
+    int first, last = -1;
     // its entries, STAT_THREADS * PICK at a time
-    const int v0 = piece * a.w_per, v1 = min(v0 + a.w_per, a.V);
+    const int v0 = f.piece * a.w_per, v1 = min(v0 + a.w_per, a.V);
     first = INT32_MAX;
     for (int b = v0; b < v1; b += STAT_THREADS * PICK) {
+        const int v = b + tid * PICK;
         double x[PICK], sum = 0.0;
+        if (v < v1) {
+            float p[PICK], q[PICK];
+            w.read(w.p, v, p);
+            if (w.residue) w.read(w.q, v, q);
+            const uint32_t taken = w.residue ? 0u : w.taken(v);
 #pragma unroll
-        for (int i = 0; i < PICK; ++i) {
-            const int v = b + tid * PICK + i;
-            x[i] = v >= v1 ? 0.0 : residue ? w.left(v) : is_listed(list, children, v) ? 0.0 : w.of_p(v);
-            sum += x[i];
+            for (int i = 0; i < PICK; ++i) {
+                const double e = w.exponential(p[i], w.p_max, w.p_c);
+                x[i] = w.residue ? fmax(e * w.p_scale - w.exponential(q[i], w.q_max, w.q_c) * w.q_scale, 0.0) : taken >> i & 1 ? 0.0 : e;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < PICK; ++i) x[i] = 0.0;
         }
+#pragma unroll
+        for (int i = 0; i < PICK; ++i) sum += x[i];
         double end = wg_before(sum, scratch);
         int from = INT32_MAX, to = last;
 #pragma unroll
@@ -528,7 +588,7 @@ __global__ __launch_bounds__(STAT_THREADS) void pick_kernel(Args a)
 
 struct Plan {
     int pieces, per_piece, w_pieces, w_per;
-    size_t stats, stops, sums;      // bytes
+    size_t stats, stops, lists, sums;      // bytes
 };
 
 Plan make_plan(const fdd_tree_verify_params& p)
@@ -545,6 +605,7 @@ Plan make_plan(const fdd_tree_verify_params& p)
     auto round = [](size_t x) { return (x + 255) & ~(size_t)255; };
     pl.stats = round((size_t)rows * pl.pieces * sizeof(Stat));
     pl.stops = round((size_t)p.N * sizeof(Stop));
+    pl.lists = round((size_t)p.N * p.B * sizeof(int32_t));
     constexpr int unit = STAT_THREADS * PICK;
     pl.w_per = (int)(((p.V + WP - 1) / WP + unit - 1) / unit * unit);
     pl.w_pieces = (int)((p.V + pl.w_per - 1) / pl.w_per);
@@ -606,7 +667,7 @@ size_t fdd_tree_verify_workspace(const fdd_tree_verify_params* p)
 {
     if (check_shape(p) != FDD_OK) return 0;
     const Plan pl = make_plan(*p);
-    return pl.stats + pl.stops + pl.sums;
+    return pl.stats + pl.stops + pl.lists + pl.sums;
 }
 
 fdd_status fdd_tree_verify(const fdd_tree_verify_params* p)
@@ -625,7 +686,7 @@ fdd_status fdd_tree_verify(const fdd_tree_verify_params* p)
     for (const void* x : lists)
         if (!aligned_to(x, 4)) return fail(FDD_ERR_UNSUPPORTED, "%s: arrays must be 4-byte aligned", kFn);
     const Plan pl = make_plan(*p);
-    const size_t need = pl.stats + pl.stops + pl.sums;
+    const size_t need = pl.stats + pl.stops + pl.lists + pl.sums;
     if (!p->workspace) return fail(FDD_ERR_WORKSPACE, "%s: workspace is NULL, %zu bytes needed", kFn, need);
     if (!aligned_to(p->workspace, 256)) return fail(FDD_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", kFn);
     if (p->workspace_bytes < need) return fail(FDD_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", kFn, p->workspace_bytes, need);
@@ -635,7 +696,8 @@ fdd_status fdd_tree_verify(const fdd_tree_verify_params* p)
     char* const ws = static_cast<char*>(p->workspace);
     a.stats = reinterpret_cast<Stat*>(ws);
     a.stops = reinterpret_cast<Stop*>(ws + pl.stats);
-    a.sums = reinterpret_cast<double*>(ws + pl.stats + pl.stops);
+    a.lists = reinterpret_cast<int32_t*>(ws + pl.stats + pl.stops);
+    a.sums = reinterpret_cast<double*>(ws + pl.stats + pl.stops + pl.lists);
     a.N = p->N; a.B = p->B; a.V = (int)p->V; a.pieces = pl.pieces; a.per_piece = pl.per_piece;
     a.w_pieces = pl.w_pieces; a.w_per = pl.w_per;
     if (!greedy) {
