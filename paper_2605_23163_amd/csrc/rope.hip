@@ -112,50 +112,62 @@ struct Unit {
             if (inverse) s[i] = -s[i];
         }
     }
-    __device__ __forceinline__ void apply(const T* x, T* y, int pairs, bool interleaved) const
+    // what a head has at this unit, and what becomes of it
+    __device__ __forceinline__ Piece<T, 2 * VE> read(const T* x, int pairs, bool interleaved) const
     {
-        if (!turns) {
-            store<T, VE, VEC>(y + first, load<T, VE, VEC>(x + first));
-            return;
-        }
         Piece<T, 2 * VE> both;
-        if (interleaved) {
-            both = load<T, 2 * VE, VEC>(x + 2 * first);
-        } else {
-            const Piece<T, VE> a = load<T, VE, VEC>(x + first), b = load<T, VE, VEC>(x + pairs + first);
-#pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                both.x[i] = a.x[i];
-                both.x[VE + i] = b.x[i];
-            }
-        }
-        Piece<T, 2 * VE> r;
+        if (turns && interleaved) return load<T, 2 * VE, VEC>(x + 2 * first);
+        const Piece<T, VE> a = load<T, VE, VEC>(x + first);
+        Piece<T, VE> b = a;
+        if (turns) b = load<T, VE, VEC>(x + pairs + first);
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
-            const float u = to_f32(interleaved ? both.x[2 * i] : both.x[i]), v = to_f32(interleaved ? both.x[2 * i + 1] : both.x[VE + i]);
-            const T p = from_f32<T>(fmaf(u, c[i], -(v * s[i]))), q = from_f32<T>(fmaf(v, c[i], u * s[i]));
-            if (interleaved) {
-                r.x[2 * i] = p;
-                r.x[2 * i + 1] = q;
-            } else {
-                r.x[i] = p;
-                r.x[VE + i] = q;
-            }
+            both.x[i] = a.x[i];
+            both.x[VE + i] = b.x[i];
         }
-        if (interleaved) {
-            store<T, 2 * VE, VEC>(y + 2 * first, r);
-        } else {
-            Piece<T, VE> a, b;
+        return both;
+    }
+    __device__ __forceinline__ void write(const Piece<T, 2 * VE>& both, T* y, int pairs, bool interleaved) const
+    {
+        Piece<T, 2 * VE> r = both;
+        if (turns)
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
-                a.x[i] = r.x[i];
-                b.x[i] = r.x[VE + i];
+                const float u = to_f32(interleaved ? both.x[2 * i] : both.x[i]), v = to_f32(interleaved ? both.x[2 * i + 1] : both.x[VE + i]);
+                const T p = from_f32<T>(fmaf(u, c[i], -(v * s[i]))), q = from_f32<T>(fmaf(v, c[i], u * s[i]));
+                r.x[interleaved ? 2 * i : i] = p;
+                r.x[interleaved ? 2 * i + 1 : VE + i] = q;
             }
-            store<T, VE, VEC>(y + first, a);
-            store<T, VE, VEC>(y + pairs + first, b);
+        if (turns && interleaved) {
+            store<T, 2 * VE, VEC>(y + 2 * first, r);
+            return;
         }
+        Piece<T, VE> a, b;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+            a.x[i] = r.x[i];
+            b.x[i] = r.x[VE + i];
+        }
+        store<T, VE, VEC>(y + first, a);
+        if (turns) store<T, VE, VEC>(y + pairs + first, b);
     }
 };
+
+// f(h) for the heads group, group + groups, .. below H, HEADS of them at a time: all reads of these come before the first write.
+constexpr int HEADS = 4;
+template <typename P, typename Read, typename Write>
+__device__ __forceinline__ void each_head(int group, int groups, int H, const Read& read, const Write& write)
+{
+    int h = group;
+    for (; h + (HEADS - 1) * groups < H; h += HEADS * groups) {
+        P x[HEADS];
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) x[i] = read(h + i * groups);
+#pragma unroll
+        for (int i = 0; i < HEADS; ++i) write(h + i * groups, x[i]);
+    }
+    for (; h < H; h += groups) write(h, read(h));
+}
 
 // units of a head: VE pairs each, then VE channels each
 template <typename T, bool VEC>
@@ -181,7 +193,7 @@ struct RopeArgs {
     FastDiv dUnits, dGroups;
 };
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool INTERLEAVED>
 __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a)
 {
     const int t = (int)(blockIdx.x * THREADS + threadIdx.x);
@@ -190,12 +202,17 @@ __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a)
     const int row = fast_div(rest, a.dGroups), group = rest - row * a.groups;
     Unit<T, VEC> unit;
     unit.set(u, a.pairs, a.rot_dim, a.turns, a.positions[row], a.magnitude, a.inverse);
-    for (int h = group; h < a.H; h += a.groups) {
-        const bool k = h >= a.Hq;
-        const T* const x = k ? static_cast<const T*>(a.k) + row * a.k_stride + (long long)(h - a.Hq) * a.D : static_cast<const T*>(a.q) + row * a.q_stride + (long long)h * a.D;
-        T* const y = k ? static_cast<T*>(a.k_out) + row * a.k_out_stride + (long long)(h - a.Hq) * a.D : static_cast<T*>(a.q_out) + row * a.q_out_stride + (long long)h * a.D;
-        unit.apply(x, y, a.pairs, a.interleaved != 0);
-    }
+    const bool interleaved = INTERLEAVED;
+    each_head<Piece<T, 2 * Unit<T, VEC>::VE>>(
+        group, a.groups, a.H,
+        [&](int h) {
+            const T* const x = h >= a.Hq ? static_cast<const T*>(a.k) + row * a.k_stride + (long long)(h - a.Hq) * a.D : static_cast<const T*>(a.q) + row * a.q_stride + (long long)h * a.D;
+            return unit.read(x, a.pairs, interleaved);
+        },
+        [&](int h, const Piece<T, 2 * Unit<T, VEC>::VE>& x) {
+            T* const y = h >= a.Hq ? static_cast<T*>(a.k_out) + row * a.k_out_stride + (long long)(h - a.Hq) * a.D : static_cast<T*>(a.q_out) + row * a.q_out_stride + (long long)h * a.D;
+            unit.write(x, y, a.pairs, interleaved);
+        });
 }
 
 struct AppendArgs {
@@ -218,7 +235,7 @@ struct AppendArgs {
     FastDiv dAll, dGroups, dB;
 };
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool INTERLEAVED>
 __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a)
 {
     constexpr int V16 = 16 / (int)sizeof(T);
@@ -243,12 +260,17 @@ __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a)
         T* const y = static_cast<T*>(a.k_pages) + head0 * a.D;
         Unit<T, VEC> unit;
         unit.set(u, a.pairs, a.rot_dim, a.turns, a.positions ? a.positions[token] : slot, a.magnitude, false);
-        for (int h = group; h < a.Hkv; h += a.groups) unit.apply(x + h * a.D, y + (((long long)h * a.D) << a.page_shift), a.pairs, a.interleaved != 0);
+        const bool interleaved = INTERLEAVED;
+        each_head<Piece<T, 2 * Unit<T, VEC>::VE>>(
+            group, a.groups, a.Hkv, [&](int h) { return unit.read(x + h * a.D, a.pairs, interleaved); },
+            [&](int h, const Piece<T, 2 * Unit<T, VEC>::VE>& z) { unit.write(z, y + (((long long)h * a.D) << a.page_shift), a.pairs, interleaved); });
     } else {
         const int at = (u - a.units) * V16;
         const T* const x = static_cast<const T*>(a.v) + token * a.v_stride + at;
         T* const y = static_cast<T*>(a.v_pages) + head0 * a.D + at;
-        for (int h = group; h < a.Hkv; h += a.groups) store<T, V16, true>(y + (((long long)h * a.D) << a.page_shift), load<T, V16, true>(x + h * a.D));
+        each_head<Piece<T, V16>>(
+            group, a.groups, a.Hkv, [&](int h) { return load<T, V16, true>(x + h * a.D); },
+            [&](int h, const Piece<T, V16>& z) { store<T, V16, true>(y + (((long long)h * a.D) << a.page_shift), z); });
     }
 }
 
@@ -462,10 +484,16 @@ fdd_status fdd_rope(const fdd_rope_params* p)
     a.dUnits = make_fastdiv((uint32_t)a.units); a.dGroups = make_fastdiv((uint32_t)a.groups);
     const dim3 grid((unsigned)((total + THREADS - 1) / THREADS));
     const hipStream_t s = static_cast<hipStream_t>(p->stream);
-    if (bf16 && vec) rope_kernel<uint16_t, true><<<grid, THREADS, 0, s>>>(a);
-    else if (bf16) rope_kernel<uint16_t, false><<<grid, THREADS, 0, s>>>(a);
-    else if (vec) rope_kernel<float, true><<<grid, THREADS, 0, s>>>(a);
-    else rope_kernel<float, false><<<grid, THREADS, 0, s>>>(a);
+    auto run = [&](auto type, auto vector) {
+        using T = decltype(type);
+        constexpr bool VEC = decltype(vector)::value;
+        if (a.interleaved) rope_kernel<T, VEC, true><<<grid, THREADS, 0, s>>>(a);
+        else rope_kernel<T, VEC, false><<<grid, THREADS, 0, s>>>(a);
+    };
+    if (bf16 && vec) run(uint16_t(), std::true_type());
+    else if (bf16) run(uint16_t(), std::false_type());
+    else if (vec) run(float(), std::true_type());
+    else run(float(), std::false_type());
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(FDD_ERR_LAUNCH, "%s: launch failed: %s", fn, hipGetErrorString(e));
     return FDD_OK;
@@ -517,10 +545,16 @@ fdd_status fdd_paged_append(const fdd_paged_cache* c, const fdd_paged_append_par
     a.dAll = make_fastdiv((uint32_t)a.all); a.dGroups = make_fastdiv((uint32_t)a.groups); a.dB = make_fastdiv((uint32_t)a.B);
     const dim3 grid((unsigned)((total + THREADS - 1) / THREADS));
     const hipStream_t s = static_cast<hipStream_t>(p->stream);
-    if (bf16 && vec) append_kernel<uint16_t, true><<<grid, THREADS, 0, s>>>(a);
-    else if (bf16) append_kernel<uint16_t, false><<<grid, THREADS, 0, s>>>(a);
-    else if (vec) append_kernel<float, true><<<grid, THREADS, 0, s>>>(a);
-    else append_kernel<float, false><<<grid, THREADS, 0, s>>>(a);
+    auto run = [&](auto type, auto vector) {
+        using T = decltype(type);
+        constexpr bool VEC = decltype(vector)::value;
+        if (a.interleaved) append_kernel<T, VEC, true><<<grid, THREADS, 0, s>>>(a);
+        else append_kernel<T, VEC, false><<<grid, THREADS, 0, s>>>(a);
+    };
+    if (bf16 && vec) run(uint16_t(), std::true_type());
+    else if (bf16) run(uint16_t(), std::false_type());
+    else if (vec) run(float(), std::true_type());
+    else run(float(), std::false_type());
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(FDD_ERR_LAUNCH, "%s: launch failed: %s", fn, hipGetErrorString(e));
     return FDD_OK;
