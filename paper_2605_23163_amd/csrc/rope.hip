@@ -58,15 +58,22 @@ __device__ __forceinline__ T from_f32(float x)
     if constexpr (std::is_same<T, float>::value) return x;
     else return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
+// How large calls move their bytes: past the L2s (32 MB in all), which what they write does not fit, nor anything that a call behind
+// could use.  us, from a graph, arrays in rotation, bf16: 16384 rows of 32 heads of 128 rotated (268 MB) 53.1 as they come, 49.5 with such
+// stores, 47.3 with such loads too; 4 prompts of up to 8192 rows of 4 x 128 into pages (101 MB) 25.5, 20.0 and 24.4.
+enum Way { CACHED, STREAM_STORES, STREAM };
+inline Way way_of(long long bytes_written, Way large) { return bytes_written > (32ll << 20) ? large : CACHED; }
+
 // 16 bytes and more at once where rows are 16-byte aligned
-template <typename T, int N, bool VEC>
+template <typename T, int N, bool VEC, int WAY>
 __device__ __forceinline__ Piece<T, N> load(const T* p)
 {
     Piece<T, N> r;
     if constexpr (VEC) {
 #pragma unroll
         for (int i = 0; i < N * (int)sizeof(T) / 16; ++i) {
-            const u32x4 w = reinterpret_cast<const u32x4*>(p)[i];
+            const u32x4* const at = reinterpret_cast<const u32x4*>(p) + i;
+            const u32x4 w = WAY == STREAM ? __builtin_nontemporal_load(at) : *at;
             __builtin_memcpy(reinterpret_cast<char*>(&r) + i * 16, &w, 16);
         }
     } else {
@@ -75,7 +82,7 @@ __device__ __forceinline__ Piece<T, N> load(const T* p)
     }
     return r;
 }
-template <typename T, int N, bool VEC>
+template <typename T, int N, bool VEC, int WAY>
 __device__ __forceinline__ void store(T* p, const Piece<T, N>& r)
 {
     if constexpr (VEC) {
@@ -83,7 +90,9 @@ __device__ __forceinline__ void store(T* p, const Piece<T, N>& r)
         for (int i = 0; i < N * (int)sizeof(T) / 16; ++i) {
             u32x4 w;
             __builtin_memcpy(&w, reinterpret_cast<const char*>(&r) + i * 16, 16);
-            reinterpret_cast<u32x4*>(p)[i] = w;
+            u32x4* const at = reinterpret_cast<u32x4*>(p) + i;
+            if constexpr (WAY != CACHED) __builtin_nontemporal_store(w, at);
+            else *at = w;
         }
     } else {
 #pragma unroll
@@ -93,7 +102,7 @@ __device__ __forceinline__ void store(T* p, const Piece<T, N>& r)
 
 // One head's share of a thread.  A thread takes VE pairs (or, behind them, VP channels that stay) of every head that it has: the
 // angles are worked out once for all of them.  VEC: 16 bytes at a time; otherwise a pair, or a channel.
-template <typename T, bool VEC>
+template <typename T, bool VEC, int WAY>
 struct Unit {
     static constexpr int VE = VEC ? 16 / (int)sizeof(T) : 1;
     float c[VE], s[VE];
@@ -116,10 +125,10 @@ struct Unit {
     __device__ __forceinline__ Piece<T, 2 * VE> read(const T* x, int pairs, bool interleaved) const
     {
         Piece<T, 2 * VE> both;
-        if (turns && interleaved) return load<T, 2 * VE, VEC>(x + 2 * first);
-        const Piece<T, VE> a = load<T, VE, VEC>(x + first);
+        if (turns && interleaved) return load<T, 2 * VE, VEC, WAY>(x + 2 * first);
+        const Piece<T, VE> a = load<T, VE, VEC, WAY>(x + first);
         Piece<T, VE> b = a;
-        if (turns) b = load<T, VE, VEC>(x + pairs + first);
+        if (turns) b = load<T, VE, VEC, WAY>(x + pairs + first);
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
             both.x[i] = a.x[i];
@@ -139,7 +148,7 @@ struct Unit {
                 r.x[interleaved ? 2 * i + 1 : VE + i] = q;
             }
         if (turns && interleaved) {
-            store<T, 2 * VE, VEC>(y + 2 * first, r);
+            store<T, 2 * VE, VEC, WAY>(y + 2 * first, r);
             return;
         }
         Piece<T, VE> a, b;
@@ -148,8 +157,8 @@ struct Unit {
             a.x[i] = r.x[i];
             b.x[i] = r.x[VE + i];
         }
-        store<T, VE, VEC>(y + first, a);
-        if (turns) store<T, VE, VEC>(y + pairs + first, b);
+        store<T, VE, VEC, WAY>(y + first, a);
+        if (turns) store<T, VE, VEC, WAY>(y + pairs + first, b);
     }
 };
 
@@ -173,7 +182,7 @@ __device__ __forceinline__ void each_head(int group, int groups, int H, const Re
 template <typename T, bool VEC>
 int units_of(int rot_dim, int D)
 {
-    constexpr int VE = Unit<T, VEC>::VE;
+    constexpr int VE = Unit<T, VEC, CACHED>::VE;
     return rot_dim / 2 / VE + (D - rot_dim) / VE;
 }
 
@@ -193,23 +202,23 @@ struct RopeArgs {
     FastDiv dUnits, dGroups;
 };
 
-template <typename T, bool VEC, bool INTERLEAVED>
+template <typename T, bool VEC, bool INTERLEAVED, int WAY>
 __global__ __launch_bounds__(THREADS) void rope_kernel(RopeArgs a)
 {
     const int t = (int)(blockIdx.x * THREADS + threadIdx.x);
     if (t >= a.total) return;
     const int rest = fast_div(t, a.dUnits), u = t - rest * a.units;
     const int row = fast_div(rest, a.dGroups), group = rest - row * a.groups;
-    Unit<T, VEC> unit;
+    Unit<T, VEC, WAY> unit;
     unit.set(u, a.pairs, a.rot_dim, a.turns, a.positions[row], a.magnitude, a.inverse);
     const bool interleaved = INTERLEAVED;
-    each_head<Piece<T, 2 * Unit<T, VEC>::VE>>(
+    each_head<Piece<T, 2 * Unit<T, VEC, WAY>::VE>>(
         group, a.groups, a.H,
         [&](int h) {
             const T* const x = h >= a.Hq ? static_cast<const T*>(a.k) + row * a.k_stride + (long long)(h - a.Hq) * a.D : static_cast<const T*>(a.q) + row * a.q_stride + (long long)h * a.D;
             return unit.read(x, a.pairs, interleaved);
         },
-        [&](int h, const Piece<T, 2 * Unit<T, VEC>::VE>& x) {
+        [&](int h, const Piece<T, 2 * Unit<T, VEC, WAY>::VE>& x) {
             T* const y = h >= a.Hq ? static_cast<T*>(a.k_out) + row * a.k_out_stride + (long long)(h - a.Hq) * a.D : static_cast<T*>(a.q_out) + row * a.q_out_stride + (long long)h * a.D;
             unit.write(x, y, a.pairs, interleaved);
         });
@@ -235,7 +244,7 @@ struct AppendArgs {
     FastDiv dAll, dGroups, dB;
 };
 
-template <typename T, bool VEC, bool INTERLEAVED>
+template <typename T, bool VEC, bool INTERLEAVED, int WAY>
 __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a)
 {
     constexpr int V16 = 16 / (int)sizeof(T);
@@ -258,19 +267,19 @@ __global__ __launch_bounds__(THREADS) void append_kernel(AppendArgs a)
     if (u < a.units) {
         const T* const x = static_cast<const T*>(a.k) + token * a.k_stride;
         T* const y = static_cast<T*>(a.k_pages) + head0 * a.D;
-        Unit<T, VEC> unit;
+        Unit<T, VEC, WAY> unit;
         unit.set(u, a.pairs, a.rot_dim, a.turns, a.positions ? a.positions[token] : slot, a.magnitude, false);
         const bool interleaved = INTERLEAVED;
-        each_head<Piece<T, 2 * Unit<T, VEC>::VE>>(
+        each_head<Piece<T, 2 * Unit<T, VEC, WAY>::VE>>(
             group, a.groups, a.Hkv, [&](int h) { return unit.read(x + h * a.D, a.pairs, interleaved); },
-            [&](int h, const Piece<T, 2 * Unit<T, VEC>::VE>& z) { unit.write(z, y + (((long long)h * a.D) << a.page_shift), a.pairs, interleaved); });
+            [&](int h, const Piece<T, 2 * Unit<T, VEC, WAY>::VE>& z) { unit.write(z, y + (((long long)h * a.D) << a.page_shift), a.pairs, interleaved); });
     } else {
         const int at = (u - a.units) * V16;
         const T* const x = static_cast<const T*>(a.v) + token * a.v_stride + at;
         T* const y = static_cast<T*>(a.v_pages) + head0 * a.D + at;
         each_head<Piece<T, V16>>(
-            group, a.groups, a.Hkv, [&](int h) { return load<T, V16, true>(x + h * a.D); },
-            [&](int h, const Piece<T, V16>& z) { store<T, V16, true>(y + (((long long)h * a.D) << a.page_shift), z); });
+            group, a.groups, a.Hkv, [&](int h) { return load<T, V16, true, WAY>(x + h * a.D); },
+            [&](int h, const Piece<T, V16>& z) { store<T, V16, true, WAY>(y + (((long long)h * a.D) << a.page_shift), z); });
     }
 }
 
@@ -484,11 +493,15 @@ fdd_status fdd_rope(const fdd_rope_params* p)
     a.dUnits = make_fastdiv((uint32_t)a.units); a.dGroups = make_fastdiv((uint32_t)a.groups);
     const dim3 grid((unsigned)((total + THREADS - 1) / THREADS));
     const hipStream_t s = static_cast<hipStream_t>(p->stream);
+    const Way way = way_of((long long)p->rows * heads * p->D * es, STREAM);
     auto run = [&](auto type, auto vector) {
         using T = decltype(type);
         constexpr bool VEC = decltype(vector)::value;
-        if (a.interleaved) rope_kernel<T, VEC, true><<<grid, THREADS, 0, s>>>(a);
-        else rope_kernel<T, VEC, false><<<grid, THREADS, 0, s>>>(a);
+        constexpr int LARGE = VEC ? STREAM : CACHED;
+        if (way == CACHED && a.interleaved) rope_kernel<T, VEC, true, CACHED><<<grid, THREADS, 0, s>>>(a);
+        else if (way == CACHED) rope_kernel<T, VEC, false, CACHED><<<grid, THREADS, 0, s>>>(a);
+        else if (a.interleaved) rope_kernel<T, VEC, true, LARGE><<<grid, THREADS, 0, s>>>(a);
+        else rope_kernel<T, VEC, false, LARGE><<<grid, THREADS, 0, s>>>(a);
     };
     if (bf16 && vec) run(uint16_t(), std::true_type());
     else if (bf16) run(uint16_t(), std::false_type());
@@ -545,11 +558,15 @@ fdd_status fdd_paged_append(const fdd_paged_cache* c, const fdd_paged_append_par
     a.dAll = make_fastdiv((uint32_t)a.all); a.dGroups = make_fastdiv((uint32_t)a.groups); a.dB = make_fastdiv((uint32_t)a.B);
     const dim3 grid((unsigned)((total + THREADS - 1) / THREADS));
     const hipStream_t s = static_cast<hipStream_t>(p->stream);
+    const Way way = way_of(2 * tokens * token * es, STREAM_STORES);
     auto run = [&](auto type, auto vector) {
         using T = decltype(type);
         constexpr bool VEC = decltype(vector)::value;
-        if (a.interleaved) append_kernel<T, VEC, true><<<grid, THREADS, 0, s>>>(a);
-        else append_kernel<T, VEC, false><<<grid, THREADS, 0, s>>>(a);
+        constexpr int LARGE = VEC ? STREAM_STORES : CACHED;
+        if (way == CACHED && a.interleaved) append_kernel<T, VEC, true, CACHED><<<grid, THREADS, 0, s>>>(a);
+        else if (way == CACHED) append_kernel<T, VEC, false, CACHED><<<grid, THREADS, 0, s>>>(a);
+        else if (a.interleaved) append_kernel<T, VEC, true, LARGE><<<grid, THREADS, 0, s>>>(a);
+        else append_kernel<T, VEC, false, LARGE><<<grid, THREADS, 0, s>>>(a);
     };
     if (bf16 && vec) run(uint16_t(), std::true_type());
     else if (bf16) run(uint16_t(), std::false_type());

@@ -83,6 +83,19 @@ def test_append(dtype, N, B, page, max_pages, Hkv, D, lens, rot, with_rows, with
     assert np.all(err <= bound), (err - bound).max()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_append_of_many_rows(dtype):
+    """More than the caches hold: 34 MB written."""
+    g = torch.Generator(device="cuda").manual_seed(10)
+    B, Hkv, D = 4200 if dtype == "bf16" else 2100, 8, 128
+    cache = make_cache(g, 2, 64, 70, Hkv, D, dtype, [30, 0])
+    k, v = (torch.randn(2, B, Hkv, D, generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+    kp, vp, bound = expected(cache, k, v, None, [B, B - 100], None, (*R.frequencies(D, 1e4), False, dtype == "bf16"))
+    F.fdd_paged_append(k, v, cache, table=F.fdd_rope_table(D), n_rows=ints([B, B - 100]))
+    assert np.array_equal(cache.v.double().cpu().numpy(), vp)
+    assert np.all(np.abs(cache.k.double().cpu().numpy() - kp) <= bound)
+
+
 def test_append_into_a_pool_beyond_32_bits():
     page, Hkv, D = 1024, 8, 128
     pages = (1 << 32) // (page * Hkv * D) + 3                     # elements of a pool: more than 2^32

@@ -121,3 +121,14 @@ def test_rope_of_nothing_and_of_wrong_arguments():
         F.fdd_rope(x[:3], pos[:3], table, out=x[1:])
     with pytest.raises(F.FddError):
         F.fdd_rope(x[..., :32].contiguous(), pos, table)
+
+
+@pytest.mark.parametrize("dtype,rows,Hq,D,interleaved", [("bf16", 1100, 128, 128, False), ("f32", 1100, 64, 128, True)])
+def test_rope_of_many_rows(dtype, rows, Hq, D, interleaved):
+    """More than the caches hold: 36 MB written."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    table = F.fdd_rope_table(D, interleaved=interleaved)
+    q = torch.randn(rows, Hq, D, generator=g, device="cuda").to(DT[dtype])
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda") * 17 + 5
+    w, m = R.frequencies(D, 1e4)
+    check(F.fdd_rope(q, pos, table), q, pos, w, m, interleaved, dtype == "bf16")
