@@ -157,9 +157,10 @@ struct Cutting {
         const int all = wave_sum(tiles) * c.Hkv;
         per_piece = max(MIN_TILES, __builtin_amdgcn_readfirstlane((all + c.W - 1) / c.W));
     }
-    // The item-th piece.  Items of a request are ordered by (KV head, piece, M-tile).  Workgroups take them as they come, neighbours
-    // on different XCDs: with neighbours on one XCD, whose M-tiles then share keys in its L2, 16 requests of one token and up to
-    // 8192 rows took 54 us instead of 45, and 16 of 64 tokens and 16384 rows 310 instead of 301.
+    // The item-th piece.  A request's (KV head, piece) pairs stand in groups of eight, and in a group one M-tile of all of them behind the
+    // other: workgroups go to the XCDs in turn, so that the M-tiles that read the same keys are on one (16 requests of 64 tokens and 16384
+    // rows 270 -> 263 us), while neighbouring pieces are on different ones (next to one another on one XCD 16 requests of one token and
+    // up to 8192 rows took 54 us instead of 45).
     __device__ __forceinline__ Piece find(const Cut& c, int lane, int item) const
     {
         const int items0 = items_of(c, r), end0 = wave_scan(items0, lane);
@@ -176,11 +177,13 @@ struct Cutting {
                 p.n = n0 + l;
                 p.r = {of(x.len), of(x.count), of(x.mtiles), of(x.tiles)};
                 p.pieces = of(pieces_of(x));
-                const int in = item - of(end - items);
-                const int rest = in / p.r.mtiles;
-                p.mt = in - rest * p.r.mtiles;
-                p.kh = rest / p.pieces;
-                p.piece = rest - p.kh * p.pieces;
+                const int in = item - of(end - items), all = c.Hkv * p.pieces;
+                const int group = in / (kNumXCD * p.r.mtiles), at = in - group * (kNumXCD * p.r.mtiles);
+                const int wide = min(kNumXCD, all - group * kNumXCD);
+                p.mt = at / wide;
+                const int head_piece = group * kNumXCD + at - p.mt * wide;
+                p.kh = head_piece / p.pieces;
+                p.piece = head_piece - p.kh * p.pieces;
                 return p;
             }
             n0 += 64;
@@ -212,6 +215,16 @@ struct Cfg {
     static constexpr int LDS = 2 * SLOTS * T_BYTES;
     static_assert(NI >= 1, "a tile has a piece for every wavefront");
 };
+
+// four neighbouring channels
+__device__ __forceinline__ void store4(float* p, const float (&x)[4]) { *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]}; }
+__device__ __forceinline__ void store4(uint16_t* p, const float (&x)[4])
+{
+    u32x2 w;
+    w[0] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[0]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[1]) << 16;
+    w[1] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[2]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[3]) << 16;
+    *reinterpret_cast<u32x2*>(p) = w;
+}
 
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Args a)
@@ -647,14 +660,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                 float x[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] = l > 0.f ? o[db][4 * v4 + j] * inv : 0.f;
-                if constexpr (C::BF16) {
-                    u32x2 w;
-                    w[0] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[0]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[1]) << 16;
-                    w[1] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[2]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x[3]) << 16;
-                    *reinterpret_cast<u32x2*>(op + db * 32 + v4 * 8) = w;
-                } else {
-                    *reinterpret_cast<f32x4*>(op + db * 32 + v4 * 8) = f32x4{x[0], x[1], x[2], x[3]};
-                }
+                store4(op + db * 32 + v4 * 8, x);
             }
     } else if (row_ok) {
         f32x4* const wo = reinterpret_cast<f32x4*>(a.ws_o) + ((long long)p.item * WAVES + wave) * (DB * 4 * 64) + lane;
@@ -679,19 +685,18 @@ struct MergeArgs {
     int Hq, max_mt;
 };
 
-// One wavefront per (request, KV head, M-tile, its 32-row wavefront, MERGE_COLS of its 16-byte columns): lane = as in the accumulators.
-// Bound by latency where pieces are many: UNROLL of them are on their way at a time.
-constexpr int MERGE_COLS = 2, UNROLL = 8;
+// One wavefront per (request, KV head, M-tile, its 32-row wavefront, 16-byte column): lane = as in the accumulators.  Bound by latency:
+// up to 16 pieces are on their way at a time, and there are as many wavefronts as columns.
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = Cfg<T, D, WAVES>;
-    constexpr int COLS = D / 8, GROUPS = COLS / MERGE_COLS;
+    constexpr int COLS = D / 8;
     const int tid = thread_id_x(), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
     int job = __builtin_amdgcn_readfirstlane((int)wg_id_x() * 4 + (tid >> 6));
-    const int col0 = job % GROUPS * MERGE_COLS;
-    job /= GROUPS;
+    const int col = job % COLS;
+    job /= COLS;
     const int wave = job % WAVES, mtile = job / WAVES;
     const int mt = mtile % a.max_mt, head = mtile / a.max_mt;
     const int n = head / a.cut.Hkv, kh = head - n * a.cut.Hkv;
@@ -714,65 +719,58 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
     const int row = mt * mrows + wave * 32 + l32;
     const bool row_ok = wave * 32 < mrows && row < rows;
     if (!row_ok) return;
-    const int first = base + (kh * pieces) * mine.mtiles + mt;
+    const int all = a.cut.Hkv * pieces;
+    // item of piece i: see Cutting::find
+    auto item_of = [&](int i) {
+        const int head_piece = kh * pieces + i, group = head_piece / kNumXCD, wide = min(kNumXCD, all - group * kNumXCD);
+        return (long long)(base + group * kNumXCD * mine.mtiles + mt * wide + head_piece - group * kNumXCD);
+    };
     typedef float f32x2 __attribute__((ext_vector_type(2)));
-    const f32x2* const ml0 = reinterpret_cast<const f32x2*>(a.ws_ml) + ((long long)first * WAVES + wave) * 32 + l32;
-    const f32x4* const wo0 = reinterpret_cast<const f32x4*>(a.ws_o) + (((long long)first * WAVES + wave) * COLS + col0) * 64 + lane;
-    const long long ml_step = (long long)mine.mtiles * WAVES * 32, wo_step = (long long)mine.mtiles * WAVES * COLS * 64;
+    const f32x2* const ml0 = reinterpret_cast<const f32x2*>(a.ws_ml) + wave * 32 + l32;
+    const f32x4* const wo0 = reinterpret_cast<const f32x4*>(a.ws_o) + (wave * COLS + col) * 64 + lane;
     float m = -INFINITY, l_sum = 0.f;
-    f32x4 y[MERGE_COLS];
+    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    auto join = [&](auto unroll) __attribute__((always_inline)) {
+        constexpr int UNROLL = decltype(unroll)::value;
+        for (int i = 0; i < pieces; i += UNROLL) {
+            f32x2 ml[UNROLL];
+            f32x4 w[UNROLL];
 #pragma unroll
-    for (int j = 0; j < MERGE_COLS; ++j) y[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < pieces; i += UNROLL) {
-        f32x2 ml[UNROLL];
-        f32x4 w[UNROLL][MERGE_COLS];
+            for (int u = 0; u < UNROLL; ++u) {
+                const long long at = item_of(min(i + u, pieces - 1));
+                ml[u] = ml0[at * (WAVES * 32)];
+                w[u] = wo0[at * (WAVES * COLS * 64)];
+            }
+            float top = m;
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int at = min(i + u, pieces - 1);
-            ml[u] = ml0[at * ml_step];
+            for (int u = 0; u < UNROLL; ++u) {
+                if (i + u >= pieces) ml[u][0] = -INFINITY;
+                top = fmaxf(top, ml[u][0]);
+            }
+            const float ref = top == -INFINITY ? 0.f : top;
+            const float old = exp2_fast(m - ref);
+            m = top;
+            l_sum *= old;
+            y = f32x4{y[0] * old, y[1] * old, y[2] * old, y[3] * old};
 #pragma unroll
-            for (int j = 0; j < MERGE_COLS; ++j) w[u][j] = wo0[at * wo_step + j * 64];
-        }
-        float top = m;
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            if (i + u >= pieces) ml[u][0] = -INFINITY;
-            top = fmaxf(top, ml[u][0]);
-        }
-        const float ref = top == -INFINITY ? 0.f : top;
-        const float old = exp2_fast(m - ref);
-        m = top;
-        l_sum *= old;
-#pragma unroll
-        for (int j = 0; j < MERGE_COLS; ++j) y[j] = f32x4{y[j][0] * old, y[j][1] * old, y[j][2] * old, y[j][3] * old};
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const float f = exp2_fast(ml[u][0] - ref);
-            l_sum = fmaf(f, ml[u][1], l_sum);
-#pragma unroll
-            for (int j = 0; j < MERGE_COLS; ++j) {
-                const f32x4 z = w[u][j];
-                y[j] = f32x4{fmaf(f, z[0], y[j][0]), fmaf(f, z[1], y[j][1]), fmaf(f, z[2], y[j][2]), fmaf(f, z[3], y[j][3])};
+            for (int u = 0; u < UNROLL; ++u) {
+                const float f = exp2_fast(ml[u][0] - ref);
+                l_sum = fmaf(f, ml[u][1], l_sum);
+                y = f32x4{fmaf(f, w[u][0], y[0]), fmaf(f, w[u][1], y[1]), fmaf(f, w[u][2], y[2]), fmaf(f, w[u][3], y[3])};
             }
         }
-    }
+    };
+    if (pieces <= 2) join(std::integral_constant<int, 2>());
+    else if (pieces <= 4) join(std::integral_constant<int, 4>());
+    else if (pieces <= 8) join(std::integral_constant<int, 8>());
+    else join(std::integral_constant<int, 16>());
     const int token = fast_div(row, a.cut.dG), g = row - token * a.cut.G;
     const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;
-    T* const op = static_cast<T*>(a.out) + (((long long)n * a.cut.B + token) * a.Hq + kh * a.cut.G + g) * D + 4 * half + col0 * 8;
+    T* const op = static_cast<T*>(a.out) + (((long long)n * a.cut.B + token) * a.Hq + kh * a.cut.G + g) * D + 4 * half + col * 8;
+    float z[4];
 #pragma unroll
-    for (int j = 0; j < MERGE_COLS; ++j) {
-        float z[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = l_sum > 0.f ? y[j][e] * inv : 0.f;
-        if constexpr (std::is_same<T, float>::value) {
-            *reinterpret_cast<f32x4*>(op + j * 8) = f32x4{z[0], z[1], z[2], z[3]};
-        } else {
-            u32x2 w;
-            w[0] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)z[0]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)z[1]) << 16;
-            w[1] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)z[2]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)z[3]) << 16;
-            *reinterpret_cast<u32x2*>(op + j * 8) = w;
-        }
-    }
+    for (int e = 0; e < 4; ++e) z[e] = l_sum > 0.f ? y[e] * inv : 0.f;
+    store4(op, z);
 #endif
 }
 
@@ -822,7 +820,7 @@ hipError_t launch(const fdd_paged_cache& c, const fdd_paged_attn_params& p, cons
     e = hipGetLastError();
     if (e != hipSuccess || !pl.partials) return e;
     MergeArgs m = {a.cut, a.ws_o, a.ws_ml, p.out, p.Hq, pl.max_mt};
-    const long long jobs = (long long)c.N * c.Hkv * pl.max_mt * WAVES * (D / 8 / MERGE_COLS);
+    const long long jobs = (long long)c.N * c.Hkv * pl.max_mt * WAVES * (D / 8);
     merge_kernel<T, D, WAVES><<<dim3((unsigned)((jobs + 3) / 4)), 256, 0, s>>>(m);
     return hipGetLastError();
 }
