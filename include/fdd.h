@@ -555,7 +555,8 @@ fdd_status fdd_tree_mask(const fdd_tree_mask_params *p);
  * per request (B = 1) is the ordinary decoding step.  Tokens n_tokens[n] .. B are not there: their K and V are not
  * used and their rows of `out` stay as they were.  A row that sees nothing (no cache, no bit) is 0.  Queries and keys arrive rotated.
  *
- * FDD_BF16: products on the matrix cores with fp32 accumulation, softmax in fp32, probabilities rounded to bf16.  FDD_F32: fp32
+ * FDD_BF16: products on the matrix cores with fp32 accumulation, softmax in fp32, probabilities rounded to bf16; where a request's
+ * keys are cut into pieces, each piece's average is off by 2^-11 of itself or 2^-39 of the row's largest element of it.  FDD_F32: fp32
  * products and sums.  The order of sums depends on lens, n_tokens and max_len of all requests, and on nothing else.
  *
  * Values: q, k and v finite, scores within fp32's range, for what is seen; keys that a row does not see may hold anything.  A NaN
@@ -607,8 +608,8 @@ fdd_status fdd_paged_attn(const fdd_paged_cache *cache, const fdd_paged_attn_par
  * tokens that are there are read, of draft_logits only those that another token follows.  Tokens outside [0, V) never stand
  * (with q(x) = 1 they take nothing out).  Uniforms are in [0, 1).
  *
- * Tests and chances are taken in fp32 (relative 2^-18 for logits within +-2^7 temperatures of the largest); what the last token is
- * drawn from is summed in fp64.  Logits: finite values and -inf for entries that can never be chosen, a row that is read needs one finite
+ * Tests and chances are taken in fp32 (a probability is off by 2^-15 of itself, for logits within 2^7 temperatures of the largest); what
+ * the last token is drawn from is summed in fp64.  Logits: finite values and -inf for entries that can never be chosen, a row that is read needs one finite
  * entry.  NaN and +inf are not supported: such a request's outputs are undefined (ids stay in range).
  */
 typedef struct fdd_tree_verify_params {

@@ -16,8 +16,12 @@
 //   * bf16: 32x32x16 instructions, tiles of 64 keys.  K's 16-byte pieces are XOR-swizzled by the row, V's 32-byte columns too, which V's
 //     transposing LDS reads (ds_read_b64_tr_b16) need.  fp32: 32x32x2 instructions, tiles of 32 keys; V is read as it lies.
 //   * The softmax reference of a row rises only when a score passes it by more than 2^8: the accumulator is rarely rescaled.
-//   * A request whose tiles are one piece is normalised and written at once; otherwise pieces leave fp32 sums and (m, l), which
-//     merge_kernel joins in the order of the pieces.
+//   * A request whose tiles are one piece is normalised and written at once; otherwise pieces leave their sums and (m, l), which
+//     merge_kernel joins in the order of the pieces.  bf16 calls of more than 64 rows leave averages in fp16 times a power of two for the
+//     row: off by 2^-11 of themselves or 2^-39 of the row's largest, where the output is rounded to 2^-8, in half the bytes, which are as
+//     many as the keys' there (4 requests of 32 tokens and 4096 rows 27.4 -> 25.5 us).  Others leave fp32 sums (16 requests of one token and
+//     up to 8192 rows 40.7 us, and 41.6 in fp16: the conversion costs more than the bytes).
+#include <atomic>
 #include <type_traits>
 #include <utility>
 
@@ -33,6 +37,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
@@ -59,8 +64,8 @@ struct Args {
     const int32_t* table;
     const uint64_t* mask;
     void* out;
-    float* ws_o;        // [item][wave][D / 4 / 2 pieces][lane] of 16 bytes: accumulators as they stand
-    float* ws_ml;       // [item][row][2]
+    float* ws_o;        // [item][wave][16-byte column][lane]: accumulators as they stand, fp32 sums or, of bf16 calls, fp16 averages
+    float* ws_ml;       // [item][row][4]: reference, sum, factor of the averages
     long long q_stride, k_stride, v_stride, mask_stride;
     int pages, page_shift, max_pages, Hq;
     int causal;
@@ -211,6 +216,8 @@ struct Cfg {
     static constexpr int NI = T_BYTES / 1024 / WAVES;    // pieces per wavefront, tile and operand
     static constexpr int RUN = NI * RPB < 16 ? NI * RPB : 16;      // rows that are moved together: they lie in one page
     static constexpr int SLOTS = WAVES == 8 ? 4 : 2;     // of K and of V
+    static constexpr bool HALF = BF16 && WAVES >= 4;     // partial results in fp16
+    static constexpr int COLS = HALF ? D / 16 : D / 8;   // 16-byte columns of a lane's partial results
     static constexpr int V_RING = SLOTS * T_BYTES;
     static constexpr int LDS = 2 * SLOTS * T_BYTES;
     static_assert(NI >= 1, "a tile has a piece for every wavefront");
@@ -662,17 +669,39 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                 for (int j = 0; j < 4; ++j) x[j] = l > 0.f ? o[db][4 * v4 + j] * inv : 0.f;
                 store4(op + db * 32 + v4 * 8, x);
             }
+    } else if constexpr (C::HALF) {
+        // averages in fp16, times a power of two that brings the row's largest to 2^14 .. 2^15
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        float top = 0.f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                o[db][v] *= inv;
+                top = fmaxf(top, __builtin_fabsf(o[db][v]));
+            }
+        top = fmaxf(top, other_half(top));
+        const int up = max(min(14 + 127 - (int)(__builtin_bit_cast(uint32_t, top) >> 23 & 255u), 126), -126);
+        const float scale = __builtin_bit_cast(float, (uint32_t)(127 + up) << 23), back = __builtin_bit_cast(float, (uint32_t)(127 - up) << 23);
+        if (!row_ok) return;
+        f16x8* const wo = reinterpret_cast<f16x8*>(a.ws_o) + ((long long)p.item * WAVES + wave) * (DB * 2 * 64) + lane;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                f16x8 w;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = (_Float16)(o[db][8 * c + j] * scale);
+                wo[(db * 2 + c) * 64] = w;
+            }
+        if (half == 0) reinterpret_cast<f32x4*>(a.ws_ml)[(long long)p.item * WAVES * 32 + wave * 32 + l32] = f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, back, 0.f};
     } else if (row_ok) {
         f32x4* const wo = reinterpret_cast<f32x4*>(a.ws_o) + ((long long)p.item * WAVES + wave) * (DB * 4 * 64) + lane;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int v4 = 0; v4 < 4; ++v4) wo[(db * 4 + v4) * 64] = f32x4{o[db][4 * v4], o[db][4 * v4 + 1], o[db][4 * v4 + 2], o[db][4 * v4 + 3]};
-        if (half == 0) {
-            float* const ml = a.ws_ml + ((long long)p.item * WAVES * 32 + wave * 32 + l32) * 2;
-            ml[0] = l > 0.f ? m_ref * a.c : -INFINITY;
-            ml[1] = l;
-        }
+        if (half == 0) reinterpret_cast<f32x4*>(a.ws_ml)[(long long)p.item * WAVES * 32 + wave * 32 + l32] = f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, 1.f, 0.f};
     }
 #endif
 }
@@ -692,7 +721,7 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = Cfg<T, D, WAVES>;
-    constexpr int COLS = D / 8;
+    constexpr int COLS = C::COLS;
     const int tid = thread_id_x(), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
     int job = __builtin_amdgcn_readfirstlane((int)wg_id_x() * 4 + (tid >> 6));
     const int col = job % COLS;
@@ -725,21 +754,31 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
         const int head_piece = kh * pieces + i, group = head_piece / kNumXCD, wide = min(kNumXCD, all - group * kNumXCD);
         return (long long)(base + group * kNumXCD * mine.mtiles + mt * wide + head_piece - group * kNumXCD);
     };
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    const f32x2* const ml0 = reinterpret_cast<const f32x2*>(a.ws_ml) + wave * 32 + l32;
-    const f32x4* const wo0 = reinterpret_cast<const f32x4*>(a.ws_o) + (wave * COLS + col) * 64 + lane;
-    float m = -INFINITY, l_sum = 0.f;
-    f32x4 y = {0.f, 0.f, 0.f, 0.f};
+    typedef std::conditional_t<C::HALF, f16x8, f32x4> Part;
+    constexpr int E = 16 / sizeof(Part{}[0]);
+    const f32x4* const ml0 = reinterpret_cast<const f32x4*>(a.ws_ml) + wave * 32 + l32;
+    const Part* const wo0 = reinterpret_cast<const Part*>(a.ws_o) + (wave * COLS + col) * 64 + lane;
+    float m = -INFINITY, l_sum = 0.f, y[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = 0.f;
     auto join = [&](auto unroll) __attribute__((always_inline)) {
         constexpr int UNROLL = decltype(unroll)::value;
         for (int i = 0; i < pieces; i += UNROLL) {
-            f32x2 ml[UNROLL];
-            f32x4 w[UNROLL];
+            f32x4 ml[UNROLL];
+            Part w[UNROLL];
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) {
                 const long long at = item_of(min(i + u, pieces - 1));
                 ml[u] = ml0[at * (WAVES * 32)];
                 w[u] = wo0[at * (WAVES * COLS * 64)];
+            }
+            // (all of them are requested before the first is awaited)
+            SCHED_FENCE();
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                u32x4 x = __builtin_bit_cast(u32x4, w[u]);
+                asm volatile("" : "+v"(ml[u]), "+v"(x));
+                w[u] = __builtin_bit_cast(Part, x);
             }
             float top = m;
 #pragma unroll
@@ -751,12 +790,16 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
             const float old = exp2_fast(m - ref);
             m = top;
             l_sum *= old;
-            y = f32x4{y[0] * old, y[1] * old, y[2] * old, y[3] * old};
+#pragma unroll
+            for (int e = 0; e < E; ++e) y[e] *= old;
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) {
                 const float f = exp2_fast(ml[u][0] - ref);
                 l_sum = fmaf(f, ml[u][1], l_sum);
-                y = f32x4{fmaf(f, w[u][0], y[0]), fmaf(f, w[u][1], y[1]), fmaf(f, w[u][2], y[2]), fmaf(f, w[u][3], y[3])};
+                // (averages count with the sum that they are of; a piece that the row sees nothing of is 0)
+                const float g = C::HALF ? f * ml[u][1] * ml[u][2] : f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) y[e] = fmaf(g, (float)w[u][e], y[e]);
             }
         }
     };
@@ -766,11 +809,14 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
     else join(std::integral_constant<int, 16>());
     const int token = fast_div(row, a.cut.dG), g = row - token * a.cut.G;
     const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;
-    T* const op = static_cast<T*>(a.out) + (((long long)n * a.cut.B + token) * a.Hq + kh * a.cut.G + g) * D + 4 * half + col * 8;
-    float z[4];
+    T* const op = static_cast<T*>(a.out) + (((long long)n * a.cut.B + token) * a.Hq + kh * a.cut.G + g) * D + 4 * half + col * (2 * E);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = l_sum > 0.f ? y[e] * inv : 0.f;
-    store4(op, z);
+    for (int c = 0; c < E / 4; ++c) {
+        float z[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = l_sum > 0.f ? y[4 * c + e] * inv : 0.f;
+        store4(op + 8 * c, z);
+    }
 #endif
 }
 
@@ -799,8 +845,8 @@ Plan make_plan(const fdd_paged_cache& c, const fdd_paged_attn_params& p)
     pl.partials = tiles > MIN_TILES;
     pl.items = mtiles + (pl.partials ? pl.W : 0);
     const size_t prow = pl.partials ? (size_t)pl.items * pl.waves * 32 : 0;
-    pl.o_bytes = (prow * c.D * 4 + 255) & ~(size_t)255;
-    pl.ml_bytes = (prow * 8 + 255) & ~(size_t)255;
+    pl.o_bytes = (prow * c.D * (c.dtype == FDD_BF16 && pl.waves >= 4 ? 2 : 4) + 255) & ~(size_t)255;
+    pl.ml_bytes = (prow * 16 + 255) & ~(size_t)255;
     return pl;
 }
 
@@ -814,13 +860,22 @@ hipError_t launch(const fdd_paged_cache& c, const fdd_paged_attn_params& p, cons
 {
     using C = Cfg<T, D, WAVES>;
     const hipStream_t s = static_cast<hipStream_t>(p.stream);
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_kernel<T, D, WAVES>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+    // the LDS limit of this instantiation is raised once per device (bit d of `done`: device d)
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
     if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (!(done.load(std::memory_order_acquire) & bit)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_kernel<T, D, WAVES>), hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS);
+        if (e != hipSuccess) return e;
+        done.fetch_or(bit, std::memory_order_release);
+    }
     attn_kernel<T, D, WAVES><<<dim3((unsigned)pl.items), WAVES * 64, C::LDS, s>>>(a);
     e = hipGetLastError();
     if (e != hipSuccess || !pl.partials) return e;
     MergeArgs m = {a.cut, a.ws_o, a.ws_ml, p.out, p.Hq, pl.max_mt};
-    const long long jobs = (long long)c.N * c.Hkv * pl.max_mt * WAVES * (D / 8);
+    const long long jobs = (long long)c.N * c.Hkv * pl.max_mt * WAVES * C::COLS;
     merge_kernel<T, D, WAVES><<<dim3((unsigned)((jobs + 3) / 4)), 256, 0, s>>>(m);
     return hipGetLastError();
 }

@@ -96,12 +96,13 @@ def attention(q, k, v, see, scale):
 def attention_bound(q, k, scale, average, absolute, bf16):
     """A probability is off by what its score is off by, twice (in the sum below it too): products are summed in fp32 in some order, D + 2
     roundings of partial sums no larger than sum |q k|, and the exponent's product and difference add 2^-22 of the scores' size.  bf16
-    probabilities are rounded to 2^-8; sums over m keys add m 2^-24 at most; the result is rounded to half a step."""
+    probabilities are rounded to 2^-8, and averages of pieces of the keys to 2^-11 (fp16, with a factor of the row's: 2^-39 of its largest
+    element at least); sums over m keys add m 2^-24 at most; the result is rounded to half a step."""
     size = (np.abs(q) @ np.abs(k).T).max() * scale if k.size else 0.0
     D, m = q.shape[-1], k.shape[0]
     eps = 2 * size * ((D + 2) * 2.0 ** -24 + 2.0 ** -22) + 2.0 ** -20 + m * 2.0 ** -24
     if bf16:
-        return absolute * (2.0 ** -8 + eps) * (1 + 2.0 ** -8) + np.abs(average) * 2.0 ** -8
+        return absolute * (2.0 ** -8 + 2.0 ** -11 + eps) * (1 + 2.0 ** -8) + absolute.max(-1, keepdims=True) * 2.0 ** -39 + np.abs(average) * 2.0 ** -8
     return absolute * eps + np.abs(average) * 2.0 ** -24
 
 
