@@ -470,11 +470,19 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
             else if (n == 1) wait_loads<H>();
             else wait_loads<0>();
         };
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            if (i < tiles) fetch(is_k, t_begin + i, i);
-            if (i + 1 < S && i < tiles) fetch(is_v, t_begin + i, i);
+        // what the first step needs; the rest of the ring follows behind the first tile (all at once, it waited behind the others')
+        if (tiles > 0) {
+            fetch(is_k, t_begin, 0);
+            fetch(is_v, t_begin, 0);
         }
+        if (tiles > 1) fetch(is_k, t_begin + 1, 1);
+        auto fill_ring = [&] {
+#pragma unroll 1
+            for (int i = 1; i + 1 < S && i < tiles; ++i) {
+                fetch(is_v, t_begin + i, i);
+                if (i + 1 < tiles) fetch(is_k, t_begin + i + 1, i + 1);
+            }
+        };
         // pages of the tile whose V is requested next in the steps that request whole tiles only
         unsigned long long pages[RUNS];
         // Step i: the probabilities of tile i (scores in s) and P V; scores of tile i + 1 into `to`.
@@ -554,8 +562,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
         };
         if (!busy) {      // the same requests, waits and barriers as below
             if (tiles > 0) {
-                wait_halves(min(2 * S - 1, 2 * tiles) - 1);
+                wait_halves(min(3, 2 * tiles) - 1);
                 wg_barrier();
+                fill_ring();
             }
 #pragma unroll 1
             for (int i = 0; i < tiles; ++i) {
@@ -566,8 +575,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
             }
         } else if (tiles > 0) {
             f32x16 s0[2], s1[2];
-            wait_halves(min(2 * S - 1, 2 * tiles) - 1);      // K of the first tile
+            wait_halves(min(3, 2 * tiles) - 1);      // K of the first tile
             wg_barrier();
+            fill_ring();
             {
                 bf16x8 f[AHEAD + 1];
                 each<0, AHEAD>([&](auto jc) __attribute__((always_inline)) { f[decltype(jc)::value] = read_k(0, jc); });
