@@ -604,9 +604,9 @@ fdd_status fdd_paged_attn(const fdd_paged_cache *cache, const fdd_paged_attn_par
  * chances[n][j] is the probability with which token j stands when it is tried first: min(1, p(x) / q(x)); 1 for token 0, 0
  * for tokens that are not there or have no parent; with temperature 0 it is 1 or 0.
  *
- * draft_logits go with chains only (parents NULL: token j follows j - 1); tokens of a tree count as chosen, not drawn.  Only rows of
- * tokens that are there are read, of draft_logits only those that another token follows.  Tokens outside [0, V) never stand
- * (with q(x) = 1 they take nothing out).  Uniforms are in [0, 1).
+ * draft_logits go with chains only (parents NULL: token j follows j - 1); tokens of a tree count as chosen, not drawn.  With
+ * temperature 0 they have no part.  Only rows of tokens that are there are read, of draft_logits only those that another
+ * token follows.  Tokens outside [0, V) never stand (with q(x) = 1 they take nothing out).  Uniforms are in [0, 1).
  *
  * Tests and chances are taken in fp32 (a probability is off by 2^-15 of itself, for logits within 2^7 temperatures of the largest); what
  * the last token is drawn from is summed in fp64.  Logits: finite values and -inf for entries that can never be chosen, a row that is read needs one finite
@@ -614,7 +614,7 @@ fdd_status fdd_paged_attn(const fdd_paged_cache *cache, const fdd_paged_attn_par
  */
 typedef struct fdd_tree_verify_params {
     int32_t N, B;                  /* B at most FDD_TREE_MAX */
-    int64_t V;                     /* below 2^31 */
+    int64_t V;                     /* at most 2^30 */
     int32_t dtype;                 /* fdd_dtype of logits and draft_logits */
     float temperature;             /* 0, or 2^-20 .. 2^20 */
     float draft_temperature;       /* 2^-20 .. 2^20; draft_logits only */

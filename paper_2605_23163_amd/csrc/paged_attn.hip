@@ -921,7 +921,7 @@ fdd_status check_shape(const fdd_paged_cache* c, const fdd_paged_attn_params* p)
     if (p->reserved != 0) return fail(FDD_ERR_UNSUPPORTED, "%s: reserved field must be 0", kFn);
     if (!finite_bits(p->scale)) return fail(FDD_ERR_UNSUPPORTED, "%s: scale is not finite", kFn);
     const long long tokens = (long long)c->N * p->B;
-    if (p->B > (1 << 24) || p->Hq > 65535 || tokens >= (1ll << 31) || tokens * p->Hq >= (1ll << 31)) return fail(FDD_ERR_SHAPE, "%s: N*B*Hq too large", kFn);
+    if (p->B > (1 << 24) || p->Hq > 65535 || tokens >= (1ll << 30) || tokens * p->Hq >= (1ll << 30)) return fail(FDD_ERR_SHAPE, "%s: N*B*Hq too large", kFn);
     const Plan pl = make_plan(*c, *p);
     const long long tiles = (pl.max_len + pl.kt - 1) / pl.kt + (p->B + pl.kt - 1) / pl.kt;
     if ((long long)c->N * c->Hkv * pl.max_mt * tiles >= (1ll << 31) - pl.W || pl.items >= (1ll << 22))

@@ -650,12 +650,12 @@ fdd_status check_shape(const fdd_tree_verify_params* p)
     if (!p) return fail(FDD_ERR_NULL, "%s: params is NULL", kFn);
     if (p->N <= 0 || p->B <= 0 || p->V <= 0) return fail(FDD_ERR_SHAPE, "%s: N, B, V must be positive (got N=%d B=%d V=%lld)", kFn, p->N, p->B, (long long)p->V);
     if (p->B > FDD_TREE_MAX) return fail(FDD_ERR_UNSUPPORTED, "%s: B=%d is above %d", kFn, p->B, FDD_TREE_MAX);
-    if (p->V >= (1ll << 31) - (1ll << 20)) return fail(FDD_ERR_SHAPE, "%s: V must be below 2^31 - 2^20", kFn);
+    if (p->V > (1ll << 30)) return fail(FDD_ERR_SHAPE, "%s: V must be at most 2^30", kFn);
     if ((long long)p->N * p->B > (1ll << 24)) return fail(FDD_ERR_SHAPE, "%s: N*B too large", kFn);
     if (p->dtype != FDD_F32 && p->dtype != FDD_BF16) return fail(FDD_ERR_DTYPE, "%s: dtype %d is neither FDD_F32 nor FDD_BF16", kFn, p->dtype);
     if (p->reserved != 0) return fail(FDD_ERR_UNSUPPORTED, "%s: reserved field must be 0", kFn);
     if (p->temperature != 0.f && !in_range(p->temperature)) return fail(FDD_ERR_UNSUPPORTED, "%s: temperature must be 0 (greedy) or from 2^-20 to 2^20", kFn);
-    if (p->draft_logits && !in_range(p->draft_temperature)) return fail(FDD_ERR_UNSUPPORTED, "%s: draft_temperature must be from 2^-20 to 2^20", kFn);
+    if (p->draft_logits && p->temperature != 0.f && !in_range(p->draft_temperature)) return fail(FDD_ERR_UNSUPPORTED, "%s: draft_temperature must be from 2^-20 to 2^20", kFn);
     return FDD_OK;
 }
 
@@ -677,7 +677,7 @@ fdd_status fdd_tree_verify(const fdd_tree_verify_params* p)
     const bool greedy = p->temperature == 0.f;
     if (!p->logits || !p->tokens || !p->path || !p->n_path || !p->emitted || (!greedy && !p->uniforms))
         return fail(FDD_ERR_NULL, "%s: logits, tokens, path, n_path and emitted must not be NULL, nor uniforms where the temperature is not 0", kFn);
-    if (p->draft_logits && p->parents) return fail(FDD_ERR_UNSUPPORTED, "%s: draft_logits go with chains only (parents must be NULL)", kFn);
+    if (!greedy && p->draft_logits && p->parents) return fail(FDD_ERR_UNSUPPORTED, "%s: draft_logits go with chains only (parents must be NULL)", kFn);
     if (p->parents && p->parents_stride != 0 && (p->parents_stride < p->B || p->parents_stride > (1ll << 28)))
         return fail(FDD_ERR_SHAPE, "%s: parents_stride=%lld must be 0, or at least B=%d and at most 2^28", kFn, (long long)p->parents_stride, p->B);
     const uintptr_t es = (uintptr_t)dtype_bytes(p->dtype);
