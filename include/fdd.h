@@ -529,7 +529,8 @@ fdd_status fdd_paged_append(const fdd_paged_cache *cache, const fdd_paged_append
  * entry of token 0 is not used.)  n_tokens[n] of the B tokens are there, clamped into [0, B].
  *
  * fdd_tree_mask: bit j mod 64 of mask[n][i][j / 64] is set where token j is i itself or one that it follows, through any number of
- * steps; positions[n][i] = lens[n] + the number of those steps.  Tokens that are not there have no bits and position 0.
+ * steps; positions[n][i] = lens[n] + the number of those steps.  Tokens that are not there have no bits and position 0.  Outputs
+ * overlap nothing.
  */
 #define FDD_TREE_MAX 1024
 typedef struct fdd_tree_mask_params {
@@ -553,7 +554,7 @@ fdd_status fdd_tree_mask(const fdd_tree_mask_params *p);
  * All rows of the cache are seen.  Token b sees token j where bit j mod 64 of mask[n][b][j / 64] is set (fdd_tree_mask, or any
  * other pattern); without a mask all tokens, as in fdd_block_attn, or with FDD_ATTN_CAUSAL_BLOCK those up to b itself.  One token
  * per request (B = 1) is the ordinary decoding step.  Tokens n_tokens[n] .. B are not there: their K and V are not
- * used and their rows of `out` stay as they were.  A row that sees nothing (no cache, no bit) is 0.  Queries and keys arrive rotated.
+ * used and their rows of `out` stay as they were.  `out` overlaps nothing.  A row that sees nothing (no cache, no bit) is 0.  Queries and keys arrive rotated.
  *
  * FDD_BF16: products on the matrix cores with fp32 accumulation, softmax in fp32, probabilities rounded to bf16; where a request's
  * keys are cut into pieces, each piece's average is off by 2^-11 of itself or 2^-39 of the row's largest element of it.  FDD_F32: fp32
@@ -608,9 +609,10 @@ fdd_status fdd_paged_attn(const fdd_paged_cache *cache, const fdd_paged_attn_par
  * temperature 0 they have no part.  Only rows of tokens that are there are read, of draft_logits only those that another
  * token follows.  Tokens outside [0, V) never stand (with q(x) = 1 they take nothing out).  Uniforms are in [0, 1).
  *
- * Tests and chances are taken in fp32 (a probability is off by 2^-15 of itself, for logits within 2^7 temperatures of the largest); what
- * the last token is drawn from is summed in fp64.  Logits: finite values and -inf for entries that can never be chosen, a row that is read needs one finite
- * entry.  NaN and +inf are not supported: such a request's outputs are undefined (ids stay in range).
+ * Tests and chances are taken in fp32 (a probability is off by 2^-15 of itself, for logits within 2^7 temperatures of the
+ * largest); what the last token is drawn from is summed in fp64.  Logits: finite values and -inf for entries that can never be
+ * chosen, a row that is read needs one finite entry.  NaN and +inf are not supported: such a request's outputs are undefined
+ * (ids stay in range).  Outputs overlap nothing.
  */
 typedef struct fdd_tree_verify_params {
     int32_t N, B;                  /* B at most FDD_TREE_MAX */

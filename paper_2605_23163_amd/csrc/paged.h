@@ -12,6 +12,22 @@ inline bool spans_overlap(const void* p, unsigned long long n, const void* q, un
     const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
     return n > 0 && m > 0 && a < b + m && b < a + n;
 }
+// Whether one of the outputs overlaps an input or another output (arrays that are not there have no bytes)
+struct Span {
+    const void* p;
+    unsigned long long bytes;
+};
+template <int OUTS, int INS>
+bool outputs_overlap(const Span (&outs)[OUTS], const Span (&ins)[INS])
+{
+    for (int i = 0; i < OUTS; ++i) {
+        for (int j = 0; j < INS; ++j)
+            if (outs[i].p && ins[j].p && spans_overlap(outs[i].p, outs[i].bytes, ins[j].p, ins[j].bytes)) return true;
+        for (int j = 0; j < i; ++j)
+            if (outs[i].p && outs[j].p && spans_overlap(outs[i].p, outs[i].bytes, outs[j].p, outs[j].bytes)) return true;
+    }
+    return false;
+}
 // (by its bits: some files are compiled without NaN)
 inline bool finite_bits(float x) { return ((__builtin_bit_cast(uint32_t, x) >> 23) & 255u) != 255u; }
 inline long long dtype_bytes(int dtype) { return dtype == FDD_BF16 ? 2 : 4; }

@@ -926,6 +926,8 @@ fdd_status check_shape(const fdd_paged_cache* c, const fdd_paged_attn_params* p)
     const long long tiles = (pl.max_len + pl.kt - 1) / pl.kt + (p->B + pl.kt - 1) / pl.kt;
     if ((long long)c->N * c->Hkv * pl.max_mt * tiles >= (1ll << 31) - pl.W || pl.items >= (1ll << 22))
         return fail(FDD_ERR_SHAPE, "%s: N*B*Hq*max_len too large", kFn);
+    // (a launch has at most 2^32 threads: the merge has a wavefront for 32 rows' four channels or eight)
+    if (pl.partials && (long long)c->N * c->Hkv * pl.max_mt * pl.waves * (c->D / 8) >= (1ll << 26)) return fail(FDD_ERR_SHAPE, "%s: N*B*Hq too large", kFn);
     return FDD_OK;
 }
 
@@ -956,23 +958,24 @@ fdd_status fdd_paged_attn(const fdd_paged_cache* c, const fdd_paged_attn_params*
     // (a tile's tokens are reached by 32-bit offsets: 63 of these of 4 bytes)
     if (p->k_stride > (1 << 23) || p->v_stride > (1 << 23)) return fail(FDD_ERR_SHAPE, "%s: k_stride and v_stride must be at most 2^23 elements", kFn);
     const long long words = (long long)p->B * ((p->B + 63) / 64);
-    if (p->mask && p->mask_stride != 0 && (p->mask_stride < words || p->mask_stride > (1ll << 40)))
-        return fail(FDD_ERR_SHAPE, "%s: mask_stride=%lld must be 0 or at least %lld words", kFn, (long long)p->mask_stride, words);
+    if (p->mask && p->mask_stride != 0 && (p->mask_stride < words || p->mask_stride > (1ll << 56) / c->N))
+        return fail(FDD_ERR_SHAPE, "%s: mask_stride=%lld must be 0 or at least %lld words, and N times it at most 2^56", kFn, (long long)p->mask_stride, words);
     const Plan pl = make_plan(*c, *p);
     Args a = {};
     a.q_stride = token_stride(p->q_stride, q_token); a.k_stride = token_stride(p->k_stride, kv_token); a.v_stride = token_stride(p->v_stride, kv_token);
     const unsigned long long out_bytes = (unsigned long long)(tokens * q_token * es), pool = pool_bytes(*c);
-    const struct { const void* p; unsigned long long bytes; } reads[] = {
-        {p->q, (unsigned long long)(((tokens - 1) * a.q_stride + q_token) * es)}, {p->block_k, (unsigned long long)(((tokens - 1) * a.k_stride + kv_token) * es)},
-        {p->block_v, (unsigned long long)(((tokens - 1) * a.v_stride + kv_token) * es)}, {c->k, pool}, {c->v, pool}};
-    for (const auto& r : reads)
-        if (spans_overlap(r.p, r.bytes, p->out, out_bytes)) return fail(FDD_ERR_UNSUPPORTED, "%s: out overlaps an input", kFn);
     const size_t need = pl.o_bytes + pl.ml_bytes;
     if (need > 0) {
         if (!p->workspace) return fail(FDD_ERR_WORKSPACE, "%s: workspace is NULL, %zu bytes needed", kFn, need);
         if (!aligned_to(p->workspace, 256)) return fail(FDD_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", kFn);
         if (p->workspace_bytes < need) return fail(FDD_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", kFn, p->workspace_bytes, need);
     }
+    const Span outs[] = {{p->out, out_bytes}, {need > 0 ? p->workspace : nullptr, need}};
+    const Span ins[] = {{p->q, (unsigned long long)(((tokens - 1) * a.q_stride + q_token) * es)}, {p->block_k, (unsigned long long)(((tokens - 1) * a.k_stride + kv_token) * es)},
+                        {p->block_v, (unsigned long long)(((tokens - 1) * a.v_stride + kv_token) * es)}, {c->k, pool}, {c->v, pool},
+                        {c->page_table, (unsigned long long)c->N * c->max_pages * 4}, {c->lens, (unsigned long long)c->N * 4},
+                        {p->mask, (unsigned long long)((c->N - 1) * p->mask_stride + words) * 8}, {p->n_tokens, (unsigned long long)c->N * 4}};
+    if (outputs_overlap(outs, ins)) return fail(FDD_ERR_UNSUPPORTED, "%s: out or the workspace overlaps another array", kFn);
     const float scale = p->scale > 0.f ? p->scale : 1.f / std::sqrt((float)c->D);
     a.cut = make_cut(*c, *p, pl);
     a.q = p->q; a.bk = p->block_k; a.bv = p->block_v; a.k_pages = c->k; a.v_pages = c->v; a.table = c->page_table; a.mask = p->mask; a.out = p->out;

@@ -588,7 +588,11 @@ fdd_status fdd_tree_mask(const fdd_tree_mask_params* p)
     if (!p->parents || (!p->mask && !p->positions)) return fail(FDD_ERR_NULL, "%s: parents and one of mask and positions must not be NULL", fn);
     if (!aligned_to(p->parents, 4) || !aligned_to(p->lens, 4) || !aligned_to(p->n_tokens, 4) || !aligned_to(p->mask, 8) || !aligned_to(p->positions, 4))
         return fail(FDD_ERR_UNSUPPORTED, "%s: mask must be 8-byte aligned, the other arrays 4-byte aligned", fn);
-    if ((long long)p->N * p->B >= (1ll << 31)) return fail(FDD_ERR_SHAPE, "%s: N*B too large", fn);
+    if (p->N >= (1 << 22) || (long long)p->N * p->B >= (1ll << 31)) return fail(FDD_ERR_SHAPE, "%s: N or N*B too large", fn);      // (a launch has at most 2^32 threads)
+    const unsigned long long N = p->N, B = p->B;
+    const Span outs[] = {{p->mask, N * B * ((B + 63) / 64) * 8}, {p->positions, N * B * 4}};
+    const Span ins[] = {{p->parents, ((N - 1) * p->parents_stride + B) * 4}, {p->lens, N * 4}, {p->n_tokens, N * 4}};
+    if (outputs_overlap(outs, ins)) return fail(FDD_ERR_UNSUPPORTED, "%s: an output overlaps another array", fn);
     TreeArgs a = {p->parents, p->parents_stride, p->lens, p->n_tokens, p->mask, p->positions, p->B};
     const dim3 grid((unsigned)p->N);
     const hipStream_t s = static_cast<hipStream_t>(p->stream);

@@ -10,7 +10,7 @@
 //   weigh   the row of that token alone, once more and in fp64: sums of pieces of what the last token is drawn from
 //           (a chain with draft_logits: both rows' sums, and in a launch behind it those of max(p - q, 0))
 //   pick    the piece that the uniform falls into, entry by entry
-// A test compares two numbers: fp32 exponentials decide it unless they are within 2^-18 of each other.  The draw compares with
+// A test compares two numbers: fp32 exponentials decide it unless they are within 2^-15 of each other.  The draw compares with
 // V borders that lie as close as the smallest probabilities: an fp32 exponential's error, summed over the row, would move one draw in a
 // few hundred (V = 152064, logits of deviation 2) to a neighbouring entry, so these sums are fp64, and only one row a request needs them.
 #include <cfloat>
@@ -651,7 +651,9 @@ fdd_status check_shape(const fdd_tree_verify_params* p)
     if (p->N <= 0 || p->B <= 0 || p->V <= 0) return fail(FDD_ERR_SHAPE, "%s: N, B, V must be positive (got N=%d B=%d V=%lld)", kFn, p->N, p->B, (long long)p->V);
     if (p->B > FDD_TREE_MAX) return fail(FDD_ERR_UNSUPPORTED, "%s: B=%d is above %d", kFn, p->B, FDD_TREE_MAX);
     if (p->V > (1ll << 30)) return fail(FDD_ERR_SHAPE, "%s: V must be at most 2^30", kFn);
-    if ((long long)p->N * p->B > (1ll << 24)) return fail(FDD_ERR_SHAPE, "%s: N*B too large", kFn);
+    // (a launch has at most 2^32 threads: 256 for each piece of a row, 1024 for a request)
+    if (p->N >= (1 << 22) || (long long)p->N * p->B >= (1ll << 24)) return fail(FDD_ERR_SHAPE, "%s: N or N*B too large", kFn);
+    if (p->N * ((p->V + STAT_THREADS * PICK - 1) / (STAT_THREADS * PICK)) >= (1ll << 24)) return fail(FDD_ERR_SHAPE, "%s: N*V too large", kFn);
     if (p->dtype != FDD_F32 && p->dtype != FDD_BF16) return fail(FDD_ERR_DTYPE, "%s: dtype %d is neither FDD_F32 nor FDD_BF16", kFn, p->dtype);
     if (p->reserved != 0) return fail(FDD_ERR_UNSUPPORTED, "%s: reserved field must be 0", kFn);
     if (p->temperature != 0.f && !in_range(p->temperature)) return fail(FDD_ERR_UNSUPPORTED, "%s: temperature must be 0 (greedy) or from 2^-20 to 2^20", kFn);
@@ -690,6 +692,11 @@ fdd_status fdd_tree_verify(const fdd_tree_verify_params* p)
     if (!p->workspace) return fail(FDD_ERR_WORKSPACE, "%s: workspace is NULL, %zu bytes needed", kFn, need);
     if (!aligned_to(p->workspace, 256)) return fail(FDD_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", kFn);
     if (p->workspace_bytes < need) return fail(FDD_ERR_WORKSPACE, "%s: workspace has %zu bytes, %zu needed", kFn, p->workspace_bytes, need);
+    const unsigned long long N = p->N, B = p->B, rows = N * B * 4, logits = N * B * (unsigned long long)p->V * es;
+    const Span outs[] = {{p->path, rows}, {p->n_path, N * 4}, {p->emitted, rows}, {p->chances, rows}, {p->workspace, need}};
+    const Span ins[] = {{p->logits, logits}, {greedy ? nullptr : p->draft_logits, logits}, {p->tokens, rows}, {p->parents, ((N - 1) * p->parents_stride + B) * 4},
+                        {greedy ? nullptr : p->uniforms, 2 * rows}, {p->n_tokens, N * 4}};
+    if (outputs_overlap(outs, ins)) return fail(FDD_ERR_UNSUPPORTED, "%s: an output or the workspace overlaps another array", kFn);
     Args a = {};
     a.logits = p->logits; a.draft = greedy ? nullptr : p->draft_logits; a.tokens = p->tokens; a.parents = p->parents; a.parents_stride = p->parents_stride;
     a.uniforms = p->uniforms; a.n_tokens = p->n_tokens; a.path = p->path; a.n_path = p->n_path; a.emitted = p->emitted; a.chances = p->chances;

@@ -134,7 +134,9 @@ def tree(**kw):
 
 
 @pytest.mark.parametrize("kw,code", [(dict(N=0), 2), (dict(B=0), 2), (dict(B=1025), 4), (dict(parents=None), 1), (dict(mask=None, positions=None), 1), (dict(parents_stride=31), 2),
-                                     (dict(parents_stride=-32), 2), (dict(parents=258), 4), (dict(mask=4100), 4), (dict(positions=8194), 4), (dict(lens=3), 4), (dict(n_tokens=3), 4)])
+                                     (dict(parents_stride=-32), 2), (dict(parents=258), 4), (dict(mask=4100), 4), (dict(positions=8194), 4), (dict(lens=3), 4), (dict(n_tokens=3), 4),
+                                     (dict(N=1 << 22, B=1), 2), (dict(positions=256), 4), (dict(positions=4096 + 1016), 4), (dict(mask=256 + 120), 4), (dict(lens=8192 + 8), 4),
+                                     (dict(n_tokens=4096 + 1020), 4)])
 def test_tree_mask_refusals(lib, kw, code):
     assert lib.fdd_tree_mask(C.byref(tree(**kw))) == code
     assert lib.fdd_last_error().decode().startswith("fdd_tree_mask:")
@@ -149,7 +151,9 @@ def attn(**kw):
     (dict(B=0), 2), (dict(Hq=0), 2), (dict(Hq=30), 2), (dict(max_len=-1), 2), (dict(flags=2), 4), (dict(reserved=1), 4), (dict(scale=float("nan")), 4), (dict(scale=float("inf")), 4),
     (dict(B=1 << 25), 2), (dict(B=1 << 23, Hq=128), 2), (dict(q=None), 1), (dict(block_k=None), 1), (dict(block_v=None), 1), (dict(out=None), 1), (dict(q=3 * BIG + 8), 4), (dict(mask=4), 4), (dict(n_tokens=2), 4),
     (dict(mask=4096, flags=1), 4), (dict(q_stride=128), 2), (dict(k_stride=4 * 128 + 2), 2), (dict(v_stride=1 << 24), 2), (dict(mask=4096, mask_stride=5), 2), (dict(out=3 * BIG), 4),
-    (dict(out=BIG), 4), (dict(workspace=None), 5), (dict(workspace=7 * BIG + 128), 5), (dict(workspace_bytes=1000), 5)])
+    (dict(out=BIG), 4), (dict(workspace=None), 5), (dict(workspace=7 * BIG + 128), 5), (dict(workspace_bytes=1000), 5),
+    (dict(mask=6 * BIG), 4), (dict(n_tokens=6 * BIG + 64), 4), (dict(workspace=6 * BIG), 4), (dict(workspace=4 * BIG), 4), (dict(mask=7 * BIG), 4),
+    (dict(mask=4096, mask_stride=1 << 55), 2), (dict(B=1 << 18, Hq=128), 2)])
 def test_attn_refusals(lib, kw, code):
     assert lib.fdd_paged_attn(C.byref(cache()), C.byref(attn(**kw))) == code
     assert lib.fdd_last_error().decode().startswith("fdd_paged_attn:")
@@ -175,7 +179,9 @@ def verify(**kw):
     (dict(temperature=float("nan")), 4), (dict(temperature=float("inf")), 4), (dict(temperature=1e-9), 4), (dict(draft_logits=3 * BIG, draft_temperature=0.0), 4), (dict(logits=None), 1),
     (dict(tokens=None), 1), (dict(uniforms=None), 1), (dict(path=None), 1), (dict(n_path=None), 1), (dict(emitted=None), 1), (dict(draft_logits=3 * BIG, parents=256), 4),
     (dict(parents=256, parents_stride=16), 2), (dict(logits=BIG + 1), 4), (dict(tokens=258), 4), (dict(chances=2), 4), (dict(workspace=None), 5), (dict(workspace=2 * BIG + 8), 5),
-    (dict(workspace_bytes=64), 5), (dict(V=(1 << 30) + 1), 2),
+    (dict(workspace_bytes=64), 5), (dict(V=(1 << 30) + 1), 2), (dict(N=1 << 22, B=1, V=8), 2), (dict(N=1 << 20, B=1, V=1 << 20), 2), (dict(N=1 << 14, B=1024), 2),
+    (dict(path=256), 4), (dict(emitted=256 + 508), 4), (dict(n_path=8192 + 4), 4), (dict(chances=16384), 4), (dict(chances=4096 + 1020), 4), (dict(workspace=BIG), 4),
+    (dict(emitted=2 * BIG), 4), (dict(parents=8192), 4), (dict(n_tokens=12288), 4),
     # (with temperature 0 draft_logits have no part: the call gets as far as its workspace)
     (dict(draft_logits=3 * BIG, parents=256, temperature=0.0, draft_temperature=0.0, workspace=None), 5)])
 def test_verify_refusals(lib, kw, code):
