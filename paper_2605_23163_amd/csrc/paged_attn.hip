@@ -1,8 +1,9 @@
 // Attention of every request's new tokens over its paged cache and over one another (fdd_paged_attn), gfx950 matrix cores.
 //
 // How the work is laid out
-//   * The query rows of a request and a KV head, r = token * G + g, are cut into M-tiles of WAVES * 32 rows, 32 for each
-//     wavefront.  All of them use every tile of keys that the workgroup brings into LDS.
+//   * The query rows of a request and a KV head, r = token * G + g, are cut into M-tiles of up to WAVES * 32 rows, as even as whole
+//     wavefronts of 32 rows allow.  All of them use every tile of keys that the workgroup brings into LDS; wavefronts without rows only
+//     help to bring it.
 //   * Keys come in tiles: those of the cache, then those of the request's own tokens.  How many a request has is known on the
 //     device only (lens, n_tokens): each workgroup works out for itself, from these two lists, how many tiles there are in
 //     all, how many of them a piece gets so that all pieces together are as many as the chip takes at once, and which
@@ -21,6 +22,16 @@
 //     row: off by 2^-11 of themselves or 2^-39 of the row's largest, where the output is rounded to 2^-8, in half the bytes, which are as
 //     many as the keys' there (4 requests of 32 tokens and 4096 rows 27.4 -> 25.5 us).  Others leave fp32 sums (16 requests of one token and
 //     up to 8192 rows 40.7 us, and 41.6 in fp16: the conversion costs more than the bytes).
+//
+// Software pipeline (bf16): a step has the scores of tile t + 1 and, beside them in the same stretch of instructions, the softmax and O += P V of
+// tile t; requests for later tiles stand between the matrix instructions.  A step of whole tiles has no branch.
+//
+// What bounds it (bf16, Hq / Hkv / D = 28 / 4 / 128).  Few rows: bytes behind a start of 5 us (lists, table, first requests) and the merge's launch:
+// 16 requests of one token and up to 8192 rows 41 us, of them the merge 5 (floor 32.5 at the rate of a large copy).  Middle: the same
+// start, 4 x 32 tokens, 4096 rows 23.5 us (attention 17, merge 6; MFMA busy 23 %).  Many rows: 16 x 64 tokens, 16384 rows 255 us, 950 TFLOP/s,
+// MFMA busy 55 % of the cycles at 1.7 to 1.85 GHz, which the chip's power leaves: a tile costs a SIMD 3080 cycles, 2048 of them MFMA, and
+// without the reads of LDS it would take 170 us.  64 rows a wavefront, which read LDS half as often, leave one wavefront a SIMD: 339 us.
+// fp32: 3 x up to 21 tokens, 2003 rows, 14 / 2 / 64: 17 us (attention 10.5, merge 6.5).
 #include <atomic>
 #include <type_traits>
 #include <utility>

@@ -10,6 +10,9 @@
 //   weigh   the row of that token alone, once more and in fp64: sums of pieces of what the last token is drawn from
 //           (a chain with draft_logits: both rows' sums, and in a launch behind it those of max(p - q, 0))
 //   pick    the piece that the uniform falls into, entry by entry
+// stats is bound by bytes, what is behind it by the latency of its launches and of the steps that depend on one another: 8 trees of 32 tokens,
+// V = 152064 in bf16, 32.4 us = stats 16.6 (4.7 TB/s), walk 6.0, weigh 5.4, pick 6.3, less what they overlap; 4 chains of 9 tokens, V = 50001 in
+// fp32 with draft_logits, 26.4 us = stats 5.7, walk 4.4, weigh 5.2 and 5.0, pick 6.2.
 // A test compares two numbers: fp32 exponentials decide it unless they are within 2^-15 of each other.  The draw compares with
 // V borders that lie as close as the smallest probabilities: an fp32 exponential's error, summed over the row, would move one draw in a
 // few hundred (V = 152064, logits of deviation 2) to a neighbouring entry, so these sums are fp64, and only one row a request needs them.
