@@ -169,6 +169,52 @@ def test_a_long_cache():
     x.check(x.run())
 
 
+def test_pages_beyond_32_bits():
+    """A pool of 5 GB: the request's pages lie behind the first 2^32 bytes, and the same ones in front of them give the same result."""
+    x = Call("bf16", [150, 3], 3, 8, 2, 128, 64, None, "causal", seed=9)
+    want = x.run()
+    small, used = x.cache, x.cache.k.shape[0]
+    pages = (5 << 30) // (2 * 64 * 128 * 2)
+    k, v = (torch.empty((pages,) + tuple(t.shape[1:]), dtype=t.dtype, device="cuda") for t in (small.k, small.v))
+    k[-used:], v[-used:] = small.k, small.v
+    table = small.page_table.clone()
+    table[(table >= 0) & (table < used)] += pages - used
+    x.cache = F.PagedCache(k, v, table, small.lens)
+    assert torch.equal(x.run(), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_entries_that_name_no_page(dtype):
+    """They are read as the nearest page there is."""
+    x = Call(dtype, [200, 90], 5, 8, 2, 64, 16, None, "causal", seed=10)
+    pages = x.cache.k.shape[0]
+    for t in (x.cache.k, x.cache.v):
+        t.nan_to_num_(0.5)
+    good, bad = x.cache.page_table.clone(), x.cache.page_table.clone()
+    good[0, 3], good[0, 12], good[1, 0] = 0, pages - 1, pages - 1
+    bad[0, 3], bad[0, 12], bad[1, 0] = -1, pages, 2 ** 31 - 1
+    x.cache.page_table.copy_(good)
+    want = x.run()
+    x.cache.page_table.copy_(bad)
+    assert torch.equal(x.run(), want)
+
+
+def test_two_streams_at_once():
+    """Calls side by side, each with a workspace of its own, give what they give alone."""
+    a, b = (Call("bf16", [1500, 700], 8, 28, 4, 128, 16, None, "tree", seed=s) for s in (11, 12))
+    want = [a.run(), b.run()]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, x in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(x.run())
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i]) for o in got[i])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_that_stay(dtype):
     x = Call(dtype, [40, 700], 20, 14, 2, 64, 16, [7, 0], "tree", seed=6)
