@@ -78,6 +78,7 @@ struct Args {
     float* ws_o;        // [item][wave][16-byte column][lane]: accumulators as they stand, fp32 sums or, of bf16 calls, fp16 averages
     float* ws_ml;       // [item][row][4]: reference, sum, factor of the averages
     long long q_stride, k_stride, v_stride, mask_stride;
+    int used;           // wavefronts of an M-tile that can have rows: the others leave nothing
     int pages, page_shift, max_pages, Hq;
     int causal;
     float c;            // scale * log2(e)
@@ -227,7 +228,7 @@ struct Cfg {
     static constexpr int NI = T_BYTES / 1024 / WAVES;    // pieces per wavefront, tile and operand
     static constexpr int RUN = NI * RPB < 16 ? NI * RPB : 16;      // rows that are moved together: they lie in one page
     static constexpr int SLOTS = WAVES == 8 ? 4 : 2;     // of K and of V
-    static constexpr bool HALF = BF16 && WAVES >= 4;     // partial results in fp16
+    static constexpr bool HALF = BF16;                   // partial results in fp16
     static constexpr int COLS = HALF ? D / 16 : D / 8;   // 16-byte columns of a lane's partial results
     static constexpr int V_RING = SLOTS * T_BYTES;
     static constexpr int LDS = 2 * SLOTS * T_BYTES;
@@ -252,7 +253,10 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
     constexpr int KT = C::KT, DB = D / 32;
     extern __shared__ __align__(16) unsigned char lds[];
     const int tid = thread_id_x(), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // (two workgroups share a compute unit, and the second one's first wavefront comes to the second SIMD: where two of four wavefronts have rows,
+    // they change places there, so that every SIMD has one.  fp32, 4 requests of 8 tokens, 28 / 4 heads of 128, 4096 rows 52.6 -> 38.4 us)
+    const int turn = WAVES == 4 && a.used == 2 && (wg_id_x() & kNumCU) ? 3 : 0;
+    const int wave = __builtin_amdgcn_readfirstlane(((tid >> 6) + turn) & (WAVES - 1));
 
     // ---- this workgroup's piece --------------------------------------------------------------------------------------
     Cutting<C> cutting;
@@ -496,6 +500,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
         };
         // pages of the tile whose V is requested next in the steps that request whole tiles only
         unsigned long long pages[RUNS];
+        float mx = -INFINITY;      // the largest score of the tile whose probabilities are next, over this lane's half of its keys
         // Step i: the probabilities of tile i (scores in s) and P V; scores of tile i + 1 into `to`.
         auto step = [&](auto next, auto whole, int i, f32x16 (&s)[2], f32x16 (&to)[2]) __attribute__((always_inline)) {
             constexpr bool NEXT = decltype(next)::value;
@@ -509,29 +514,52 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                 if (i + S < tiles) fetch(is_k, t_begin + i + S, i % S);
             }
             const int k_base = (i + 1) % S * C::T_BYTES, v_base = i % S * C::T_BYTES;
-            const float mc = m_ref * a.c;
-            float sum = 0.f;
-            bf16x8 pf[4], f[AHEAD + 1];
+            typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+            bf16x8 f[AHEAD + 1];
+            u32x4 pw[4];         // probabilities, B operands of P V
+            float mc = 0.f;
             auto read = [&](auto jc) __attribute__((always_inline)) {
                 constexpr int j = decltype(jc)::value;
                 if constexpr (j < NQ) return read_k(k_base, jc);
                 else return read_v(v_base, std::integral_constant<int, j - NQ>());
             };
-            auto probability = [&](auto entry) __attribute__((always_inline)) {
+            // An exponential is taken in three stages, each beside the next one's or the one after next's: none waits for what it needs.
+            auto scale = [&](auto entry) __attribute__((always_inline)) {
                 constexpr int e = decltype(entry)::value;
-                const float x = exp2_fast(fmaf(s[e / 16][e % 16], a.c, -mc));
-                sum += x;
+                float x = fmaf(s[e / 16][e % 16], a.c, -mc);
+                asm volatile("" : "+v"(x));
                 s[e / 16][e % 16] = x;
-                if constexpr (e & 1) {
-                    pf[e / 8][e % 8 - 1] = (__bf16)s[e / 16][e % 16 - 1];
-                    pf[e / 8][e % 8] = (__bf16)x;
-                }
             };
-            constexpr int J0 = NEXT ? 0 : NQ;
-            if constexpr (!NEXT) each<0, 16>(probability);
+            auto tick = [&](auto tc) __attribute__((always_inline)) {
+                constexpr int t = decltype(tc)::value;
+                if constexpr (t < 32) {
+                    float x = exp2_fast(s[t / 16][t % 16]);
+                    asm volatile("" : "+v"(x));
+                    s[t / 16][t % 16] = x;
+                }
+                SCHED_FENCE();
+                if constexpr (t % 2 == 0 && t > 0) {
+                    constexpr int e = t - 2;
+                    const bf16x2 pair = {(__bf16)s[e / 16][e % 16], (__bf16)s[e / 16][e % 16 + 1]};
+                    uint32_t w = __builtin_bit_cast(uint32_t, pair);
+                    asm volatile("" : "+v"(w));
+                    pw[e / 8][e / 2 % 4] = w;
+                }
+                if constexpr (t + 2 < 32) scale(std::integral_constant<int, t + 2>());
+                SCHED_FENCE();
+            };
+            // tick t stands in slot t * SPAN / TICKS
+            constexpr int J0 = NEXT ? 0 : NQ, TICKS = 33, SPAN = NQ + NP - DB;
+            static_assert(8 * SPAN / TICKS < NQ && 16 * SPAN / TICKS < NQ + DB && 24 * SPAN / TICKS < NQ + 2 * DB && 32 * SPAN / TICKS < NQ + 3 * DB, "probabilities before their use");
             each<J0, J0 + AHEAD>([&](auto jc) __attribute__((always_inline)) { f[decltype(jc)::value % (AHEAD + 1)] = read(jc); });
             SCHED_FENCE();
-            float mx0 = -INFINITY, mx1 = -INFINITY;
+            update_reference(mx);
+            mc = m_ref * a.c;
+            mx = -INFINITY;
+            SCHED_FENCE();
+            scale(std::integral_constant<int, 0>());
+            scale(std::integral_constant<int, 1>());
+            SCHED_FENCE();
             each<J0, NQ + NP>([&](auto jc) __attribute__((always_inline)) {
                 constexpr int j = decltype(jc)::value;
                 if constexpr (j + AHEAD < NQ + NP) f[(j + AHEAD) % (AHEAD + 1)] = read(std::integral_constant<int, j + AHEAD>());
@@ -541,35 +569,40 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                     if constexpr (j == NQ + NP / 4) find_pages(t_begin + i + S, pages);
                     if constexpr (j == NQ + NP / 2) fetch_full(is_k, t_begin + i + S, i % S, pages);
                 }
+                if constexpr (!NEXT && j == NQ) each<0, (NQ * TICKS + SPAN - 1) / SPAN>(tick);
                 if constexpr (j < NQ) {
                     if constexpr (j % QF) to[j / QF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, qf[j % QF]), to[j / QF], 0, 0, 0);
                     else to[j / QF] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, qf[j % QF]), f32x16{}, 0, 0, 0);
-                    each<j * 16 / NQ, (j + 1) * 16 / NQ>(probability);
                 } else {
                     constexpr int jj = j - NQ;
-                    o[jj % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, pf[jj / DB], o[jj % DB], 0, 0, 0);
-                    if constexpr (jj < NP / 2) {
-                        each<16 + jj * 32 / NP, 16 + (jj + 1) * 32 / NP>(probability);
-                    } else if constexpr (NEXT) {
-                        each<(jj - NP / 2) * 32 / NP, (jj - NP / 2 + 1) * 32 / NP>([&](auto pair) __attribute__((always_inline)) {
-                            constexpr int e = 2 * decltype(pair)::value;
-                            if constexpr (e & 2) mx1 = fmaxf(mx1, fmaxf(to[e / 16][e % 16], to[e / 16][e % 16 + 1]));
-                            else mx0 = fmaxf(mx0, fmaxf(to[e / 16][e % 16], to[e / 16][e % 16 + 1]));
-                        });
-                    }
+                    o[jj % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, __builtin_bit_cast(bf16x8, pw[jj / DB]), o[jj % DB], 0, 0, 0);
+                }
+                SCHED_FENCE();
+                each<(j * TICKS + SPAN - 1) / SPAN < TICKS ? (j * TICKS + SPAN - 1) / SPAN : TICKS, ((j + 1) * TICKS + SPAN - 1) / SPAN < TICKS ? ((j + 1) * TICKS + SPAN - 1) / SPAN : TICKS>(tick);
+                if constexpr (NEXT && j >= NQ + 2) {
+                    constexpr int q = j - NQ - 2;
+                    each<q * 16 / (NP - 2), (q + 1) * 16 / (NP - 2)>([&](auto vc) __attribute__((always_inline)) {
+                        constexpr int v = decltype(vc)::value;
+                        mx = fmaxf(fmaxf(mx, to[0][v]), to[1][v]);
+                        asm volatile("" : "+v"(mx));
+                    });
                 }
                 SCHED_FENCE();
             });
-            l_run += sum;
-            if (NEXT) {
-                float mx = fmaxf(mx0, mx1);
-                if constexpr (!decltype(whole)::value)
-                    if (is_masked(t_begin + i + 1)) {
-                        mask_scores(t_begin + i + 1, to);
-                        mx = largest(to);
-                    }
-                update_reference(mx);
-            }
+            // (summed as rounded: numerator and denominator see the same values)
+            const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+            float sum0 = 0.f, sum1 = 0.f;
+            each<0, 8>([&](auto kc) __attribute__((always_inline)) {
+                constexpr int k = 2 * decltype(kc)::value;
+                sum0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)pw[k / 4][k % 4]), ones, sum0, false);
+                sum1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)pw[k / 4][k % 4 + 1]), ones, sum1, false);
+            });
+            l_run += sum0 + sum1;
+            if constexpr (NEXT && !decltype(whole)::value)
+                if (is_masked(t_begin + i + 1)) {
+                    mask_scores(t_begin + i + 1, to);
+                    mx = largest(to);
+                }
         };
         if (!busy) {      // the same requests, waits and barriers as below
             if (tiles > 0) {
@@ -601,7 +634,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                 });
             }
             if (is_masked(t_begin)) mask_scores(t_begin, s0);
-            update_reference(largest(s0));
+            mx = largest(s0);
             // (two steps a round: the scores change places without moves)
             const std::true_type yes;
             const std::false_type no;
@@ -705,7 +738,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
         const int up = max(min(14 + 127 - (int)(__builtin_bit_cast(uint32_t, top) >> 23 & 255u), 126), -126);
         const float scale = __builtin_bit_cast(float, (uint32_t)(127 + up) << 23), back = __builtin_bit_cast(float, (uint32_t)(127 - up) << 23);
         if (!row_ok) return;
-        f16x8* const wo = reinterpret_cast<f16x8*>(a.ws_o) + ((long long)p.item * WAVES + wave) * (DB * 2 * 64) + lane;
+        f16x8* const wo = reinterpret_cast<f16x8*>(a.ws_o) + ((long long)p.item * a.used + wave) * (DB * 2 * 64) + lane;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -715,14 +748,14 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                 for (int j = 0; j < 8; ++j) w[j] = (_Float16)(o[db][8 * c + j] * scale);
                 wo[(db * 2 + c) * 64] = w;
             }
-        if (half == 0) reinterpret_cast<f32x4*>(a.ws_ml)[(long long)p.item * WAVES * 32 + wave * 32 + l32] = f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, back, 0.f};
+        if (half == 0) reinterpret_cast<f32x4*>(a.ws_ml)[((long long)p.item * a.used + wave) * 32 + l32] = f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, back, 0.f};
     } else if (row_ok) {
-        f32x4* const wo = reinterpret_cast<f32x4*>(a.ws_o) + ((long long)p.item * WAVES + wave) * (DB * 4 * 64) + lane;
+        f32x4* const wo = reinterpret_cast<f32x4*>(a.ws_o) + ((long long)p.item * a.used + wave) * (DB * 4 * 64) + lane;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int v4 = 0; v4 < 4; ++v4) wo[(db * 4 + v4) * 64] = f32x4{o[db][4 * v4], o[db][4 * v4 + 1], o[db][4 * v4 + 2], o[db][4 * v4 + 3]};
-        if (half == 0) reinterpret_cast<f32x4*>(a.ws_ml)[(long long)p.item * WAVES * 32 + wave * 32 + l32] = f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, 1.f, 0.f};
+        if (half == 0) reinterpret_cast<f32x4*>(a.ws_ml)[((long long)p.item * a.used + wave) * 32 + l32] = f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, 1.f, 0.f};
     }
 #endif
 }
@@ -732,22 +765,23 @@ struct MergeArgs {
     const float* ws_o;
     const float* ws_ml;
     void* out;
-    int Hq, max_mt;
+    int Hq, max_mt, used;
 };
 
 // One wavefront per (request, KV head, M-tile, its 32-row wavefront, 16-byte column): lane = as in the accumulators.  Bound by latency:
 // up to 16 pieces are on their way at a time, and there are as many wavefronts as columns.
-template <typename T, int D, int WAVES>
+template <typename T, int D, int WAVES, int SPLIT>
 __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     using C = Cfg<T, D, WAVES>;
     constexpr int COLS = C::COLS;
     const int tid = thread_id_x(), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
-    int job = __builtin_amdgcn_readfirstlane((int)wg_id_x() * 4 + (tid >> 6));
+    const int share = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
+    int job = SPLIT > 1 ? (int)wg_id_x() : __builtin_amdgcn_readfirstlane((int)wg_id_x() * 4 + (tid >> 6));
     const int col = job % COLS;
     job /= COLS;
-    const int wave = job % WAVES, mtile = job / WAVES;
+    const int wave = job % a.used, mtile = job / a.used;
     const int mt = mtile % a.max_mt, head = mtile / a.max_mt;
     const int n = head / a.cut.Hkv, kh = head - n * a.cut.Hkv;
     if (n >= a.cut.N) return;
@@ -767,8 +801,9 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
     if (pieces <= 1 || mt >= mine.mtiles) return;
     const int rows = mine.count * a.cut.G, mrows = rows_per_mtile(rows, mine.mtiles);
     const int row = mt * mrows + wave * 32 + l32;
-    const bool row_ok = wave * 32 < mrows && row < rows;
-    if (!row_ok) return;
+    if (wave * 32 >= mrows || mt * mrows + wave * 32 >= rows) return;
+    const bool row_ok = row < min((mt + 1) * mrows, rows);
+    if (SPLIT == 1 && !row_ok) return;
     const int all = a.cut.Hkv * pieces;
     // item of piece i: see Cutting::find
     auto item_of = [&](int i) {
@@ -782,16 +817,17 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
     float m = -INFINITY, l_sum = 0.f, y[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) y[e] = 0.f;
+    const int first = pieces * share / SPLIT, last = pieces * (share + 1) / SPLIT, mine_all = last - first;
     auto join = [&](auto unroll) __attribute__((always_inline)) {
         constexpr int UNROLL = decltype(unroll)::value;
-        for (int i = 0; i < pieces; i += UNROLL) {
+        for (int i = first; i < last; i += UNROLL) {
             f32x4 ml[UNROLL];
             Part w[UNROLL];
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) {
-                const long long at = item_of(min(i + u, pieces - 1));
-                ml[u] = ml0[at * (WAVES * 32)];
-                w[u] = wo0[at * (WAVES * COLS * 64)];
+                const long long at = item_of(min(i + u, last - 1));
+                ml[u] = ml0[at * (a.used * 32)];
+                w[u] = wo0[at * (a.used * COLS * 64)];
             }
             // (all of them are requested before the first is awaited)
             SCHED_FENCE();
@@ -804,7 +840,7 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
             float top = m;
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) {
-                if (i + u >= pieces) ml[u][0] = -INFINITY;
+                if (i + u >= last) ml[u][0] = -INFINITY;
                 top = fmaxf(top, ml[u][0]);
             }
             const float ref = top == -INFINITY ? 0.f : top;
@@ -824,10 +860,34 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
             }
         }
     };
-    if (pieces <= 2) join(std::integral_constant<int, 2>());
-    else if (pieces <= 4) join(std::integral_constant<int, 4>());
-    else if (pieces <= 8) join(std::integral_constant<int, 8>());
+    if (mine_all <= 2) join(std::integral_constant<int, 2>());
+    else if (mine_all <= 4) join(std::integral_constant<int, 4>());
+    else if (mine_all <= 8) join(std::integral_constant<int, 8>());
     else join(std::integral_constant<int, 16>());
+    if constexpr (SPLIT > 1) {
+        // the wavefronts' shares, in their order
+        __shared__ float s_m[SPLIT][64], s_l[SPLIT][64], s_y[SPLIT][E][64];
+        s_m[share][lane] = m;
+        s_l[share][lane] = l_sum;
+#pragma unroll
+        for (int e = 0; e < E; ++e) s_y[share][e][lane] = y[e];
+        __syncthreads();
+        if (share || !row_ok) return;
+        float top = m;
+#pragma unroll
+        for (int w = 1; w < SPLIT; ++w) top = fmaxf(top, s_m[w][lane]);
+        const float ref = top == -INFINITY ? 0.f : top, own = exp2_fast(m - ref);
+        l_sum *= own;
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] *= own;
+#pragma unroll
+        for (int w = 1; w < SPLIT; ++w) {
+            const float x = exp2_fast(s_m[w][lane] - ref);
+            l_sum = fmaf(x, s_l[w][lane], l_sum);
+#pragma unroll
+            for (int e = 0; e < E; ++e) y[e] = fmaf(x, s_y[w][e][lane], y[e]);
+        }
+    }
     const int token = fast_div(row, a.cut.dG), g = row - token * a.cut.G;
     const float inv = l_sum > 0.f ? 1.f / l_sum : 0.f;
     T* const op = static_cast<T*>(a.out) + (((long long)n * a.cut.B + token) * a.Hq + kh * a.cut.G + g) * D + 4 * half + col * (2 * E);
@@ -844,7 +904,7 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
 // ---- host ----------------------------------------------------------------------------------------------------------------
 
 struct Plan {
-    int waves, kt, max_mt, W;
+    int waves, used, kt, max_mt, W;
     int max_len;
     long long items;            // no call has more pieces
     bool partials;              // some request may have more than one piece
@@ -855,7 +915,8 @@ Plan make_plan(const fdd_paged_cache& c, const fdd_paged_attn_params& p)
 {
     Plan pl;
     const long long rows = (long long)p.B * (p.Hq / c.Hkv);
-    pl.waves = rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 || c.dtype == FDD_F32 ? 4 : 8;
+    pl.waves = rows <= 128 || c.dtype == FDD_F32 ? 4 : 8;
+    pl.used = rows < pl.waves * 32 ? (int)((rows + 31) / 32) : pl.waves;
     pl.kt = c.dtype == FDD_BF16 ? 64 : 32;
     const int capacity = c.max_pages * c.page_size;
     pl.max_len = p.max_len > 0 ? (p.max_len < capacity ? p.max_len : capacity) : capacity;
@@ -865,8 +926,8 @@ Plan make_plan(const fdd_paged_cache& c, const fdd_paged_attn_params& p)
     const long long mtiles = (long long)c.N * c.Hkv * pl.max_mt;
     pl.partials = tiles > MIN_TILES;
     pl.items = mtiles + (pl.partials ? pl.W : 0);
-    const size_t prow = pl.partials ? (size_t)pl.items * pl.waves * 32 : 0;
-    pl.o_bytes = (prow * c.D * (c.dtype == FDD_BF16 && pl.waves >= 4 ? 2 : 4) + 255) & ~(size_t)255;
+    const size_t prow = pl.partials ? (size_t)pl.items * pl.used * 32 : 0;
+    pl.o_bytes = (prow * c.D * (c.dtype == FDD_BF16 ? 2 : 4) + 255) & ~(size_t)255;
     pl.ml_bytes = (prow * 16 + 255) & ~(size_t)255;
     return pl;
 }
@@ -895,9 +956,12 @@ hipError_t launch(const fdd_paged_cache& c, const fdd_paged_attn_params& p, cons
     attn_kernel<T, D, WAVES><<<dim3((unsigned)pl.items), WAVES * 64, C::LDS, s>>>(a);
     e = hipGetLastError();
     if (e != hipSuccess || !pl.partials) return e;
-    MergeArgs m = {a.cut, a.ws_o, a.ws_ml, p.out, p.Hq, pl.max_mt};
-    const long long jobs = (long long)c.N * c.Hkv * pl.max_mt * WAVES * C::COLS;
-    merge_kernel<T, D, WAVES><<<dim3((unsigned)((jobs + 3) / 4)), 256, 0, s>>>(m);
+    MergeArgs m = {a.cut, a.ws_o, a.ws_ml, p.out, p.Hq, pl.max_mt, pl.used};
+    const long long mtiles = (long long)c.N * c.Hkv * pl.max_mt, jobs = mtiles * pl.used * C::COLS, pieces = pl.W / mtiles;
+    // A request's many pieces: four wavefronts a job (one request of a token and 32768 rows, 128 pieces a KV head, 32.7 -> 22.7 us; 16 wavefronts
+    // 23.7; 4 requests of 32 tokens, 13 pieces, 24.8 and 26.0)
+    if (pieces < 24) merge_kernel<T, D, WAVES, 1><<<dim3((unsigned)((jobs + 3) / 4)), 256, 0, s>>>(m);
+    else merge_kernel<T, D, WAVES, 4><<<dim3((unsigned)jobs), 256, 0, s>>>(m);
     return hipGetLastError();
 }
 
@@ -906,7 +970,7 @@ hipError_t launch_waves(const fdd_paged_cache& c, const fdd_paged_attn_params& p
 {
     if constexpr (std::is_same<T, uint16_t>::value)
         if (pl.waves == 8) return launch<T, D, 8>(c, p, pl, a);
-    return pl.waves == 1 ? launch<T, D, 1>(c, p, pl, a) : pl.waves == 2 ? launch<T, D, 2>(c, p, pl, a) : launch<T, D, 4>(c, p, pl, a);
+    return launch<T, D, 4>(c, p, pl, a);
 }
 
 }  // namespace paged_attn
@@ -938,7 +1002,7 @@ fdd_status check_shape(const fdd_paged_cache* c, const fdd_paged_attn_params* p)
     if ((long long)c->N * c->Hkv * pl.max_mt * tiles >= (1ll << 31) - pl.W || pl.items >= (1ll << 22))
         return fail(FDD_ERR_SHAPE, "%s: N*B*Hq*max_len too large", kFn);
     // (a launch has at most 2^32 threads: the merge has a wavefront for 32 rows' four channels or eight)
-    if (pl.partials && (long long)c->N * c->Hkv * pl.max_mt * pl.waves * (c->D / 8) >= (1ll << 26)) return fail(FDD_ERR_SHAPE, "%s: N*B*Hq too large", kFn);
+    if (pl.partials && (long long)c->N * c->Hkv * pl.max_mt * pl.used * (c->D / 8) >= (1ll << 26)) return fail(FDD_ERR_SHAPE, "%s: N*B*Hq too large", kFn);
     return FDD_OK;
 }
 
@@ -993,6 +1057,7 @@ fdd_status fdd_paged_attn(const fdd_paged_cache* c, const fdd_paged_attn_params*
     a.ws_o = static_cast<float*>(p->workspace);
     a.ws_ml = reinterpret_cast<float*>(static_cast<char*>(p->workspace) + pl.o_bytes);
     a.mask_stride = p->mask_stride;
+    a.used = pl.used;
     a.pages = c->pages; a.page_shift = __builtin_ctz((unsigned)c->page_size); a.max_pages = c->max_pages; a.Hq = p->Hq;
     a.causal = (p->flags & FDD_ATTN_CAUSAL_BLOCK) != 0;
     a.c = scale * 1.4426950408889634f;
