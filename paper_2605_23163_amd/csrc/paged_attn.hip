@@ -137,13 +137,14 @@ __device__ __forceinline__ Request request(const Cut& c, int n)
 }
 
 __device__ __forceinline__ int wave_sum(int x) { return (int)wave_reduce((uint32_t)x, [](uint32_t p, uint32_t q) { return p + q; }); }
-__device__ __forceinline__ int wave_scan(int x, int lane)      // inclusive
+__device__ __forceinline__ int wave_scan(int x)      // inclusive
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, true);      // row_shr 1, 2, 4, 8: rows of 16 lanes
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);     // row_bcast15: the last lane of rows 0 and 2 to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);     // row_bcast31: lane 31 to rows 2 and 3
     return x;
 }
 
@@ -180,7 +181,7 @@ struct Cutting {
     // up to 8192 rows took 54 us instead of 45).
     __device__ __forceinline__ Piece find(const Cut& c, int lane, int item) const
     {
-        const int items0 = items_of(c, r), end0 = wave_scan(items0, lane);
+        const int items0 = items_of(c, r), end0 = wave_scan(items0);
         Piece p;
         p.n = -1;
         p.item = item;
@@ -209,7 +210,7 @@ struct Cutting {
             x = {0, 0, 0, 0};
             if (n0 + lane < c.N) x = request<C>(c, n0 + lane);
             items = items_of(c, x);
-            end = base + wave_scan(items, lane);
+            end = base + wave_scan(items);
         }
     }
 };
@@ -915,7 +916,9 @@ Plan make_plan(const fdd_paged_cache& c, const fdd_paged_attn_params& p)
 {
     Plan pl;
     const long long rows = (long long)p.B * (p.Hq / c.Hkv);
-    pl.waves = rows <= 128 || c.dtype == FDD_F32 ? 4 : 8;
+    // Four wavefronts up to 128 rows, and up to 256 where there are few (request, KV head) pairs: more, shorter pieces start sooner than keys are brought
+    // twice (us, 4 wavefronts and 8: 8 requests of 224 rows, 2048 keys 23.6 and 24.8, 4 of 4096 24.4 and 25.2; 16 of 16384 150 and 145, 64 of 2048 100 and 87).
+    pl.waves = rows <= 128 || (rows <= 256 && c.N * c.Hkv <= 32) || c.dtype == FDD_F32 ? 4 : 8;
     pl.used = rows < pl.waves * 32 ? (int)((rows + 31) / 32) : pl.waves;
     pl.kt = c.dtype == FDD_BF16 ? 64 : 32;
     const int capacity = c.max_pages * c.page_size;
