@@ -711,6 +711,14 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
 
     // ---- out ---------------------------------------------------------------------------------------------------------------
     const float l = l_run + other_half(l_run);
+    // Partial results go through the L2s to memory (aux 16: device scope): the merge's wavefronts are on other XCDs, and what is left
+    // dirty goes out only when the launch has ended (4 requests of 32 tokens, 4096 rows 24.1 -> 23.3 us; 16 of a token, whose stores are parts of lines,
+    // 40.4 -> 40.8: a branch for these cost as much).
+    const long long place = (long long)p.item * a.used + wave;
+    constexpr int O_BYTES = DB * (C::HALF ? 2 : 4) * 1024;
+    const __amdgpu_buffer_rsrc_t o_rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(a.ws_o) + place * O_BYTES, 0, O_BYTES, RSRC_FLAGS);
+    const __amdgpu_buffer_rsrc_t ml_rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>(a.ws_ml) + place * 512, 0, 512, RSRC_FLAGS);
+    auto put = [](const __amdgpu_buffer_rsrc_t& rsrc, int at, u32x4 w) __attribute__((always_inline)) { __builtin_amdgcn_raw_buffer_store_b128(w, rsrc, at, 0, 16); };
     if (p.pieces == 1) {
         if (!row_ok) return;
         const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -739,7 +747,6 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
         const int up = max(min(14 + 127 - (int)(__builtin_bit_cast(uint32_t, top) >> 23 & 255u), 126), -126);
         const float scale = __builtin_bit_cast(float, (uint32_t)(127 + up) << 23), back = __builtin_bit_cast(float, (uint32_t)(127 - up) << 23);
         if (!row_ok) return;
-        f16x8* const wo = reinterpret_cast<f16x8*>(a.ws_o) + ((long long)p.item * a.used + wave) * (DB * 2 * 64) + lane;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -747,16 +754,16 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                 f16x8 w;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) w[j] = (_Float16)(o[db][8 * c + j] * scale);
-                wo[(db * 2 + c) * 64] = w;
+                put(o_rsrc, (db * 2 + c) * 1024 + lane * 16, __builtin_bit_cast(u32x4, w));
             }
-        if (half == 0) reinterpret_cast<f32x4*>(a.ws_ml)[((long long)p.item * a.used + wave) * 32 + l32] = f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, back, 0.f};
+        if (half == 0) put(ml_rsrc, l32 * 16, __builtin_bit_cast(u32x4, f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, back, 0.f}));
     } else if (row_ok) {
-        f32x4* const wo = reinterpret_cast<f32x4*>(a.ws_o) + ((long long)p.item * a.used + wave) * (DB * 4 * 64) + lane;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int v4 = 0; v4 < 4; ++v4) wo[(db * 4 + v4) * 64] = f32x4{o[db][4 * v4], o[db][4 * v4 + 1], o[db][4 * v4 + 2], o[db][4 * v4 + 3]};
-        if (half == 0) reinterpret_cast<f32x4*>(a.ws_ml)[((long long)p.item * a.used + wave) * 32 + l32] = f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, 1.f, 0.f};
+            for (int v4 = 0; v4 < 4; ++v4)
+                put(o_rsrc, (db * 4 + v4) * 1024 + lane * 16, __builtin_bit_cast(u32x4, f32x4{o[db][4 * v4], o[db][4 * v4 + 1], o[db][4 * v4 + 2], o[db][4 * v4 + 3]}));
+        if (half == 0) put(ml_rsrc, l32 * 16, __builtin_bit_cast(u32x4, f32x4{l > 0.f ? m_ref * a.c : -INFINITY, l, 1.f, 0.f}));
     }
 #endif
 }
