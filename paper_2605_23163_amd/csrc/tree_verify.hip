@@ -13,6 +13,8 @@
 // stats is bound by bytes, what is behind it by the latency of its launches and of the steps that depend on one another: 8 trees of 32 tokens,
 // V = 152064 in bf16, 32.4 us = stats 16.6 (4.7 TB/s), walk 6.0, weigh 5.4, pick 6.3, less what they overlap; 4 chains of 9 tokens, V = 50001 in
 // fp32 with draft_logits, 26.4 us = stats 5.7, walk 4.4, weigh 5.2 and 5.0, pick 6.2.
+// (walk in every workgroup of weigh, a launch less: 8 trees of 32 tokens 33.0 -> 31.0 us, but one of 16, V = 152064, 18.4 -> 20.8 and 2 of 200, V = 50001,
+// 29.5 -> 32.5: not kept.)
 // A test compares two numbers: fp32 exponentials decide it unless they are within 2^-15 of each other.  The draw compares with
 // V borders that lie as close as the smallest probabilities: an fp32 exponential's error, summed over the row, would move one draw in a
 // few hundred (V = 152064, logits of deviation 2) to a neighbouring entry, so these sums are fp64, and only one row a request needs them.
