@@ -18,20 +18,24 @@
 //     transposing LDS reads (ds_read_b64_tr_b16) need.  fp32: 32x32x2 instructions, tiles of 32 keys; V is read as it lies.
 //   * The softmax reference of a row rises only when a score passes it by more than 2^8: the accumulator is rarely rescaled.
 //   * A request whose tiles are one piece is normalised and written at once; otherwise pieces leave their sums and (m, l), which
-//     merge_kernel joins in the order of the pieces.  bf16 calls of more than 64 rows leave averages in fp16 times a power of two for the
-//     row: off by 2^-11 of themselves or 2^-39 of the row's largest, where the output is rounded to 2^-8, in half the bytes, which are as
-//     many as the keys' there (4 requests of 32 tokens and 4096 rows 27.4 -> 25.5 us).  Others leave fp32 sums (16 requests of one token and
-//     up to 8192 rows 40.7 us, and 41.6 in fp16: the conversion costs more than the bytes).
+//     merge_kernel joins in the order of the pieces.  bf16 calls leave averages in fp16 times a power of two for the row: off by 2^-11 of themselves or
+//     2^-39 of the row's largest, where the output is rounded to 2^-8, in half the bytes, which can be as many as the keys' (4 requests of 32
+//     tokens and 4096 rows 27.4 -> 25.5 us).  fp32 calls leave sums.
 //
 // Software pipeline (bf16): a step has the scores of tile t + 1 and, beside them in the same stretch of instructions, the softmax and O += P V of
-// tile t; requests for later tiles stand between the matrix instructions.  A step of whole tiles has no branch.
+// tile t; requests for later tiles stand between the matrix instructions.  A step of whole tiles has no branch.  Exponentials come in three
+// stages spread over the slots, none waiting for the one before (16 requests of 64 tokens and 16384 rows 251 -> 245 us).
 //
-// What bounds it (bf16, Hq / Hkv / D = 28 / 4 / 128).  Few rows: bytes behind a start of 5 us (lists, table, first requests) and the merge's launch:
-// 16 requests of one token and up to 8192 rows 41 us, of them the merge 5 (floor 32.5 at the rate of a large copy).  Middle: the same
-// start, 4 x 32 tokens, 4096 rows 23.5 us (attention 17, merge 6; MFMA busy 23 %).  Many rows: 16 x 64 tokens, 16384 rows 255 us, 950 TFLOP/s,
-// MFMA busy 55 % of the cycles at 1.7 to 1.85 GHz, which the chip's power leaves: a tile costs a SIMD 3080 cycles, 2048 of them MFMA, and
-// without the reads of LDS it would take 170 us.  64 rows a wavefront, which read LDS half as often, leave one wavefront a SIMD: 339 us.
-// fp32: 3 x up to 21 tokens, 2003 rows, 14 / 2 / 64: 17 us (attention 10.5, merge 6.5).
+// Few rows have four wavefronts all the same: one alone takes 100 cycles for each of the 32 requests of a tile.  16 requests of one token and up to 8192
+// rows, the attention alone 34.8 -> 29.6 us, 4 of 100 rows 12.1 -> 8.3.
+//
+// What bounds it (bf16, Hq / Hkv / D = 28 / 4 / 128).  Few rows: bytes, 5.7 TB/s in the attention, and the merge's launch: 16 requests of one token and
+// up to 8192 rows 40.4 us, of them attention 29.3, merge 5.5 (floor 32.5 at the rate of a large copy).  Middle: a start of 5 us (lists, table, first
+// requests): 4 x 32 tokens, 4096 rows 21.6 us (attention 16, merge 6).  Many rows: 16 x 64 tokens, 16384 rows 245 us, 985 TFLOP/s: the
+// clock that the chip's power leaves, 1.7 to 1.85 GHz, and reads of LDS, without which the loop took 170 us of 237.  64 rows a wavefront, which
+// read LDS half as often, leave one wavefront a SIMD: 339 us instead of 277 (as it was then).
+// fp32, matrix pipe: 3 x up to 21 tokens, 2003 rows, 14 / 2 / 64: 14.7 us (attention 10.5, merge 4.6).  16 x 1 token, 4096 rows, 28 / 4 / 128 82 us, floor
+// 52: one wavefront of four has rows, and 7 of them.
 #include <atomic>
 #include <type_traits>
 #include <utility>
@@ -688,7 +692,6 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
                     o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(*reinterpret_cast<const float*>(vp + db * 128), s[0][v], o[db], 0, 0, 0);
             }
         };
-        constexpr int LOADS = 2 * C::NI;
 #pragma unroll
         for (int i = 0; i < S - 1; ++i)
             if (t_begin + i < t_end) {
@@ -697,8 +700,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
             }
         int slot = 0;
         for (int t = t_begin; t < t_end; ++t) {
-            if (S == 3 && t + 1 < t_end) wait_loads<LOADS>();
-            else wait_loads<0>();
+            wait_loads<0>();
             wg_barrier();       // the tile is there, and everyone is done with the slot that the next one goes to
             if (t + S - 1 < t_end) {
                 fetch(is_k, t + S - 1, slot == 0 ? S - 1 : slot - 1);
@@ -776,8 +778,9 @@ struct MergeArgs {
     int Hq, max_mt, used;
 };
 
-// One wavefront per (request, KV head, M-tile, its 32-row wavefront, 16-byte column): lane = as in the accumulators.  Bound by latency:
-// up to 16 pieces are on their way at a time, and there are as many wavefronts as columns.
+// One wavefront, or SPLIT of them, per (request, KV head, M-tile, its 32-row wavefront, 16-byte column): lane = as in the accumulators.  Bound by
+// latency: up to 16 pieces are on their way at a time, and there are as many wavefronts as columns.  16 requests of one token and up to 8192 rows
+// 5.5 us; one of 32768 rows, 128 pieces a KV head, 7.6.
 template <typename T, int D, int WAVES, int SPLIT>
 __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
 {
