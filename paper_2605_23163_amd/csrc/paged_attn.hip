@@ -26,8 +26,8 @@
 // tile t; requests for later tiles stand between the matrix instructions.  A step of whole tiles has no branch.  Exponentials come in three
 // stages spread over the slots, none waiting for the one before (16 requests of 64 tokens and 16384 rows 251 -> 245 us).
 //
-// Few rows have four wavefronts all the same: one alone takes 100 cycles for each of the 32 requests of a tile.  16 requests of one token and up to 8192
-// rows, the attention alone 34.8 -> 29.6 us, 4 of 100 rows 12.1 -> 8.3.
+// Few rows have four wavefronts all the same, so that none makes a tile's 32 requests alone: 16 requests of one token and up to 8192 rows, the attention
+// without the merge, 34.8 -> 29.6 us, 4 of 100 rows 12.1 -> 8.3.
 //
 // What bounds it (bf16, Hq / Hkv / D = 28 / 4 / 128).  Few rows: bytes, 5.7 TB/s in the attention, and the merge's launch: 16 requests of one token and
 // up to 8192 rows 40.4 us, of them attention 29.3, merge 5.5 (floor 32.5 at the rate of a large copy).  Middle: a start of 5 us (lists, table, first

@@ -169,6 +169,14 @@ def test_a_long_cache():
     x.check(x.run())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Hq", [(8, 28), (5, 8), (13, 28), (9, 64)])
+def test_more_pieces_than_compute_units(dtype, B, Hq):
+    """Wavefronts of the second workgroups on a compute unit may have other rows; M-tiles of one to four wavefronts and of two M-tiles."""
+    x = Call(dtype, [2500, 1999, 2111, 64, 3000, 2345], B, Hq, 4, 128, 16, [B, B, B - 2, B, B, 1], "tree", seed=B)
+    x.check(x.run())
+
+
 def test_pages_beyond_32_bits():
     """A pool of 5 GB: the request's pages lie behind the first 2^32 bytes, and the same ones in front of them give the same result."""
     x = Call("bf16", [150, 3], 3, 8, 2, 128, 64, None, "causal", seed=9)
