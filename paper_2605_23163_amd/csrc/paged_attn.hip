@@ -427,7 +427,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 4 ? 2 : 1) void attn_kernel(Ar
     };
     constexpr int KB = KT / 32;
     // keys of tile t that the row does not see: whether there are any, and their scores out of the way
-    auto is_masked = [&](int t) { return t >= cache_tiles || (t + 1) * KT > len; };
+    const int first_token = fast_div(min(row0 + wave * 32, rows - 1), a.cut.dG);
+    auto is_masked = [&](int t) {
+        if (t < cache_tiles) return (t + 1) * KT > len;
+        const int end = (t - cache_tiles + 1) * KT;
+        return end > count || bits || (a.causal && end - 1 > first_token);
+    };
     auto mask_scores = [&](int t, f32x16 (&s)[KB]) __attribute__((always_inline)) {
         const bool cache = t < cache_tiles;
         const int key0 = cache ? t * KT : (t - cache_tiles) * KT;
