@@ -609,8 +609,9 @@ fdd_status fdd_paged_attn(const fdd_paged_cache *cache, const fdd_paged_attn_par
  * temperature 0 they have no part.  Only rows of tokens that are there are read, of draft_logits only those that another
  * token follows.  Tokens outside [0, V) never stand (with q(x) = 1 they take nothing out).  Uniforms are in [0, 1).
  *
- * Tests and chances are taken in fp32 (a probability is off by 2^-15 of itself, for logits within 2^7 temperatures of the
- * largest); what the last token is drawn from is summed in fp64.  Logits: finite values and -inf for entries that can never be
+ * In a test or a chance p(x) and q(x) are off by 2^-16 of themselves, however small they are, and W, without draft_logits, by 2^-16 of
+ * what was taken out of it (a row's fp32 exponentials are summed in fp64, all else is fp64; chances are rounded to fp32); what the last token is
+ * drawn from is fp64 throughout.  Logits: finite values and -inf for entries that can never be
  * chosen, a row that is read needs one finite entry.  NaN and +inf are not supported: such a request's outputs are undefined
  * (ids stay in range).  Outputs overlap nothing.
  */

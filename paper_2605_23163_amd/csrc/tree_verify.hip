@@ -15,9 +15,14 @@
 // fp32 with draft_logits, 26.4 us = stats 5.7, walk 4.4, weigh 5.2 and 5.0, pick 6.2.
 // (walk in every workgroup of weigh, a launch less: 8 trees of 32 tokens 33.0 -> 31.0 us, but one of 16, V = 152064, 18.4 -> 20.8 and 2 of 200, V = 50001,
 // 29.5 -> 32.5: not kept.)
-// A test compares two numbers: fp32 exponentials decide it unless they are within 2^-15 of each other.  The draw compares with
-// V borders that lie as close as the smallest probabilities: an fp32 exponential's error, summed over the row, would move one draw in a
-// few hundred (V = 152064, logits of deviation 2) to a neighbouring entry, so these sums are fp64, and only one row a request needs them.
+// A test compares a probability with what the children that fell have left of the row.  stats takes fp32 exponentials and adds them in fp64, the
+// tokens' own exponentials and all that walk does with them are fp64: a probability is off by what the row's sum is, 2^-16 of itself at
+// most, however small it is.  (An entry a octaves below the reference has an exponent of three roundings, 3 ln2 a 2^-24 of the entry, and a
+// row's entries are log2 V octaves below on average, their weights counted, at most; 2^-22.4 for the sums of 8, 2^-23 for the exponential and for each time
+// that the reference moves, by 8 octaves and more in a thread; then the threads', wavefronts' and pieces' references, whose distances add up once more.)
+// What is left, one less the probabilities that fell, is off by 2^-16 of what fell.
+// The draw compares with V borders that lie as close as the smallest probabilities: an fp32 exponential's error, summed over the row, would move one draw in a
+// few hundred (V = 152064, logits of deviation 2) to a neighbouring entry, so these exponentials are fp64 too, and only one row a request needs them.
 #include <cfloat>
 
 #include "paged.h"
@@ -33,7 +38,7 @@ constexpr double LOG2E = 1.4426950408889634074;
 constexpr double NOTHING_LEFT = 0x1p-40;
 
 struct Stat {        // of a piece of a row
-    float max;
+    float max;       // (not greedy: the reference, up to 8 octaves of the exponentials below the largest)
     int arg;         // greedy: lowest id of the largest
     double sum;      // of exp((x - max) / temperature)
 };
@@ -66,6 +71,7 @@ struct Args {
     int N, B, V, pieces, per_piece;       // per_piece: entries, a multiple of 8
     int w_pieces, w_per;                  // of the row that is drawn from
     float c, draft_c;                     // log2(e) / temperature
+    float slack, draft_slack;             // 8 octaves
     double c64, draft_c64;
 };
 
@@ -99,6 +105,8 @@ __device__ __forceinline__ void entries(const T* p, float (&x)[16 / sizeof(T)])
     }
 }
 
+__device__ __forceinline__ double exponential(float x, double top, double c) { return exp2(((double)x - top) * c); }
+
 __device__ __forceinline__ double wave_sum(double x)
 {
 #pragma unroll
@@ -111,16 +119,18 @@ template <typename T, bool GREEDY>
 __global__ __launch_bounds__(STAT_THREADS) void stats_kernel(Args a)
 {
     constexpr int VE = 16 / sizeof(T);
-    __shared__ float s_max[STAT_THREADS / 64], s_sum[STAT_THREADS / 64];
+    __shared__ float s_max[STAT_THREADS / 64];
+    __shared__ double s_sum[STAT_THREADS / 64];
     __shared__ int s_arg[STAT_THREADS / 64];
     const int piece = blockIdx.x % a.pieces, row = blockIdx.x / a.pieces, which = blockIdx.y;
     const int n = row / a.B, i = row - n * a.B;
     const int count = count_of(a, n);
     if (i >= count || (which && i + 1 >= count)) return;       // (a draft's last row has no token behind it)
     const T* const x = static_cast<const T*>(which ? a.draft : a.logits) + (long long)row * a.V;
-    const float c = which ? a.draft_c : a.c;
+    const float c = which ? a.draft_c : a.c, slack = which ? a.draft_slack : a.slack;
     const int v0 = piece * a.per_piece, v1 = min(v0 + a.per_piece, a.V);
-    float m = -FLT_MAX, s = 0.f;          // (never above the entries, but for -inf, which weighs nothing)
+    float m = -FLT_MAX;          // (never above the entries, but for -inf, which weighs nothing)
+    double s = 0.0;
     int arg = v0;
     bool any = false;
     auto take = [&](const float* y, int count_y, int v) {
@@ -138,11 +148,13 @@ __global__ __launch_bounds__(STAT_THREADS) void stats_kernel(Args a)
                 any = true;
             }
         } else {
-            if (best > m) {
-                s *= __builtin_amdgcn_exp2f((m - best) * c);
+            if (best > m + slack) {       // (rarely: each time rounds the sum)
+                s *= (double)__builtin_amdgcn_exp2f((m - best) * c);
                 m = best;
             }
-            for (int j = 0; j < count_y; ++j) s += __builtin_amdgcn_exp2f((y[j] - m) * c);
+            float few = 0.f;
+            for (int j = 0; j < count_y; ++j) few += __builtin_amdgcn_exp2f((y[j] - m) * c);
+            s += (double)few;
         }
     };
     const int whole = v0 + (v1 - v0) / VE * VE;
@@ -158,13 +170,14 @@ __global__ __launch_bounds__(STAT_THREADS) void stats_kernel(Args a)
     if (GREEDY && !any) m = -INFINITY, arg = a.V;          // (a thread without entries)
     // join the threads
     for (int d = 1; d < 64; d *= 2) {
-        const float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d);
+        const float m2 = __shfl_xor(m, d);
         const int arg2 = __shfl_xor(arg, d);
         if constexpr (GREEDY) {
             if (m2 > m || (m2 == m && arg2 < arg)) m = m2, arg = arg2;
         } else {
+            const double s2 = __shfl_xor(s, d);
             const float top = fmaxf(m, m2);
-            s = s * __builtin_amdgcn_exp2f((m - top) * c) + s2 * __builtin_amdgcn_exp2f((m2 - top) * c);
+            s = s * (double)__builtin_amdgcn_exp2f((m - top) * c) + s2 * (double)__builtin_amdgcn_exp2f((m2 - top) * c);
             m = top;
         }
     }
@@ -175,7 +188,7 @@ __global__ __launch_bounds__(STAT_THREADS) void stats_kernel(Args a)
     double sum = 0.0;
     for (int w = 0; w < STAT_THREADS / 64; ++w)
         if (GREEDY ? s_max[w] > m || (s_max[w] == m && s_arg[w] < arg) : s_max[w] > m) m = s_max[w], arg = s_arg[w];
-    for (int w = 0; w < STAT_THREADS / 64; ++w) sum += (double)(s_sum[w] * __builtin_amdgcn_exp2f((s_max[w] - m) * c));
+    for (int w = 0; w < STAT_THREADS / 64; ++w) sum += s_sum[w] * (double)__builtin_amdgcn_exp2f((s_max[w] - m) * c);
     Stat r;
     r.max = m;
     r.arg = min(arg, a.V - 1);
@@ -191,7 +204,8 @@ __global__ __launch_bounds__(WALK_THREADS) void walk_kernel(Args a)
     __shared__ float s_max[2][FDD_TREE_MAX];
     __shared__ double s_sum[2][FDD_TREE_MAX];
     __shared__ int s_arg[FDD_TREE_MAX], s_token[FDD_TREE_MAX], s_parent[FDD_TREE_MAX];
-    __shared__ float s_p[FDD_TREE_MAX], s_q[FDD_TREE_MAX], s_u[FDD_TREE_MAX];      // of a token, under its parent's rows
+    __shared__ double s_p[FDD_TREE_MAX], s_q[FDD_TREE_MAX];      // of a token, under its parent's rows
+    __shared__ float s_u[FDD_TREE_MAX];
     const int n = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool draft = !GREEDY && a.draft;
     const long long row0 = (long long)n * a.B;
@@ -240,43 +254,43 @@ __global__ __launch_bounds__(WALK_THREADS) void walk_kernel(Args a)
     }
     __syncthreads();
     if (j < a.B) {
-        float p = 0.f, q = 1.f, chance = there && j == 0 ? 1.f : 0.f;
+        double p = 0.0, q = 1.0, chance = there && j == 0 ? 1.0 : 0.0;
         if (there && parent >= 0 && inside) {
             if constexpr (GREEDY) {
-                p = token == s_arg[parent] ? 1.f : 0.f;
+                p = token == s_arg[parent] ? 1.0 : 0.0;
             } else {
-                p = (float)((double)__builtin_amdgcn_exp2f((of_p - s_max[0][parent]) * a.c) / s_sum[0][parent]);
-                if (draft) q = (float)((double)__builtin_amdgcn_exp2f((of_q - s_max[1][parent]) * a.draft_c) / s_sum[1][parent]);
+                p = exponential(of_p, s_max[0][parent], a.c64) / s_sum[0][parent];
+                if (draft) q = exponential(of_q, s_max[1][parent], a.draft_c64) / s_sum[1][parent];
             }
-            chance = draft && q > 0.f ? fminf(1.f, p / q) : draft && p > 0.f ? 1.f : fminf(1.f, p);
+            chance = draft && q > 0.0 ? fmin(1.0, p / q) : draft && p > 0.0 ? 1.0 : fmin(1.0, p);
         }
-        if (a.chances) a.chances[row0 + j] = chance;
+        if (a.chances) a.chances[row0 + j] = (float)chance;
         // a token that an earlier child of the same parent has is no longer there when it is tried
         bool again = false;
         if (!draft && !GREEDY && there && parent >= 0)
             for (int i = parent + 1; i < j; ++i) again = again || (s_parent[i] == parent && s_token[i] == token);
-        s_p[j] = again ? 0.f : p;
+        s_p[j] = again ? 0.0 : p;
         s_q[j] = q;
     }
     __syncthreads();
     if (wave) return;
     // children have higher numbers than their parent and are tried in order, so one pass over the tokens meets all of them
     int now = 0, steps = 0;        // (uniform)
-    float left = 1.f;              // of p, behind the children that fell
+    double left = 1.0;             // of p, behind the children that fell
     for (int j0 = 0; j0 < count; j0 += 64) {
         const int k = j0 + lane;
         const bool here = k > 0 && k < count;
         const int up = here ? s_parent[k] : -1, x = here ? s_token[k] : -1;
-        const float p = here ? s_p[k] : 0.f, q = here ? s_q[k] : 1.f, v = here ? s_u[k] : 0.f;
+        const double p = here ? s_p[k] : 0.0, uq = here ? (double)s_u[k] * s_q[k] : 0.0;
         int from = j0;
         for (;;) {
             const uint64_t tried = __builtin_amdgcn_ballot_w64(here && up == now && k >= from);
             if (tried == 0) break;
             const int l = __builtin_ctzll(tried);
-            auto of = [&](float y) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, y), l)); };
-            const float p_l = of(p), q_l = of(q), u_l = of(v);
+            auto of = [&](double y) { return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(y), l), __builtin_amdgcn_readlane(__double2loint(y), l)); };
+            const double p_l = of(p), uq_l = of(uq);
             from = j0 + l + 1;
-            const bool stands = GREEDY ? p_l > 0.f : u_l * q_l * left < p_l;
+            const bool stands = GREEDY ? p_l > 0.0 : uq_l * left < p_l;
             if (stands) {
                 now = j0 + l;
                 if (lane == l) {
@@ -284,7 +298,7 @@ __global__ __launch_bounds__(WALK_THREADS) void walk_kernel(Args a)
                     a.path[row0 + steps + 1] = k;
                 }
                 ++steps;
-                left = 1.f;
+                left = 1.0;
             } else {
                 left -= p_l;
             }
@@ -362,7 +376,6 @@ struct Weights {
             for (int i = 0; i < PICK; ++i) x[i] = v + i < V ? entry(row + v + i) : -INFINITY;
         }
     }
-    __device__ __forceinline__ static double exponential(float x, double top, double c) { return exp2(((double)x - top) * c); }
     // bits of the entries at v that were children's
     __device__ __forceinline__ uint32_t taken(int v) const
     {
@@ -495,15 +508,15 @@ __global__ __launch_bounds__(STAT_THREADS) void weigh_kernel(Args a)
         if (w.residue) w.read(w.q, v, y);
         if constexpr (RESIDUE) {
 #pragma unroll
-            for (int i = 0; i < PICK; ++i) left += fmax(w.exponential(x[i], w.p_max, w.p_c) * w.p_scale - w.exponential(y[i], w.q_max, w.q_c) * w.q_scale, 0.0);
+            for (int i = 0; i < PICK; ++i) left += fmax(exponential(x[i], w.p_max, w.p_c) * w.p_scale - exponential(y[i], w.q_max, w.q_c) * w.q_scale, 0.0);
         } else {
             const uint32_t taken = w.taken(v);
 #pragma unroll
             for (int i = 0; i < PICK; ++i) {
-                const double e = w.exponential(x[i], w.p_max, w.p_c);
+                const double e = exponential(x[i], w.p_max, w.p_c);
                 all += e;
                 left += taken >> i & 1 ? 0.0 : e;
-                if (w.residue) other += w.exponential(y[i], w.q_max, w.q_c);
+                if (w.residue) other += exponential(y[i], w.q_max, w.q_c);
             }
         }
     }
@@ -562,8 +575,8 @@ __global__ __launch_bounds__(STAT_THREADS) void pick_kernel(Args a)
             const uint32_t taken = w.residue ? 0u : w.taken(v);
 #pragma unroll
             for (int i = 0; i < PICK; ++i) {
-                const double e = w.exponential(p[i], w.p_max, w.p_c);
-                x[i] = w.residue ? fmax(e * w.p_scale - w.exponential(q[i], w.q_max, w.q_c) * w.q_scale, 0.0) : taken >> i & 1 ? 0.0 : e;
+                const double e = exponential(p[i], w.p_max, w.p_c);
+                x[i] = w.residue ? fmax(e * w.p_scale - exponential(q[i], w.q_max, w.q_c) * w.q_scale, 0.0) : taken >> i & 1 ? 0.0 : e;
             }
         } else {
 #pragma unroll
@@ -715,10 +728,12 @@ fdd_status fdd_tree_verify(const fdd_tree_verify_params* p)
     if (!greedy) {
         a.c64 = LOG2E / (double)p->temperature;
         a.c = (float)a.c64;
+        a.slack = 8.f / a.c;
     }
     if (a.draft) {
         a.draft_c64 = LOG2E / (double)p->draft_temperature;
         a.draft_c = (float)a.draft_c64;
+        a.draft_slack = 8.f / a.draft_c;
     }
     const hipStream_t s = static_cast<hipStream_t>(p->stream);
     const hipError_t e = p->dtype == FDD_BF16 ? launch<uint16_t>(a, greedy, s) : launch<float>(a, greedy, s);
