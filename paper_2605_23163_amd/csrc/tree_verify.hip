@@ -671,7 +671,7 @@ fdd_status check_shape(const fdd_tree_verify_params* p)
     if (p->V > (1ll << 30)) return fail(FDD_ERR_SHAPE, "%s: V must be at most 2^30", kFn);
     // (a launch has at most 2^32 threads: 256 for each piece of a row, 1024 for a request)
     if (p->N >= (1 << 22) || (long long)p->N * p->B >= (1ll << 24)) return fail(FDD_ERR_SHAPE, "%s: N or N*B too large", kFn);
-    if (p->N * ((p->V + STAT_THREADS * PICK - 1) / (STAT_THREADS * PICK)) >= (1ll << 24)) return fail(FDD_ERR_SHAPE, "%s: N*V too large", kFn);
+    if ((long long)p->N * make_plan(*p).w_pieces >= (1ll << 24)) return fail(FDD_ERR_SHAPE, "%s: N*V too large", kFn);
     if (p->dtype != FDD_F32 && p->dtype != FDD_BF16) return fail(FDD_ERR_DTYPE, "%s: dtype %d is neither FDD_F32 nor FDD_BF16", kFn, p->dtype);
     if (p->reserved != 0) return fail(FDD_ERR_UNSUPPORTED, "%s: reserved field must be 0", kFn);
     if (p->temperature != 0.f && !in_range(p->temperature)) return fail(FDD_ERR_UNSUPPORTED, "%s: temperature must be 0 (greedy) or from 2^-20 to 2^20", kFn);
