@@ -561,7 +561,9 @@ fdd_status fdd_tree_mask(const fdd_tree_mask_params *p);
  * products and sums.  The order of sums depends on lens, n_tokens and max_len of all requests, and on nothing else.
  *
  * Values: q, k and v finite, scores within fp32's range, for what is seen; keys that a row does not see may hold anything.  A NaN
- * or an infinity in V of a token that is there, or in a cached row, reaches all rows of its request and KV head.
+ * or an infinity in V of a token that is there, or in a cached row, reaches all rows of its request and KV head.  FDD_F32 passes a
+ * NaN or an infinity in q or in a key on as arithmetic gives it, to the rows that see it (a row whose scores are all -inf is 0).
+ * FDD_BF16: such rows are undefined.
  */
 typedef struct fdd_paged_attn_params {
     int32_t B, Hq;

@@ -27,7 +27,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + os.path.j
 # The bf16 attention and vocabulary kernels produce no NaN from finite inputs (masked
 # scores are -inf and every inf - inf is avoided by construction), so max/min need no NaN
 # quieting there; the kernels of log probabilities write the NaN of a row
-# without entries as bits.  The fp32 attention kernel passes the caller's NaN and infinities on.
+# without entries as bits.  The fp32 attention kernels (attn_f32.hip, paged_attn_f32.hip) pass the caller's NaN and infinities on.
 EXTRA = {"attn_bf16.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
          "logprobs.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
          "paged_attn.hip": ["-fno-honor-nans", "-mno-amdgpu-ieee"],
