@@ -460,7 +460,9 @@ typedef struct fdd_rope_table {
  * lie `stride` elements apart (0 = dense); heads and channels of a row are dense.  q_out may be q itself with the same stride (in
  * place), and k_out k; otherwise no output overlaps anything.  Any alignment of the type; 16-byte aligned rows and a rot_dim
  * whose half is a multiple of 16 bytes are faster.  rows = 0 is a call that does nothing.
- * FDD_ROPE_INVERSE turns the other way, by the same magnitude: the gradient of the rows with respect to what was rotated. */
+ * FDD_ROPE_INVERSE turns the other way, by the same magnitude: the gradient of the rows with respect to what was rotated.
+ * A row has one position.  Rows of several (time, row and column of an image's token), each with pairs of its own, take a call in
+ * place for each, whose table has 0 for the frequencies of the other pairs, which stay as they are (and magnitude 1 in all calls but one). */
 #define FDD_ROPE_INVERSE 1
 typedef struct fdd_rope_params {
     int32_t rows, Hq, Hk, D;       /* Hk: heads of k, ignored where k is NULL; D at most 1024 */
