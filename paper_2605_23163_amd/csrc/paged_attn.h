@@ -6,8 +6,10 @@
 //     help to bring it.
 //   * Keys come in tiles: those of the cache, then those of the request's own tokens.  How many a request has is known on the
 //     device only (lens, n_tokens): each workgroup works out for itself, from these two lists, how many tiles there are in
-//     all, how many of them a piece gets so that all pieces together are as many as the chip takes at once, and which
-//     piece is its own (`Cutting`).  A long request is cut into more pieces than a short one; the host only knows a bound.
+//     all, how many of them a piece gets, all over the W workgroups that the chip takes at once, and which
+//     piece is its own (`Cutting`).  A long request is cut into more pieces than a short one; the host only knows a bound.  Both quotients are
+//     rounded up, a piece's tiles and an M-tile's pieces, so that there are up to W + M-tiles pieces, and those beyond W wait for the others: with 64
+//     tokens and 8192 rows 8 requests are 256 pieces of 33 tiles for W = 256, 74 us, 6 are 288 of 22, 86 us.
 //   * Scores are produced transposed, S^T = K Q^T, with 32x32 matrix instructions: each lane then owns one query row
 //     (lane % 32) and half of the keys, so that maximum and sum of the streaming softmax are in-lane reductions plus
 //     one exchange between the halves, and the same registers are the B operand of O^T += V^T P^T.
@@ -19,8 +21,12 @@
 //   * The softmax reference of a row rises only when a score passes it by more than 2^8: the accumulator is rarely rescaled.
 //   * A request whose tiles are one piece is normalised and written at once; otherwise pieces leave their sums and (m, l), which
 //     merge_kernel joins in the order of the pieces.  bf16 calls leave averages in fp16 times a power of two for the row: off by 2^-11 of themselves or
-//     2^-39 of the row's largest, where the output is rounded to 2^-8, in half the bytes, which can be as many as the keys' (4 requests of 32
-//     tokens and 4096 rows 27.4 -> 25.5 us).  fp32 calls leave sums.
+//     2^-39 of the row's largest, where the output is rounded to 2^-8, in half the bytes, which can be as many as the keys'.  fp32 sums in their place
+//     take 1 % or less off the error in norm (16 requests of one token 2.32e-3 -> 2.31e-3) and cost, us from a graph: 4 requests of 32 tokens and 4096 rows 23.3 -> 25.5,
+//     16 of 8 and 8192 57.0 -> 60.8, 64 of one token and 1024 33.4 -> 34.9; 16 of one token and up to 8192 41.1 -> 40.7, one of 32768 22.6 -> 21.8.
+//     fp32 calls leave sums.
+//   * bf16 probabilities are rounded to bf16, which is what the matrix instructions take (summed as rounded): that and the output's rounding, 1.7e-3 in norm,
+//     make 2.2e-3 to 2.4e-3 against 64 bits.
 //
 // Software pipeline (bf16): a step has the scores of tile t + 1 and, beside them in the same stretch of instructions, the softmax and O += P V of
 // tile t; requests for later tiles stand between the matrix instructions.  A step of whole tiles has no branch.  Exponentials come in three
@@ -29,13 +35,15 @@
 // Few rows have four wavefronts all the same, so that none makes a tile's 32 requests alone: 16 requests of one token and up to 8192 rows, the attention
 // without the merge, 34.8 -> 29.6 us, 4 of 100 rows 12.1 -> 8.3.
 //
-// What bounds it (bf16, Hq / Hkv / D = 28 / 4 / 128).  Few rows: bytes, 5.7 TB/s in the attention, and the merge's launch: 16 requests of one token and
-// up to 8192 rows 40.4 us, of them attention 29.3, merge 5.5 (floor 32.5 at the rate of a large copy).  Middle: a start of 5 us (lists, table, first
-// requests): 4 x 32 tokens, 4096 rows 21.6 us (attention 16, merge 6).  Many rows: 16 x 64 tokens, 16384 rows 245 us, 985 TFLOP/s: the
+// What bounds it (bf16, Hq / Hkv / D = 28 / 4 / 128).  Few rows: bytes, 5.6 TB/s in the attention, and the merge's launch: 16 requests of one token and
+// up to 8192 rows 40.5 us, of them attention 29.7, merge 5.5 (floor 32.5 at the rate of a large copy).  Middle: a start of 5 us (lists, table, first
+// requests): 4 x 32 tokens, 4096 rows 22.6 us (attention 16.2, merge 6.7).  Many rows: 16 x 64 tokens, 16384 rows 245 to 260 us, 985 to 928 TFLOP/s from card to card: the
 // clock that the chip's power leaves, 1.7 to 1.85 GHz, and reads of LDS, without which the loop took 170 us of 237.  64 rows a wavefront, which
 // read LDS half as often, leave one wavefront a SIMD: 339 us instead of 277 (as it was then).
-// fp32, matrix pipe: 3 x up to 21 tokens, 2003 rows, 14 / 2 / 64: 14.7 us (attention 10.5, merge 4.6).  16 x 1 token, 4096 rows, 28 / 4 / 128 82 us, floor
-// 52: one wavefront of four has rows, and 7 of them.
+// A prompt in one call: pieces are dealt as if every token saw all, and tiles of the request's own tokens take the steps with branches: 2048 tokens in order, no cache, 88 us
+// (floor 25), each seeing all 95 (50), 2 x 512 behind 4096 rows 102 (53).
+// fp32, matrix pipe: 3 x up to 21 tokens, 2003 rows, 14 / 2 / 64: 14.7 us (attention 10.5, merge 4.5).  16 x 1 token, 4096 rows, 28 / 4 / 128 83 us, floor
+// 52: one wavefront of four has rows, and 7 of them.  A prompt of 1024 tokens in order 147 us, floor 49.
 #pragma once
 #include <atomic>
 #include <type_traits>
@@ -786,7 +794,7 @@ struct MergeArgs {
 
 // One wavefront, or SPLIT of them, per (request, KV head, M-tile, its 32-row wavefront, 16-byte column): lane = as in the accumulators.  Bound by
 // latency: up to 16 pieces are on their way at a time, and there are as many wavefronts as columns.  16 requests of one token and up to 8192 rows
-// 5.5 us; one of 32768 rows, 128 pieces a KV head, 7.6.
+// 5.5 us; one of 32768 rows, 103 pieces a KV head, 7.4.
 template <typename T, int D, int WAVES, int SPLIT>
 __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
 {
@@ -933,7 +941,8 @@ inline Plan make_plan(const fdd_paged_cache& c, const fdd_paged_attn_params& p)
     Plan pl;
     const long long rows = (long long)p.B * (p.Hq / c.Hkv);
     // Four wavefronts up to 128 rows, and up to 256 where there are few (request, KV head) pairs: more, shorter pieces start sooner than keys are brought
-    // twice (us, 4 wavefronts and 8: 8 requests of 224 rows, 2048 keys 23.6 and 24.8, 4 of 4096 24.4 and 25.2; 16 of 16384 150 and 145, 64 of 2048 100 and 87).
+    // twice (us, 4 wavefronts and 8: 8 requests of 224 rows, 2048 keys 23.6 and 24.8, 4 of 4096 24.4 and 25.2; 16 of 16384 150 and 145, 64 of 2048 100 and 87; numbers of
+    // requests whose pieces are W and no more in either form).
     pl.waves = rows <= 128 || (rows <= 256 && c.N * c.Hkv <= 32) || c.dtype == FDD_F32 ? 4 : 8;
     pl.used = rows < pl.waves * 32 ? (int)((rows + 31) / 32) : pl.waves;
     pl.kt = c.dtype == FDD_BF16 ? 64 : 32;
@@ -977,7 +986,7 @@ hipError_t launch(const fdd_paged_cache& c, const fdd_paged_attn_params& p, cons
     if (e != hipSuccess || !pl.partials) return e;
     MergeArgs m = {a.cut, a.ws_o, a.ws_ml, p.out, p.Hq, pl.max_mt, pl.used};
     const long long mtiles = (long long)c.N * c.Hkv * pl.max_mt, jobs = mtiles * pl.used * C::COLS, pieces = pl.W / mtiles;
-    // A request's many pieces: four wavefronts a job (one request of a token and 32768 rows, 128 pieces a KV head, 32.7 -> 22.7 us; 16 wavefronts
+    // A request's many pieces: four wavefronts a job (one request of a token and 32768 rows, 103 pieces a KV head, 32.7 -> 22.7 us; 16 wavefronts
     // 23.7; 4 requests of 32 tokens, 13 pieces, 24.8 and 26.0)
     if (pieces < 24) merge_kernel<T, D, WAVES, 1><<<dim3((unsigned)((jobs + 3) / 4)), 256, 0, s>>>(m);
     else merge_kernel<T, D, WAVES, 4><<<dim3((unsigned)jobs), 256, 0, s>>>(m);

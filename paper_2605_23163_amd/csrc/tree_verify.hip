@@ -11,10 +11,10 @@
 //           (a chain with draft_logits: both rows' sums, and in a launch behind it those of max(p - q, 0))
 //   pick    the piece that the uniform falls into, entry by entry
 // stats is bound by bytes, what is behind it by the latency of its launches and of the steps that depend on one another: 8 trees of 32 tokens,
-// V = 152064 in bf16, 32.4 us = stats 16.6 (4.7 TB/s), walk 6.0, weigh 5.4, pick 6.3, less what they overlap; 4 chains of 9 tokens, V = 50001 in
-// fp32 with draft_logits, 26.4 us = stats 5.7, walk 4.4, weigh 5.2 and 5.0, pick 6.2.
+// V = 152064 in bf16, 33.1 us = stats 17.0 (4.6 TB/s), walk 6.3, weigh 5.3, pick 6.1, less what they overlap; 4 chains of 9 tokens, V = 50001 in
+// fp32 with draft_logits, 27.2 us = stats 6.0, walk 4.8, weigh 5.2 and 4.9, pick 6.1.  Greedy, from a graph: the same trees 19.6 us, the chains 8.4.
 // (walk in every workgroup of weigh, a launch less: 8 trees of 32 tokens 33.0 -> 31.0 us, but one of 16, V = 152064, 18.4 -> 20.8 and 2 of 200, V = 50001,
-// 29.5 -> 32.5: not kept.)
+// 29.5 -> 32.5, as they were then: not kept.)
 // A test compares a probability with what the children that fell have left of the row.  stats takes fp32 exponentials and adds them in fp64, the
 // tokens' own exponentials and all that walk does with them are fp64: a probability is off by what the row's sum is, 2^-16 of itself at
 // most, however small it is.  (An entry a octaves below the reference has an exponent of three roundings, 3 ln2 a 2^-24 of the entry, and a
